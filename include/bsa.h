@@ -324,6 +324,105 @@ BSA_API bsa_status_t bsa_mask_stats_noalloc(const uint8_t* mask_dev, int heads, 
                                     int64_t* stats_out_dev, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Positions and windows -- what a model computes around the block-sparse forward, at token granularity: rotary positions
+ * of Q and K, and attention whose mask is a window around each query plus a few first tokens (no counterpart in the
+ * paper).  Both take strided tensors, so that views of a fused projection or of a longer cache need no copy, and keep
+ * no state between calls: no plan, nothing to destroy, any number of calls at once on any streams, recordable into a
+ * CUDA graph.
+ *
+ * A view: element strides of a tensor [batch][heads][rows][d]; d is contiguous.  data must lie on a 16-byte boundary and
+ * every stride of a dimension with more than one entry must be a positive multiple of 8 elements (16 bytes), else
+ * INVALID_ARG (GPU untouched); strides of dimensions with one entry are ignored.  Entries of an output may not overlap.
+ */
+typedef struct bsa_view {
+    void* data;
+    int64_t batch, head, row;
+} bsa_view_t;
+
+/* How the channels of a head pair up, in the first R of them (R = sum of axis_dim): (2i, 2i+1) or (i, i + R/2). */
+enum { BSA_PAIRS_INTERLEAVED = 0, BSA_PAIRS_HALVES = 1 };
+#define BSA_MAX_AXES 4
+
+/* ---------------------------------------------------------------------------------------------
+ * bsa_rope -- rotary positions with one to four axes (time, height, width of a clip's latent tokens; one axis: text).
+ *
+ * Pair i of a token's R/2 channel pairs belongs to one axis a(i): the first axis_dim[0]/2 pairs to axis 0, the next
+ * axis_dim[1]/2 to axis 1, and so on.  The pair (x, y) becomes (x cos t - y sin t, x sin t + y cos t) with
+ * t = pos[a(i)] * freq[i]; channels from R on stay as they are.  The same rotation goes to every head of Q and of K.
+ *   freq[i]: freq_host[i] if given (R/2 values, host memory, read during the call); else theta^(-2 i' / axis_dim[a]) with i'
+ *   counted from the axis's first pair, or, with shared_freq, theta^(-2 i / R).
+ *   pos: pos_dev[b][n][a] if given (int32, device memory, [batch][N][n_axes], pos_batch elements between batch entries,
+ *   0: one set for all); else tokens first .. first + prod(grid) - 1 stand on the grid, row-major with the last axis
+ *   fastest, shifted by origin[a], and all other tokens (text in front or behind, padding) stay as they are.
+ * inverse = 1 rotates by -t: the gradient of the rotation's input from its output's (the rotation is orthogonal).
+ * Angles are taken modulo one turn in 64-bit fixed point before anything is rounded, so that they hold at any int32
+ * position; products and sums are fp32, rounded once to the element type.
+ * Outputs may be the inputs themselves (same data and strides); any other overlap is not allowed.
+ * Errors: INVALID_ARG (null or misaligned pointers, sizes below one, odd axis_dim, R > d, a grid that does not fit into N
+ * tokens), UNSUPPORTED (d not a multiple of 8 or above 256, N above 2^29), CUDA.
+ */
+typedef struct bsa_rope_desc {
+    int32_t batch, heads, heads_kv, d;  /* heads_kv: heads of K, 0: there is no K                      */
+    int64_t N;
+    int32_t dtype;                      /* BSA_DTYPE_*                                                 */
+    int32_t n_axes;                     /* 1 .. BSA_MAX_AXES                                           */
+    int32_t axis_dim[BSA_MAX_AXES];     /* channels of each axis, even (0: the axis rotates nothing)   */
+    int32_t pairs;                      /* BSA_PAIRS_*                                                 */
+    int32_t shared_freq;
+    int32_t inverse;
+    int32_t reserved;                   /* 0                                                           */
+    double theta;                       /* > 0 unless freq_host is given                               */
+    const double* freq_host;            /* finite values, or NULL                                      */
+    const int32_t* pos_dev;             /* or NULL: the grid                                           */
+    int64_t pos_batch;
+    int64_t first;                      /* >= 0                                                        */
+    int32_t grid[BSA_MAX_AXES];         /* >= 1 each (entries from n_axes on are ignored)              */
+    int32_t origin[BSA_MAX_AXES];
+} bsa_rope_desc_t;
+BSA_API bsa_status_t bsa_rope(const bsa_rope_desc_t* desc, const bsa_view_t* Q, const bsa_view_t* K /* may be NULL */,
+                              const bsa_view_t* Q_out, const bsa_view_t* K_out /* may be NULL */, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * bsa_window_forward / bsa_window_backward -- attention over a sliding window and a few first tokens ("sinks").
+ *
+ * Row i of a sequence's N queries stands at position p = q_start + i of its kv_len keys.  It sees the keys j with
+ *     j <= p + right   and   ( j >= p - left   or   j < sinks ),      0 <= j < kv_len,
+ * so right = 0 is causal, and sinks lift the left limit only.  A row at no position of its sequence (p < 0 or
+ * p >= kv_len: padding) sees nothing: O = 0, LSE = -inf, and it adds nothing to any gradient.
+ *     S = scale * q . k,   LSE = log sum exp S,   O = sum exp(S - LSE) v      over the keys that the row sees.
+ * Query head h reads key head h / (heads / heads_kv).  Keys that no row of a 256-row tile sees (beyond kv_len, left of the
+ * window) may hold anything, NaN included; a key that some row of a tile sees and another does not has to be finite for the
+ * other's sake (its weight there is zero).
+ *   Scores, softmax and accumulators are fp32; P (and dS in the backward) is rounded to the element type for its product,
+ *   outputs are rounded once.  No atomics touch a result: the same call gives the same bits.
+ * Forward: writes O [batch, heads, N, d] and LSE (fp32, contiguous [batch][heads][N], natural log).
+ * Backward: from Q, K, V, the forward's O and LSE and the gradient dO of O,
+ *     P = exp(S - LSE),  dV = P^T dO,  dS = P * (dO V^T - rowsum(dO * O)),  dQ = scale dS K,  dK = scale dS^T Q,
+ *   dK and dV summed over the query heads that share a key head and written for all N_kv rows (zero where nothing sees the
+ *   key).  workspace_dev: bsa_window_workspace_bytes(desc) bytes of device memory on a 256-byte boundary, the call's own until its
+ *   work on the stream is done (calls that may overlap each bring their own).
+ * A bounded device wait that expires ends the kernel with BSA_ERR_DEVICE_TIMEOUT in bsa_window_status; it never hangs.
+ * Errors: INVALID_ARG (null, misaligned or overlapping strides, sizes below one, left or right below -1, sinks below 0, heads not
+ * a multiple of heads_kv, workspace too small), UNSUPPORTED (d not 64 or 128, N or N_kv above 2^29, more than 65535
+ * sequences x heads), CUDA.
+ */
+typedef struct bsa_window_desc {
+    int32_t batch, heads, heads_kv, d;  /* d: 64 or 128                                                */
+    int64_t N, N_kv;                    /* query rows; key rows of the tensors (a cache's capacity)    */
+    int64_t left, right;                /* -1: no limit on that side                                   */
+    int64_t sinks;
+    int32_t dtype;                      /* BSA_DTYPE_*                                                 */
+    float scale;                        /* 0: 1/sqrt(d)                                                */
+    const int32_t* q_start_dev;         /* [batch] device memory, or NULL: kv_len - N (the last N positions) */
+    const int32_t* kv_len_dev;          /* [batch] device memory, clamped to [0, N_kv]; NULL: N_kv     */
+} bsa_window_desc_t;
+BSA_API bsa_status_t bsa_window_forward(const bsa_window_desc_t* desc, const bsa_view_t* Q, const bsa_view_t* K,
+                                        const bsa_view_t* V, const bsa_view_t* O, float* LSE_dev, void* stream);
+/* The current device's status word of the windowed kernels, and clears it: 0, or BSA_ERR_DEVICE_TIMEOUT if a bounded wait of any of
+ * their calls has expired since the last look (that call's outputs are undefined then).  Synchronises the device. */
+BSA_API bsa_status_t bsa_window_status(int* status_out);
+
+/* ---------------------------------------------------------------------------------------------
  * Introspection (tests, benches, the offline profiler).  These synchronise with the plan's stream.
  */
 BSA_API bsa_status_t bsa_plan_get_info(const bsa_plan_t* plan, bsa_plan_info_t* info_out);

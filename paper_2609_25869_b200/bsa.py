@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, List, Optional, Tuple
 
 import numpy as np
@@ -96,6 +97,9 @@ def lib() -> ctypes.CDLL:
     L.bsa_request_host.argtypes = [vp, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp, ctypes.POINTER(Options),
                                    ctypes.POINTER(PlanInfo)]
     L.bsa_mask_stats_noalloc.argtypes = [vp, i32, i32, i32, vp, vp]
+    L.bsa_rope.argtypes = [ctypes.c_char_p] * 5 + [vp]
+    L.bsa_window_forward.argtypes = [ctypes.c_char_p] * 5 + [vp, vp]
+    L.bsa_window_status.argtypes = [ctypes.POINTER(ctypes.c_int)]
     L.bsa_plan_get_info.argtypes = [vp, ctypes.POINTER(PlanInfo)]
     L.bsa_plan_export_csr.argtypes = [vp, vp, vp]
     L.bsa_plan_export_tiles.argtypes = [vp, i32, vp, vp, vp, i64, ctypes.POINTER(i64)]
@@ -361,6 +365,156 @@ def request_host(mask: np.ndarray, B_Q: int, B_KV: int, N: int, heads: int, d: i
     _check(lib().bsa_request_host(ptr(mask), B_Q, B_KV, N, heads, d, ptr(Q), ptr(K), ptr(V), ptr(O), ptr(LSE),
                                   ctypes.byref(opt), ctypes.byref(inf)), "bsa_request_host")
     return inf.as_dict()
+
+
+# ---------------------------------------------------------------- positions and windows
+# The C structs as packed bytes: filling a ctypes structure field by field takes longer than the smallest kernels.
+_VIEW = struct.Struct("@Pqqq")                       # bsa_view_t
+_ROPE = struct.Struct("@4iq2i4i4idPPqq4i4i")         # bsa_rope_desc_t
+_WINDOW = struct.Struct("@4iqqqqqifPP")              # bsa_window_desc_t
+PAIRS = {"interleaved": 0, "halves": 1}  # BSA_PAIRS_*
+_DTYPE_IDS: Dict = {}
+
+
+def _dtype_id(t, what: str) -> int:
+    if not _DTYPE_IDS:
+        import torch
+        _DTYPE_IDS.update({torch.bfloat16: 0, torch.float16: 1})
+    if not t.is_cuda or t.dtype not in _DTYPE_IDS:
+        raise ValueError(f"{what} has to be a bf16 or fp16 CUDA tensor")
+    return _DTYPE_IDS[t.dtype]
+
+
+def _view(t, nhd: bool, like, what: str):
+    """(batch, heads, rows, d, packed bsa_view_t) of ``[heads, rows, d]`` / ``[batch, heads, rows, d]``, or of
+    ``[rows, heads, d]`` / ``[batch, rows, heads, d]`` with ``nhd``; of the type and on the device of ``like``."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        b, sb = 1, 0
+        h, n, d = shape
+        sh, sn, sd = stride
+    elif len(shape) == 4:
+        b, h, n, d = shape
+        sb, sh, sn, sd = stride
+    else:
+        raise ValueError(f"{what} has to have three or four dimensions")
+    if nhd:
+        h, n, sh, sn = n, h, sn, sh
+    if like is not None and (t.dtype is not like.dtype or t.device != like.device):
+        raise ValueError(f"{what} has to have the type and the device of Q")
+    if sd != 1 and d > 1:
+        raise ValueError(f"{what} has to be contiguous in its last dimension")
+    return b, h, n, d, _VIEW.pack(t.data_ptr(), sb, sh, sn)
+
+
+def _int32_ptr(t, shape, device, what: str) -> int:
+    import torch
+    if t is None:
+        return 0
+    if t.dtype is not torch.int32 or t.device != device or tuple(t.shape) not in shape or not t.is_contiguous():
+        raise ValueError(f"{what} has to be a contiguous int32 tensor {' or '.join(map(str, shape))} on the device of Q")
+    return t.data_ptr()
+
+
+def _on_device(device, call, stream):
+    """``call(stream pointer)`` with ``device`` current, on ``stream`` or the device's current stream."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return call(_stream_ptr(stream))
+    with torch.cuda.device(device):
+        return call(_stream_ptr(stream))
+
+
+def rope(Q, K=None, *, axes, positions=None, grid=None, first: int = 0, origin=None, theta: float = 10000.0, freq=None,
+         pairs: str = "interleaved", shared_freq: bool = False, inverse: bool = False, layout: str = "hnd", out=None,
+         stream=None):
+    """``bsa_rope``: rotary positions of Q and, with the same angles, of K.  Returns ``(Q', K')``, or ``Q'`` without K.
+
+    Q, K: bf16 or fp16 CUDA tensors ``[heads, N, d]`` or ``[batch, heads, N, d]`` (``layout="nhd"``: heads behind N), any
+    strides that are multiples of 8 elements.  ``axes``: channels that each of the one to four axes rotates.  Either
+    ``positions``, int32 ``[N, len(axes)]`` or ``[batch, N, len(axes)]``, or ``grid`` = the axes' lengths: the tokens from
+    ``first`` on stand on it row-major, ``origin`` added, and the others stay as they are.  ``freq``: the pairs' own
+    frequencies instead of ``theta``'s.  ``inverse=True`` is the way back: gradients, or positions taken off.
+    ``out``: the tensors to write (``(Q, K)`` themselves for in place), e.g. views of a cache."""
+    import torch
+    nhd = LAYOUTS[layout] == 1
+    dt = _dtype_id(Q, "Q")
+    b, h, n, d, vq = _view(Q, nhd, None, "Q")
+    if out is None:
+        oq, ok = torch.empty_like(Q), None if K is None else torch.empty_like(K)
+    else:
+        oq, ok = (out, None) if K is None else out
+        if oq.shape != Q.shape or (K is not None and ok.shape != K.shape):
+            raise ValueError("out has to have the shapes of Q and K")
+    voq = _view(oq, nhd, Q, "out")[4]
+    hk, vk, vok = 0, None, None
+    if K is not None:
+        bk, hk, nk, dk, vk = _view(K, nhd, Q, "K")
+        if (bk, nk, dk) != (b, n, d):
+            raise ValueError("Q and K have to agree in batch, tokens and channels")
+        vok = _view(ok, nhd, Q, "out")[4]
+    na = len(axes)
+    if not 1 <= na <= 4 or (positions is None) == (grid is None):
+        raise ValueError("one to four axes, and either positions or a grid")
+    if grid is not None and (len(grid) != na or (origin is not None and len(origin) != na)):
+        raise ValueError("grid and origin have one entry per axis")
+    pos = _int32_ptr(positions, ((n, na), (1, n, na), (b, n, na)), Q.device, "positions")
+    per_batch = n * na if positions is not None and positions.dim() == 3 and positions.shape[0] > 1 else 0
+    freqs = None if freq is None else (ctypes.c_double * len(freq))(*freq)
+    if freq is not None and 2 * len(freq) != sum(axes):
+        raise ValueError("freq has one entry per pair of channels")
+    pad = (0,) * (4 - na)
+    desc = _ROPE.pack(b, h, hk, d, n, dt, na, *axes, *pad, PAIRS[pairs], shared_freq, inverse, 0, theta,
+                      0 if freqs is None else ctypes.addressof(freqs), pos, per_batch, first,
+                      *(grid or (0,) * na), *pad, *(origin or (0,) * na), *pad)
+    _check(_on_device(Q.device, lambda st: lib().bsa_rope(desc, vq, vk, voq, vok, st), stream), "bsa_rope")
+    return oq if K is None else (oq, ok)
+
+
+def _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, layout):
+    """(packed bsa_window_desc_t, packed views of Q, K, V, shape of LSE): what forward and backward check alike."""
+    nhd = LAYOUTS[layout] == 1
+    dt = _dtype_id(Q, "Q")
+    b, h, n, d, vq = _view(Q, nhd, None, "Q")
+    bk, hk, nk, dk, vk = _view(K, nhd, Q, "K")
+    if V.shape != K.shape or bk != b or dk != d or Q.dim() != K.dim():
+        raise ValueError("K and V have to have one shape, and batch and channels of Q")
+    vv = _view(V, nhd, Q, "V")[4]
+    desc = _WINDOW.pack(b, h, hk, d, n, nk, left, right, sinks, dt, scale, _int32_ptr(q_start, ((b,),), Q.device, "q_start"),
+                        _int32_ptr(kv_len, ((b,),), Q.device, "kv_len"))
+    return desc, vq, vk, vv, ((b, h, n) if Q.dim() == 4 else (h, n))
+
+
+def window_forward(Q, K, V, *, left: int, right: int = 0, sinks: int = 0, q_start=None, kv_len=None, scale: float = 0.0,
+                   layout: str = "hnd", O=None, LSE=None, stream=None):
+    """``bsa_window_forward``: attention of each query to the keys ``p - left .. p + right`` around its position and to the
+    first ``sinks`` keys (those up to ``p + right``); -1: no limit on that side.  Returns ``(O, LSE)``.
+
+    Q ``[heads, N, d]`` or ``[batch, heads, N, d]``, K and V likewise with ``heads_kv`` heads and ``N_kv`` tokens
+    (``layout="nhd"``: heads behind tokens); any strides that are multiples of 8 elements.  ``q_start``, ``kv_len``: int32
+    CUDA tensors ``[batch]``, each sequence's first query position and its number of keys (default: the queries are the last N
+    of N_kv positions).  LSE is fp32 ``[batch, heads, N]`` (``[heads, N]``) in either layout."""
+    import torch
+    desc, vq, vk, vv, shape = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, layout)
+    if O is None:
+        O = torch.empty_like(Q)
+    elif O.shape != Q.shape:
+        raise ValueError("O has to have the shape of Q")
+    if LSE is None:
+        LSE = Q.new_empty(shape, dtype=torch.float32)
+    elif tuple(LSE.shape) != shape or LSE.dtype is not torch.float32 or LSE.device != Q.device or not LSE.is_contiguous():
+        raise ValueError(f"LSE has to be a contiguous fp32 tensor {shape} on the device of Q")
+    vo = _view(O, LAYOUTS[layout] == 1, Q, "O")[4]
+    _check(_on_device(Q.device, lambda st: lib().bsa_window_forward(desc, vq, vk, vv, vo, LSE.data_ptr(), st), stream),
+           "bsa_window_forward")
+    return O, LSE
+
+
+def window_status() -> int:
+    """``bsa_window_status``: 0, or the status that a windowed kernel on the current device has left since the last look."""
+    out = ctypes.c_int(0)
+    _check(lib().bsa_window_status(ctypes.byref(out)), "bsa_window_status")
+    return out.value
 
 
 NOALLOC_MAX_ROWS = 1 << 20

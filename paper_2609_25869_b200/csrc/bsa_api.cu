@@ -38,7 +38,7 @@ static std::atomic<unsigned> g_select_generation{0};
 void count_launch(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 
 static thread_local char g_cuda_err[256] = "";
-static void set_cuda_err(cudaError_t e, const char* where) {
+void set_cuda_err(cudaError_t e, const char* where) {
     snprintf(g_cuda_err, sizeof g_cuda_err, "%s: %s", where, cudaGetErrorString(e));
 }
 

@@ -2747,6 +2747,20 @@ bool encode_kv_map(CUtensorMap* m, const void* base, int64_t N, int heads, int d
     return encode_map4(m, base, N, heads, d, box_rows, f16, nhd);
 }
 
+bool encode_view_map(CUtensorMap* m, const bsa_view_t& v, int64_t rows, int heads, int batch, int d, int box_rows, bool f16) {
+    EncodeTiledFn enc = get_encode_fn();
+    if (!enc) return false;
+    const cuuint64_t any = (cuuint64_t)d * 2;  // the stride of a dimension with one entry is never used
+    cuuint64_t dims[5] = {64, (cuuint64_t)rows, (cuuint64_t)(d / 64), (cuuint64_t)heads, (cuuint64_t)batch};
+    cuuint64_t strides[4] = {rows > 1 ? (cuuint64_t)v.row * 2 : any, 128, heads > 1 ? (cuuint64_t)v.head * 2 : any,
+                             batch > 1 ? (cuuint64_t)v.batch * 2 : any};
+    cuuint32_t box[5] = {64, (cuuint32_t)box_rows, (cuuint32_t)(d / 64), 1, 1};
+    cuuint32_t es[5] = {1, 1, 1, 1, 1};
+    return enc(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, v.data, dims, strides, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Shared-memory budget: 227 KB per CTA minus each kernel's static shared memory (barriers, exchange
 // buffer), which the compiler rounds up to the 1024-byte alignment of the dynamic part.
 static int static_smem_bytes(int kernel) { return (kernel == 2 || kernel == 4) ? 3072 : 1024; }

@@ -1,0 +1,109 @@
+// What the windowed attention kernels share: who sees whom.
+#pragma once
+#include <limits.h>
+
+#include "bsa_common.h"
+#include "sm100_ptx.cuh"
+
+namespace bsa {
+
+// Set by kernels whose bounded wait expired; read by bsa_window_status.  One word per device.
+cudaError_t window_status_word(int** out);
+
+constexpr int kWinT = 128;             // rows and keys of a tile
+constexpr int kWinNoLimit = 1 << 29;   // left or right where there is no limit: beyond every position
+
+// A call's sizes and mask.  Positions stay below 2^30, sums of two below 2^31: plain int arithmetic.
+struct WindowGeom {
+    int batch, heads, heads_kv, group;  // group = heads / heads_kv
+    int N, N_kv;
+    int left, right, sinks;
+    const int32_t* q_start;
+    const int32_t* kv_len;
+};
+
+struct Sequence {
+    int start, len;  // position of row 0, number of keys
+};
+__device__ __forceinline__ Sequence load_sequence(const WindowGeom& g, int b) {
+    Sequence s;
+    s.len = g.kv_len ? min(max(__ldg(g.kv_len + b), 0), g.N_kv) : g.N_kv;
+    s.start = g.q_start ? min(max(__ldg(g.q_start + b), -kWinNoLimit), kWinNoLimit) : s.len - g.N;
+    return s;
+}
+
+// The keys that rows [r0, r1) of a sequence see between them: [0, sink_hi) and [lo, hi), sink_hi <= lo; and, for the tiles that
+// need no mask, the keys that all of them see: those below all_hi that are sinks or not below all_lo.  Rows at no position of
+// the sequence are left out of both.
+struct KeyRange {
+    int lo, hi, sink_hi;
+    int all_lo, all_hi;
+};
+__device__ __forceinline__ KeyRange key_range(const WindowGeom& g, const Sequence& s, int r0, int r1) {
+    KeyRange k;
+    const int p0 = max(s.start + r0, 0), p1 = min(s.start + min(r1, g.N), s.len) - 1;
+    if (p0 > p1) {
+        k.lo = k.hi = k.sink_hi = k.all_lo = k.all_hi = 0;
+        return k;
+    }
+    k.hi = min(s.len, p1 + g.right + 1);
+    k.lo = max(0, p0 - g.left);
+    k.sink_hi = min(min(g.sinks, k.hi), k.lo);
+    k.all_hi = min(s.len, p0 + g.right + 1);
+    k.all_lo = p1 - g.left;
+    return k;
+}
+__device__ __forceinline__ bool tile_is_full(const WindowGeom& g, const KeyRange& k, int key0) {
+    return key0 + kWinT <= k.all_hi && (key0 >= k.all_lo || key0 + kWinT <= g.sinks);
+}
+
+// 128-key tiles of a range: [0, st) and [w0, w1).
+struct TileSpan {
+    int st, w0, w1;
+    __device__ __forceinline__ int count() const { return st + (w1 - w0); }
+    __device__ __forceinline__ int tile(int j) const { return j < st ? j : w0 + (j - st); }
+    __device__ __forceinline__ bool has(int t) const { return t < st || (t >= w0 && t < w1); }
+};
+__device__ __forceinline__ TileSpan tile_span(const KeyRange& k) {
+    TileSpan t;
+    t.w0 = k.lo / kWinT;
+    t.w1 = (k.hi + kWinT - 1) / kWinT;
+    t.st = min((k.sink_hi + kWinT - 1) / kWinT, t.w0);
+    return t;
+}
+// The tiles of either span (an empty span: w0 = w1 = 0).
+__device__ __forceinline__ TileSpan join(const TileSpan& a, const TileSpan& b) {
+    if (a.w1 == 0) return b;
+    if (b.w1 == 0) return a;
+    TileSpan t;
+    t.w0 = min(a.w0, b.w0);
+    t.w1 = max(a.w1, b.w1);
+    t.st = min(max(a.st, b.st), t.w0);
+    return t;
+}
+
+// Row i's view of a tile that starts at key0, as bounds on the column: it sees c < hi with c >= lo or c < sink.
+struct RowMask {
+    int lo, hi, sink;
+};
+__device__ __forceinline__ RowMask row_mask(const WindowGeom& g, const Sequence& s, int pos, int key0) {
+    RowMask m;
+    const bool seen = pos >= 0 && pos < s.len;
+    m.hi = (seen ? min(s.len, pos + g.right + 1) : 0) - key0;
+    m.lo = pos - g.left - key0;
+    m.sink = g.sinks - key0;
+    return m;
+}
+
+// ---- host side (bsa_window.cu) ----
+struct WindowArgs {
+    WindowGeom g;
+    int d;
+    bool f16;
+    float scale;
+    int device, num_sms;
+};
+// Checks a description and fills `a` in; the current device becomes the call's.
+bsa_status_t window_args(const bsa_window_desc_t* t, WindowArgs* a);
+
+}  // namespace bsa

@@ -2,20 +2,21 @@
 //
 //   S = scale Q K^T,  LSE = log sum exp S,  O = sum exp(S - LSE) V   over the keys that a row sees
 //
-// One CTA takes 256 query rows of one head as two 128-row slots that share every K and V tile of 128 keys: a 128x128x128
-// product with both operands in shared memory reads them at the full 128 B/clk, and with one slot per tile the copies of K
-// and V would come on top of that; with two they are half as many.  The tiles that a slot needs follow from its rows'
-// positions (no list, no mask in memory): a run of tiles around the diagonal and the sinks' tiles; a tile that only one slot
-// needs is left out for the other.  Bounds on the columns of a row are applied only in tiles that some row of the slot does
-// not see whole.
-//   warps 0-3 / 4-7 : softmax of slot 0 / 1 (thread = row)     warps 8-11 : epilogue of both slots
-//   warp 12 : TMA producer    warp 13 : MMA issuer (d = 64: Q K^T)    warp 14 : d = 64: P V issuer
-// Tensor memory: d = 128: S0, S1, O0, O1 take all 512 columns; P takes the place of the scores that it comes from, and a
-// slot's next Q K^T is issued behind its P V (one thread issues both, in order).  While one slot's softmax runs, the other's
-// two products do.  P is handed over in halves of 64 keys, so that P V starts while the second half's exponentials run.
-// d = 64: P has columns of its own, so a slot's next scores are computed as soon as the last have been read.
-// Work per 128-key tile and slot: 4 * 128 * 128 * d flops (1024 clk at d = 128) and 128 * 128 exponentials (1024 clk at 16 per
-// clk and SM): the tensor pipe and the special-function unit bind together at d = 128, the latter alone at d = 64.
+// A persistent CTA takes 128 query rows of one head at a time and walks over the 128-key tiles that they see: a run of tiles
+// around the diagonal and the sinks' tiles, computed from the rows' positions (no list, no mask in memory).  Bounds on a
+// row's columns are applied only in tiles that some row does not see whole.
+//   warps 0-3 / 4-7 : softmax warpgroups (thread = row); tile t belongs to warpgroup t mod 2, and S and P buffer t mod 2 with it
+//   warp 8 : Q and K producer   warp 9 : Q K^T issuer   warp 10 : P V issuer   warp 11 : V producer   warps 12-15 : epilogue
+// Work per tile: 4 * 128 * 128 * d flops (1024 clk at d = 128) and 128 * 128 exponentials (1024 clk at 16 per clk and SM): at
+// d = 128 the tensor pipe and the special-function unit bind together, at d = 64 the latter alone.  A warpgroup's softmax takes
+// about 2000 clk of a tile (maxima, exponentials, their latencies), so two must run at once and neither may wait for
+// products: S and P have their own columns, Q K^T runs two tiles ahead.
+// (Measured against 256 rows per CTA with a slot of 128 per warpgroup and P in the place of S, which reads K and V from shared
+// memory half as often: 115200 tokens, 24 heads, window 8191, d = 128: 12.1 ms; a slot's softmax, P V and Q K^T then follow each
+// other, 4400 clk per tile and slot.)
+// d = 128: tensor memory has room for one accumulator, so both warpgroups follow one reference maximum per row, handed from tile to
+// tile through shared memory.  d = 64: each has an accumulator and a reference of its own, joined by the epilogue.
+// Tensor-memory columns: S0 0, S1 128, O 256 (d = 64: O0 256, O1 320), P0 384, P1 448.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -34,17 +35,14 @@ __device__ int g_window_status = 0;
 constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;
 constexpr float kRescale = 8.0f;  // log2 units: P stays below 2^8 between rescales
-constexpr int kSlotRows = 128, kCtaRows = 256;
 
 template <int D>
 struct Cfg {
-    static constexpr bool kOwnP = (D == 64);
-    static constexpr int kTile = kWinT * D * 2;                 // bytes of a 128-row tile of Q, K or V
-    static constexpr int kQBuffers = (D == 64) ? 2 : 1;         // of two slots each
-    static constexpr int kStages = (D == 64) ? 8 : 5;           // K and V tiles in turn
-    static constexpr int kSmem = (kQBuffers * 2 + kStages) * kTile;
-    static constexpr uint32_t kS0 = 0, kS1 = 128, kO0 = 256, kO1 = (D == 64) ? 320 : 384;
-    static constexpr uint32_t kP0 = kOwnP ? 384 : kS0, kP1 = kOwnP ? 448 : kS1;
+    static constexpr bool kOwnO = (D == 64);              // an accumulator per softmax warpgroup
+    static constexpr int kTile = kWinT * D * 2;           // bytes of a 128-row tile of Q, K or V
+    static constexpr int kK = (D == 64) ? 4 : 2, kV = (D == 64) ? 4 : 3;  // tiles in the rings
+    static constexpr int kSmem = (2 + kK + kV) * kTile;   // two Q tiles
+    static constexpr uint32_t kS0 = 0, kS1 = 128, kO0 = 256, kO1 = kOwnO ? 320 : 256, kP0 = 384, kP1 = 448;
 };
 
 struct Params {
@@ -53,25 +51,26 @@ struct Params {
     long long o_batch, o_head, o_row;
     float* LSE;
     float scale_log2;  // scale * log2(e)
-    int n_qt;          // 256-row tiles of a sequence
+    int n_qt;          // 128-row tiles of a sequence
     int n_items;
     int longest_first; // no left limit: later tiles are longer
 };
 
 struct __align__(8) Barriers {
     uint64_t q_full[2], q_empty[2];
-    uint64_t kv_full[8], kv_empty[8];
-    uint64_t s_full[2], s_free[2], p_half[2][2], pv_done[2];
-    uint64_t o_full[2], o_free[2], e_ready[2], e_taken[2];
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+    uint64_t s_full[2], s_free[2], p_ready[2], pv_done[2];
+    uint64_t o_full, o_free, e_ready, e_taken;
 };
 
 struct Item {
     int b, h, row0;
     Sequence seq;
-    KeyRange r0, r1;
-    TileSpan t0, t1, both;
+    KeyRange range;
+    TileSpan tiles;
 };
 
+// The CTA's k-th item, dealt in alternating directions; false past the end.
 __device__ __forceinline__ bool load_item(const Params& p, int k, Item& it) {
     const int G = gridDim.x;
     const int idx = k * G + ((k & 1) ? (G - 1 - (int)blockIdx.x) : (int)blockIdx.x);
@@ -87,13 +86,10 @@ __device__ __forceinline__ bool load_item(const Params& p, int k, Item& it) {
     }
     it.b = bh / p.g.heads;
     it.h = bh - it.b * p.g.heads;
-    it.row0 = qt * kCtaRows;
+    it.row0 = qt * kWinT;
     it.seq = load_sequence(p.g, it.b);
-    it.r0 = key_range(p.g, it.seq, it.row0, it.row0 + kSlotRows);
-    it.r1 = key_range(p.g, it.seq, it.row0 + kSlotRows, it.row0 + kCtaRows);
-    it.t0 = tile_span(it.r0);
-    it.t1 = tile_span(it.r1);
-    it.both = join(it.t0, it.t1);
+    it.range = key_range(p.g, it.seq, it.row0, it.row0 + kWinT);
+    it.tiles = tile_span(it.range);
     return true;
 }
 
@@ -124,6 +120,39 @@ struct Ring {
     }
 };
 
+__device__ __forceinline__ float row_max(const uint32_t (&r)[kWinT]) {
+    float m0 = -INFINITY, m1 = m0, m2 = m0, m3 = m0;
+#pragma unroll
+    for (int i = 0; i < kWinT; i += 8) {
+        m0 = max3(m0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+        m1 = max3(m1, __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+        m2 = max3(m2, __uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
+        m3 = max3(m3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
+    }
+    return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+}
+
+// A word of a row's reference: the value's two lowest mantissa bits make room for (publish index + 1) mod 4, so that one read
+// tells whether the value is the one that is waited for.  False: the wait expired.
+__device__ __forceinline__ bool take_reference(volatile uint32_t* slot, uint32_t tag, volatile uint32_t* abortp, float& m) {
+    uint32_t word = *slot;
+    long long t0 = 0;
+    for (uint32_t spins = 1; (word & 3u) != tag; ++spins) {
+        if ((spins & 63u) == 0) {
+            if (*abortp) return false;
+            const long long now = clock64();
+            if (t0 == 0) t0 = now;
+            if (now - t0 > *reinterpret_cast<volatile long long*>(&g_wait_limit_cycles)) {
+                *abortp = 1;
+                return false;
+            }
+        }
+        word = *slot;
+    }
+    m = __uint_as_float(word & ~3u);
+    return true;
+}
+
 template <int D, bool F16>
 __global__ void __launch_bounds__(kThreads, 1)
 window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -132,12 +161,15 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     constexpr int SUB = kWinT * 128;  // bytes of a [128 rows][64 columns] sub-tile
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* sQ = smem;
-    uint8_t* sKV = smem + C::kQBuffers * 2 * C::kTile;
+    uint8_t* sK = sQ + 2 * C::kTile;
+    uint8_t* sV = sK + C::kK * C::kTile;
     __shared__ Barriers bars;
-    __shared__ float fin_m[2][kSlotRows], fin_l[2][kSlotRows];  // an item's reference maxima (log2 domain) and row sums
+    __shared__ uint32_t mref[2][kWinT];  // d = 128: [publishing warpgroup][row]; d = 64: an item's references, plain
+    __shared__ float lfin[2][kWinT];     // an item's row sums, by warpgroup (d = 128: in its final reference)
+    __shared__ float mfin[kWinT];        // d = 128: that reference (log2 domain)
     __shared__ uint32_t tmem_base_s, abort_flag;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     if (smem_u32(smem) & 1023u) {  // never expected; fail with a status instead of corrupting tiles
         if (tid == 0) atomicExch(&g_window_status, (int)BSA_ERR_CUDA);
         return;
@@ -149,25 +181,27 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             mbar_init(smem_u32(&bars.q_empty[i]), 1);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
             mbar_init(smem_u32(&bars.s_free[i]), 128);
-            mbar_init(smem_u32(&bars.p_half[i][0]), 128);
-            mbar_init(smem_u32(&bars.p_half[i][1]), 128);
+            mbar_init(smem_u32(&bars.p_ready[i]), 128);
             mbar_init(smem_u32(&bars.pv_done[i]), 1);
-            mbar_init(smem_u32(&bars.o_full[i]), 1);
-            mbar_init(smem_u32(&bars.o_free[i]), 128);
-            mbar_init(smem_u32(&bars.e_ready[i]), 128);
-            mbar_init(smem_u32(&bars.e_taken[i]), 128);
         }
-        for (int i = 0; i < C::kStages; ++i) {
-            mbar_init(smem_u32(&bars.kv_full[i]), 1);
-            mbar_init(smem_u32(&bars.kv_empty[i]), 1);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(smem_u32(&bars.k_full[i]), 1);
+            mbar_init(smem_u32(&bars.k_empty[i]), 1);
+            mbar_init(smem_u32(&bars.v_full[i]), 1);
+            mbar_init(smem_u32(&bars.v_empty[i]), 1);
         }
+        mbar_init(smem_u32(&bars.o_full), 1);
+        mbar_init(smem_u32(&bars.o_free), 128);
+        mbar_init(smem_u32(&bars.e_ready), 256);
+        mbar_init(smem_u32(&bars.e_taken), 128);
         fence_mbar_init();
     }
-    if (warp == 13) {
+    if (tid < 2 * kWinT) (&mref[0][0])[tid] = 0u;  // a tag that matches no first publish
+    if (warp == 9) {
         tmem_alloc(smem_u32(&tmem_base_s), kTmemCols);
         tmem_relinquish();
     }
-    if (warp == 12 && lane == 0) {
+    if (warp == 8 && lane == 0) {
         prefetch_tensormap(&tmQ);
         prefetch_tensormap(&tmK);
         prefetch_tensormap(&tmV);
@@ -175,296 +209,241 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_base_s;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
     volatile uint32_t* abortp = &abort_flag;
     Item it;
 
     if (warp >= 12) {
-        reg_dec<48>();
-        if (warp == 12 && lane == 0) {
-            // =========================== producer ===========================
-            Ring ring;
-            uint32_t n_q = 0;
-            bool ok = true;
-            for (int k = 0; ok && load_item(p, k, it); ++k) {
-                const int n = it.both.count();
-                if (n == 0) continue;
-                const int hk = it.h / p.g.group;
-                const uint32_t qb = n_q % C::kQBuffers;
-                ok = mbar_wait(smem_u32(&bars.q_empty[qb]), ((n_q / C::kQBuffers) & 1) ^ 1, abortp);
-                if (!ok) break;
-                const uint32_t q_bar = smem_u32(&bars.q_full[qb]), q_dst = smem_u32(sQ) + qb * 2 * C::kTile;
-                const bool s0 = it.t0.w1 > 0, s1 = it.t1.w1 > 0;
-                mbar_arrive_expect_tx(q_bar, (int(s0) + int(s1)) * C::kTile);
-                if (s0) tma_load_rows(q_dst, &tmQ, q_bar, it.row0, it.h, it.b);
-                if (s1) tma_load_rows(q_dst + C::kTile, &tmQ, q_bar, it.row0 + kSlotRows, it.h, it.b);
-                ++n_q;
-                for (int j = 0; j < n && ok; ++j) {
-                    const int key0 = it.both.tile(j) * kWinT;
-#pragma unroll
-                    for (int kv = 0; kv < 2; ++kv) {
-                        ok = ok && mbar_wait(smem_u32(&bars.kv_empty[ring.stage]), ring.phase ^ 1, abortp);
-                        if (!ok) break;
-                        const uint32_t bar = smem_u32(&bars.kv_full[ring.stage]);
-                        mbar_arrive_expect_tx(bar, C::kTile);
-                        tma_load_rows(smem_u32(sKV) + ring.stage * C::kTile, kv ? &tmV : &tmK, bar, key0, hk, it.b);
-                        ring.advance<C::kStages>();
-                    }
-                }
-            }
-            if (!ok) let_copies_land();
-        } else if (warp == 13 && lane == 0) {
-            // =========================== MMA issuer (d = 64: Q K^T only) ===========================
-            constexpr uint32_t idesc_qk = make_idesc_f32(kSlotRows, kWinT, 0, 0, F16);
-            constexpr uint32_t idesc_pv = make_idesc_f32(kSlotRows, D, 0, 1, F16);
-            const uint64_t descQ = make_smem_desc_sw128(smem_u32(sQ), 16, 1024);
-            const uint64_t descK = make_smem_desc_sw128(smem_u32(sKV), 16, 1024);
-            const uint64_t descV = make_smem_desc_sw128(smem_u32(sKV), SUB, 1024);
-            Ring ring;                 // of the tile being looked at: K, then V
-            uint32_t n_q = 0;
-            uint32_t n_s[2] = {0, 0};  // score tiles issued
-            uint32_t n_p[2] = {0, 0};  // P V issued
-            uint32_t n_o[2] = {0, 0};  // accumulators begun
-            bool ok = true;
-            for (int k = 0; ok && load_item(p, k, it); ++k) {
-                const int n = it.both.count();
-                if (n == 0) continue;
-                const uint32_t qb = n_q % C::kQBuffers;
-                ok = mbar_wait(smem_u32(&bars.q_full[qb]), (n_q / C::kQBuffers) & 1, abortp);
-                if (!ok) break;
-                ++n_q;
-                bool pend[2] = {false, false}, first[2] = {true, true};
-                int v_stage = 0;
-                uint32_t v_phase = 0;
-                auto issue_pv = [&](int x, bool last_user, bool last_tile) -> bool {
-                    const uint32_t d_o = tmem + (x ? C::kO1 : C::kO0), a_p = tmem + (x ? C::kP1 : C::kP0);
-                    if (first[x]) {  // the accumulator has been drained
-                        if (!mbar_wait(smem_u32(&bars.o_free[x]), (n_o[x] & 1) ^ 1, abortp)) return false;
-                        ++n_o[x];
-                    }
-                    if (!mbar_wait(smem_u32(&bars.kv_full[v_stage]), v_phase, abortp)) return false;
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        if (!mbar_wait(smem_u32(&bars.p_half[x][half]), n_p[x] & 1, abortp)) return false;
-                        tc_fence_after();
-#pragma unroll
-                        for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-                            mma_ts(d_o, a_p + kk * 8, descV + (uint64_t)((v_stage * C::kTile + kk * 2048) >> 4), idesc_pv,
-                                   (!first[x] || kk > 0) ? 1u : 0u);
-                    }
-                    if (last_user) mma_commit(smem_u32(&bars.kv_empty[v_stage]));
-                    mma_commit(smem_u32(&bars.pv_done[x]));
-                    if (last_tile) mma_commit(smem_u32(&bars.o_full[x]));
-                    first[x] = false;
-                    ++n_p[x];
-                    return true;
-                };
-                int left_over[2] = {it.t0.count(), it.t1.count()};  // tiles of each slot whose P V is to come
-                for (int j = 0; j <= n && ok; ++j) {
-                    const int tile = j < n ? it.both.tile(j) : -1;
-                    const bool act[2] = {j < n && it.t0.has(tile), j < n && it.t1.has(tile)};
-                    const int k_stage = ring.stage;
-                    if (j < n) ok = mbar_wait(smem_u32(&bars.kv_full[k_stage]), ring.phase, abortp);
-                    if (!ok) break;
-                    const bool last_pv1 = pend[1];
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (!C::kOwnP && pend[x]) {
-                            ok = ok && issue_pv(x, x == 1 || !last_pv1, --left_over[x] == 0);
-                            if (!ok) break;
-                            pend[x] = false;
-                        }
-                        if (act[x]) {
-                            if (C::kOwnP && n_s[x] > 0) {  // the last scores of this slot have been read
-                                ok = mbar_wait(smem_u32(&bars.s_free[x]), (n_s[x] - 1) & 1, abortp);
-                                if (!ok) break;
-                            }
-                            tc_fence_after();
-                            const uint64_t q0 = descQ + (uint64_t)(((qb * 2 + x) * C::kTile) >> 4);
-                            const uint64_t k0 = descK + (uint64_t)((k_stage * C::kTile) >> 4);
-                            const uint32_t d_s = tmem + (x ? C::kS1 : C::kS0);
-#pragma unroll
-                            for (int kk = 0; kk < D / 16; ++kk) {
-                                const uint64_t off = (uint64_t)(((kk / 4) * SUB + (kk % 4) * 32) >> 4);
-                                mma_ss(d_s, q0 + off, k0 + off, idesc_qk, kk > 0);
-                            }
-                            mma_commit(smem_u32(&bars.s_full[x]));
-                            ++n_s[x];
-                            pend[x] = true;
-                        }
-                    }
-                    if (!ok || j == n) break;
-                    mma_commit(smem_u32(&bars.kv_empty[k_stage]));
-                    if (j == n - 1) mma_commit(smem_u32(&bars.q_empty[qb]));
-                    ring.advance<C::kStages>();
-                    v_stage = ring.stage;
-                    v_phase = ring.phase;
-                    ring.advance<C::kStages>();
-                }
-            }
-        } else if (C::kOwnP && warp == 14 && lane == 0) {
-            // =========================== P V issuer (d = 64) ===========================
-            constexpr uint32_t idesc_pv = make_idesc_f32(kSlotRows, D, 0, 1, F16);
-            const uint64_t descV = make_smem_desc_sw128(smem_u32(sKV), SUB, 1024);
-            Ring ring;
-            uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0};
-            bool ok = true;
-            for (int k = 0; ok && load_item(p, k, it); ++k) {
-                const int n = it.both.count();
-                bool first[2] = {true, true};
-                int left_over[2] = {it.t0.count(), it.t1.count()};
-                for (int j = 0; j < n && ok; ++j) {
-                    const int tile = it.both.tile(j);
-                    const bool act[2] = {it.t0.has(tile), it.t1.has(tile)};
-                    ring.advance<C::kStages>();  // past K
-                    ok = mbar_wait(smem_u32(&bars.kv_full[ring.stage]), ring.phase, abortp);
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (!ok || !act[x]) continue;
-                        if (first[x]) {
-                            ok = mbar_wait(smem_u32(&bars.o_free[x]), (n_o[x] & 1) ^ 1, abortp);
-                            if (!ok) break;
-                            ++n_o[x];
-                        }
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            ok = ok && mbar_wait(smem_u32(&bars.p_half[x][half]), n_p[x] & 1, abortp);
-                            if (!ok) break;
-                            tc_fence_after();
-#pragma unroll
-                            for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-                                mma_ts(tmem + (x ? C::kO1 : C::kO0), tmem + (x ? C::kP1 : C::kP0) + kk * 8,
-                                       descV + (uint64_t)((ring.stage * C::kTile + kk * 2048) >> 4), idesc_pv, (!first[x] || kk > 0) ? 1u : 0u);
-                        }
-                        if (!ok) break;
-                        mma_commit(smem_u32(&bars.pv_done[x]));
-                        if (--left_over[x] == 0) mma_commit(smem_u32(&bars.o_full[x]));
-                        first[x] = false;
-                        ++n_p[x];
-                    }
-                    if (!ok) break;
-                    mma_commit(smem_u32(&bars.kv_empty[ring.stage]));
-                    ring.advance<C::kStages>();
-                }
-            }
-        }
-    } else if (warp >= 8) {
         // =========================== epilogue ===========================
         reg_dec<80>();
         const int tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        uint32_t n_e[2] = {0, 0};
-        bool ok = true;
-        for (int k = 0; ok && load_item(p, k, it); ++k) {
-#pragma unroll 1
-            for (int x = 0; x < 2 && ok; ++x) {
-                const int row = it.row0 + x * kSlotRows + tw;
-                const bool row_ok = row < p.g.N;
-                const int pos = it.seq.start + row;
-                const bool seen = pos >= 0 && pos < it.seq.len;
-                uint16_t* orow = p.O + (long long)it.b * p.o_batch + (long long)it.h * p.o_head + (long long)row * p.o_row;
-                float* lse_out = p.LSE + ((long long)it.b * p.g.heads + it.h) * p.g.N + row;
-                if ((x ? it.t1.w1 : it.t0.w1) == 0) {  // no row of the slot sees anything
-                    if (row_ok) {
+        uint32_t n_it = 0, g = 0;  // items with tiles, tiles so far
+        for (int k = 0; load_item(p, k, it); ++k) {
+            const int row = it.row0 + tw;
+            const bool row_ok = row < p.g.N;
+            const int pos = it.seq.start + row;
+            const bool seen = pos >= 0 && pos < it.seq.len;
+            uint16_t* orow = p.O + (long long)it.b * p.o_batch + (long long)it.h * p.o_head + (long long)row * p.o_row;
+            float* lse_out = p.LSE + ((long long)it.b * p.g.heads + it.h) * p.g.N + row;
+            const int n = it.tiles.count();
+            if (n == 0) {  // no row of the tile sees anything
+                if (row_ok) {
 #pragma unroll
-                        for (int c = 0; c < D / 8; ++c) reinterpret_cast<uint4*>(orow)[c] = make_uint4(0, 0, 0, 0);
-                        *lse_out = -INFINITY;
-                    }
-                    continue;
+                    for (int c = 0; c < D / 8; ++c) reinterpret_cast<uint4*>(orow)[c] = make_uint4(0, 0, 0, 0);
+                    *lse_out = -INFINITY;
                 }
-                ok = mbar_wait_warp(smem_u32(&bars.e_ready[x]), n_e[x] & 1, abortp);
-                if (!ok) break;
-                const float l = fin_l[x][tw], m = fin_m[x][tw];
-                mbar_arrive(smem_u32(&bars.e_taken[x]));
-                const bool any = seen && l > 0.f;
-                const float inv = any ? 1.f / l : 0.f;
-                if (row_ok) *lse_out = any ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
-                ok = mbar_wait_warp(smem_u32(&bars.o_full[x]), n_e[x] & 1, abortp);
-                if (!ok) break;
-                ++n_e[x];
-                tc_fence_after();
+                continue;
+            }
+            if (!mbar_wait_warp(smem_u32(&bars.e_ready), n_it & 1, abortp)) break;
+            // warpgroup a had the item's first tile: an item's bits do not depend on its place among the CTA's
+            const uint32_t a = g & 1u;
+            float l, m, wa = 1.f, wb = 0.f;
+            if constexpr (C::kOwnO) {
+                const float ma = __uint_as_float(mref[a][tw]), mb = __uint_as_float(mref[a ^ 1u][tw]);
+                m = fmaxf(ma, mb);
+                wa = ma == -INFINITY ? 0.f : ex2_approx(ma - m);
+                wb = mb == -INFINITY ? 0.f : ex2_approx(mb - m);
+                l = fmaf(lfin[a ^ 1u][tw], wb, lfin[a][tw] * wa);
+            } else {
+                l = lfin[a][tw] + lfin[a ^ 1u][tw];
+                m = mfin[tw];
+            }
+            mbar_arrive(smem_u32(&bars.e_taken));
+            const bool any = seen && l > 0.f;
+            const float inv = any ? 1.f / l : 0.f;
+            if (row_ok) *lse_out = any ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
+            if (!mbar_wait_warp(smem_u32(&bars.o_full), n_it & 1, abortp)) break;
+            ++n_it;
+            g += (uint32_t)n;
+            tc_fence_after();
+            constexpr int CW = C::kOwnO ? 16 : 32;
+            const float sa = inv * wa, sb = inv * wb;
 #pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld32(t_lane + (x ? C::kO1 : C::kO0) + c * 32, o);
+            for (int c = 0; c < D / CW; ++c) {
+                uint32_t o[CW];
+                if constexpr (C::kOwnO) {
+                    uint32_t ob[CW];
+                    tmem_ld16(t_lane + (a ? C::kO1 : C::kO0) + c * CW, o);
+                    tmem_ld16(t_lane + (a ? C::kO0 : C::kO1) + c * CW, ob);
                     tc_wait_ld();
-                    if (c == D / 32 - 1) {
-                        tc_fence_before();
-                        mbar_arrive(smem_u32(&bars.o_free[x]));
+#pragma unroll
+                    for (int e = 0; e < CW; ++e) {
+                        const float v = __uint_as_float(o[e]) * sa;
+                        o[e] = __float_as_uint(n > 1 ? fmaf(__uint_as_float(ob[e]), sb, v) : v);  // (one tile: the other is stale)
                     }
-                    if (row_ok) {
+                } else {
+                    tmem_ld32(t_lane + C::kO0 + c * CW, o);
+                    tc_wait_ld();
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            uint32_t v[4];
+                    for (int e = 0; e < CW; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * sa);
+                }
+                if (c == D / CW - 1) {  // drained: the next item's first P V may overwrite it
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&bars.o_free));
+                }
+                if (row_ok) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float a = __uint_as_float(o[q * 8 + 2 * e]) * inv, b = __uint_as_float(o[q * 8 + 2 * e + 1]) * inv;
-                                v[e] = seen ? pack_16x2<F16>(a, b) : 0u;
-                            }
-                            *reinterpret_cast<uint4*>(orow + c * 32 + q * 8) = make_uint4(v[0], v[1], v[2], v[3]);
-                        }
+                    for (int q = 0; q < CW / 8; ++q) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            v[e] = seen ? pack_16x2<F16>(__uint_as_float(o[q * 8 + 2 * e]), __uint_as_float(o[q * 8 + 2 * e + 1])) : 0u;
+                        *reinterpret_cast<uint4*>(orow + c * CW + q * 8) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
             }
         }
+    } else if (warp >= 8) {
+        reg_dec<48>();
+        if (warp == 8 && lane == 0) {
+            // =========================== Q and K producer ===========================
+            Ring ring;
+            uint32_t n_q = 0;
+            bool ok = true;
+            for (int k = 0; ok && load_item(p, k, it); ++k) {
+                const int n = it.tiles.count(), hk = it.h / p.g.group;
+                if (n == 0) continue;
+                const uint32_t qb = n_q & 1;
+                ok = mbar_wait(smem_u32(&bars.q_empty[qb]), ((n_q >> 1) & 1) ^ 1, abortp);
+                if (!ok) break;
+                mbar_arrive_expect_tx(smem_u32(&bars.q_full[qb]), C::kTile);
+                tma_load_rows(smem_u32(sQ) + qb * C::kTile, &tmQ, smem_u32(&bars.q_full[qb]), it.row0, it.h, it.b);
+                ++n_q;
+                for (int j = 0; j < n; ++j, ring.advance<C::kK>()) {
+                    ok = mbar_wait(smem_u32(&bars.k_empty[ring.stage]), ring.phase ^ 1, abortp);
+                    if (!ok) break;
+                    const uint32_t bar = smem_u32(&bars.k_full[ring.stage]);
+                    mbar_arrive_expect_tx(bar, C::kTile);
+                    tma_load_rows(smem_u32(sK) + ring.stage * C::kTile, &tmK, bar, it.tiles.tile(j) * kWinT, hk, it.b);
+                }
+            }
+            if (!ok) let_copies_land();
+        } else if (warp == 11 && lane == 0) {
+            // =========================== V producer ===========================
+            Ring ring;
+            bool ok = true;
+            for (int k = 0; ok && load_item(p, k, it); ++k) {
+                const int n = it.tiles.count(), hk = it.h / p.g.group;
+                for (int j = 0; j < n; ++j, ring.advance<C::kV>()) {
+                    ok = mbar_wait(smem_u32(&bars.v_empty[ring.stage]), ring.phase ^ 1, abortp);
+                    if (!ok) break;
+                    const uint32_t bar = smem_u32(&bars.v_full[ring.stage]);
+                    mbar_arrive_expect_tx(bar, C::kTile);
+                    tma_load_rows(smem_u32(sV) + ring.stage * C::kTile, &tmV, bar, it.tiles.tile(j) * kWinT, hk, it.b);
+                }
+            }
+            if (!ok) let_copies_land();
+        } else if (warp == 9) {
+            // =========================== Q K^T issuer ===========================
+            // (Here and below the whole warp walks through the loop and one elected lane issues: with uniform control flow the
+            // descriptors stay in uniform registers.  From one lane's registers an instruction took about 100 clk to issue.)
+            constexpr uint32_t idesc = make_idesc_f32(kWinT, kWinT, 0, 0, F16);
+            const uint64_t descQ = make_smem_desc_sw128(smem_u32(sQ), 16, 1024), descK = make_smem_desc_sw128(smem_u32(sK), 16, 1024);
+            const bool leader = elect_one();
+            Ring ring;
+            uint32_t n_q = 0, g = 0;
+            bool ok = true;
+            for (int k = 0; ok && load_item(p, k, it); ++k) {
+                const int n = it.tiles.count();
+                if (n == 0) continue;
+                const uint32_t qb = n_q & 1;
+                ok = mbar_wait_warp(smem_u32(&bars.q_full[qb]), (n_q >> 1) & 1, abortp);
+                ++n_q;
+                const uint64_t q0 = descQ + (uint64_t)((qb * C::kTile) >> 4);
+                for (int j = 0; ok && j < n; ++j, ++g) {
+                    if (g >= 2) ok = mbar_wait_warp(smem_u32(&bars.s_free[g & 1]), ((g >> 1) - 1) & 1, abortp);  // scores read
+                    ok = ok && mbar_wait_warp(smem_u32(&bars.k_full[ring.stage]), ring.phase, abortp);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t k0 = descK + (uint64_t)((ring.stage * C::kTile) >> 4);
+                    const uint32_t d_s = tmem + ((g & 1) ? C::kS1 : C::kS0);
+                    if (leader) {
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const uint64_t off = (uint64_t)(((kk / 4) * SUB + (kk % 4) * 32) >> 4);
+                            mma_ss(d_s, q0 + off, k0 + off, idesc, kk > 0);
+                        }
+                        mma_commit(smem_u32(&bars.s_full[g & 1]));
+                        mma_commit(smem_u32(&bars.k_empty[ring.stage]));
+                        if (j == n - 1) mma_commit(smem_u32(&bars.q_empty[qb]));
+                    }
+                    ring.advance<C::kK>();
+                }
+            }
+        } else if (warp == 10) {
+            // =========================== P V issuer ===========================
+            constexpr uint32_t idesc = make_idesc_f32(kWinT, D, 0, 1, F16);
+            const uint64_t descV = make_smem_desc_sw128(smem_u32(sV), SUB, 1024);
+            const bool leader = elect_one();
+            Ring ring;
+            uint32_t n_it = 0, g = 0;
+            bool ok = true;
+            for (int k = 0; ok && load_item(p, k, it); ++k) {
+                const int n = it.tiles.count();
+                if (n == 0) continue;
+                ok = mbar_wait_warp(smem_u32(&bars.o_free), (n_it & 1) ^ 1, abortp);  // the accumulator has been drained
+                ++n_it;
+                for (int j = 0; ok && j < n; ++j, ++g) {
+                    ok = mbar_wait_warp(smem_u32(&bars.v_full[ring.stage]), ring.phase, abortp) &&
+                         mbar_wait_warp(smem_u32(&bars.p_ready[g & 1]), (g >> 1) & 1, abortp);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t v0 = descV + (uint64_t)((ring.stage * C::kTile) >> 4);
+                    const uint32_t d_o = tmem + ((g & 1) ? C::kO1 : C::kO0), a_p = tmem + ((g & 1) ? C::kP1 : C::kP0);
+                    const uint32_t keep = j >= (C::kOwnO ? 2 : 1);
+                    if (leader) {
+#pragma unroll
+                        for (int kk = 0; kk < kWinT / 16; ++kk)
+                            mma_ts(d_o, a_p + kk * 8, v0 + (uint64_t)(kk * 128), idesc, kk > 0 ? 1u : keep);
+                        mma_commit(smem_u32(&bars.v_empty[ring.stage]));
+                        mma_commit(smem_u32(&bars.pv_done[g & 1]));
+                        if (j == n - 1) mma_commit(smem_u32(&bars.o_full));
+                    }
+                    ring.advance<C::kV>();
+                }
+            }
+        }
     } else {
-        // =========================== softmax of slot x ===========================
+        // =========================== softmax warpgroup x ===========================
         reg_inc<192>();
         const int x = warp >> 2, tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t t_s = t_lane + (x ? C::kS1 : C::kS0), t_p = t_lane + (x ? C::kP1 : C::kP0), t_o = t_lane + (x ? C::kO1 : C::kO0);
+        const uint32_t b_s = smem_u32(&bars.s_full[x]), b_own_pv = smem_u32(&bars.pv_done[x]), b_other_pv = smem_u32(&bars.pv_done[x ^ 1]);
         const float c2 = p.scale_log2;
-        uint32_t n_s = 0, n_e = 0;
-        Ring ring;
+        uint32_t g = 0, n_it = 0;
+        bool taken = x == 0;  // d = 128: the publish of the tile in front of this warpgroup's next one has been read, or there is none
         bool ok = true;
         for (int k = 0; ok && load_item(p, k, it); ++k) {
-            const int n = it.both.count();
-            const TileSpan own = x ? it.t1 : it.t0;
-            const KeyRange rng = x ? it.r1 : it.r0;
-            if (own.w1 == 0) {
-                for (int j = 0; j < n; ++j) {
-                    ring.advance<C::kStages>();
-                    ring.advance<C::kStages>();
-                }
-                continue;
-            }
-            const int pos = it.seq.start + it.row0 + x * kSlotRows + tw;
-            // keys that some row of the CTA sees: all others may hold anything
-            const int any_lo = it.t0.w1 == 0 ? it.r1.lo : it.t1.w1 == 0 ? it.r0.lo : min(it.r0.lo, it.r1.lo);
-            const int any_hi = max(it.r0.hi, it.r1.hi);
-            float m_ref = -INFINITY, l = 0.f;
-            bool first = true;
-            for (int j = 0; j < n; ++j) {
-                const int tile = it.both.tile(j), key0 = tile * kWinT;
-                ring.advance<C::kStages>();  // past K
-                const int v_stage = ring.stage;
-                const uint32_t v_phase = ring.phase;
-                ring.advance<C::kStages>();
-                if (!own.has(tile)) continue;
-                const bool full = tile_is_full(p.g, rng, key0);
-                ok = mbar_wait_warp(smem_u32(&bars.s_full[x]), n_s & 1, abortp);
+            const int n = it.tiles.count();
+            if (n == 0) continue;
+            const int pos = it.seq.start + it.row0 + tw;
+            float m_ref = -INFINITY, l = 0.f;  // the reference of this warpgroup's last tile, and its sum in it
+            for (int j = ((g & 1) == (uint32_t)x) ? 0 : 1; j < n; j += 2) {
+                const uint32_t t = g + j;
+                const int key0 = it.tiles.tile(j) * kWinT;
+                ok = mbar_wait_warp(b_s, (t >> 1) & 1, abortp);
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t r[kWinT];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, &r[c * 32]);
                 tc_wait_ld();
-                if constexpr (C::kOwnP) {
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&bars.s_free[x]));
-                }
-                if (!full) {
+                tc_fence_before();
+                mbar_arrive(smem_u32(&bars.s_free[x]));
+                if (!tile_is_full(p.g, it.range, key0)) {
                     const RowMask mk = row_mask(p.g, it.seq, pos, key0);
 #pragma unroll
                     for (int i = 0; i < kWinT; ++i)
                         r[i] = (i < mk.hi && (i >= mk.lo || i < mk.sink)) ? r[i] : 0xff800000u;  // -inf
-                    // V rows that nobody sees: their weight is zero, which times NaN would not be
-                    const int from = any_hi - key0, below = any_lo - key0;
+                    // V rows that no row of this tile sees may hold anything: their weight is zero, which times NaN would not be
+                    const int from = it.range.hi - key0, below = it.range.lo - key0;
                     if (from < kWinT || (below > 0 && p.g.sinks - key0 < below)) {
-                        ok = mbar_wait_warp(smem_u32(&bars.kv_full[v_stage]), v_phase, abortp);
+                        ok = mbar_wait_warp(smem_u32(&bars.v_full[t % C::kV]), (t / C::kV) & 1, abortp);
                         if (!ok) break;
                         if (tw >= from || (tw < below && key0 + tw >= p.g.sinks)) {
-                            uint4* v = reinterpret_cast<uint4*>(sKV + v_stage * C::kTile + tw * 128);
+                            uint4* v = reinterpret_cast<uint4*>(sV + (t % C::kV) * C::kTile + tw * 128);
 #pragma unroll
                             for (int s = 0; s < D / 64; ++s)
 #pragma unroll
@@ -473,89 +452,108 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                         fence_proxy_async_smem();
                     }
                 }
-                float m0 = -INFINITY, m1 = m0, m2 = m0, m3 = m0;
-#pragma unroll
-                for (int i = 0; i < kWinT; i += 8) {
-                    m0 = max3(m0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-                    m1 = max3(m1, __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-                    m2 = max3(m2, __uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
-                    m3 = max3(m3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
+                const float mx = row_max(r) * c2;
+                float m_old = m_ref;  // d = 128: the reference after tile t - 1, which the other warpgroup had
+                if constexpr (!C::kOwnO) {
+                    if (!taken) {
+                        ok = take_reference(&mref[x ^ 1][tw], (((t - 1) >> 1) + 1) & 3u, abortp, m_old);
+                        if (j == 0) m_old = -INFINITY;  // (of the item before: read only so that its slot may be written again)
+                    } else if (j == 0) {
+                        m_old = -INFINITY;
+                    }
+                    taken = false;
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
                 }
-                const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * c2;
-                float alpha = 1.f;
-                bool moved = false;
-                if (mx > m_ref + kRescale) {
-                    alpha = ex2_approx(m_ref - mx);  // m_ref = -inf: 0
-                    moved = m_ref != -INFINITY;
-                    m_ref = mx;
-                }
-                if (!first && __any_sync(0xffffffffu, moved)) {  // the accumulator follows the new reference
-                    ok = mbar_wait_warp(smem_u32(&bars.pv_done[x]), (n_s - 1) & 1, abortp);
+                float m_new = m_old;
+                if (mx > m_old + kRescale) m_new = __uint_as_float(__float_as_uint(mx) & ~3u);
+                if constexpr (!C::kOwnO) *reinterpret_cast<volatile uint32_t*>(&mref[x][tw]) = __float_as_uint(m_new) | (((t >> 1) + 1) & 3u);
+                const bool moved = m_new != m_old && m_old != -INFINITY;
+                if (j > 0 && __any_sync(0xffffffffu, moved)) {  // the accumulator follows, once all products before are in it
+                    ok = C::kOwnO ? mbar_wait_warp(b_own_pv, ((t >> 1) - 1) & 1, abortp) : mbar_wait_warp(b_other_pv, ((t - 1) >> 1) & 1, abortp);
                     if (!ok) break;
                     tc_fence_after();
+                    if (!C::kOwnO || j >= 2) {
+                        const float alpha = moved ? ex2_approx(m_old - m_new) : 1.f;
 #pragma unroll 1
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t o[16];
-                        tmem_ld16(t_o + c * 16, o);
-                        tc_wait_ld();
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t o[16];
+                            tmem_ld16(t_o + c * 16, o);
+                            tc_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                        tmem_st16(t_o + c * 16, o);
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                            tmem_st16(t_o + c * 16, o);
+                        }
                     }
                 }
-                first = false;
-                const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
+                if (m_ref != m_new) {
+                    l *= ex2_approx(m_ref - m_new);  // (m_ref = -inf: l is zero)
+                    m_ref = m_new;
+                }
+                const float neg_m = (m_new == -INFINITY) ? 0.f : -m_new;
                 const uint64_t c22 = pack_f32x2(c2, c2), nm2 = pack_f32x2(neg_m, neg_m);
                 uint64_t sum01 = pack_f32x2(0.f, 0.f), sum23 = sum01;
-                if constexpr (C::kOwnP) {  // the last P of this slot has been read
-                    if (n_s > 0) ok = mbar_wait_warp(smem_u32(&bars.pv_done[x]), (n_s - 1) & 1, abortp);
+#pragma unroll
+                for (int i = 0; i < kWinT; i += 4) {
+                    float x0, x1, x2, x3;
+                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), c22, nm2), x0, x1);
+                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), c22, nm2), x2, x3);
+                    const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
+                    sum01 = add_f32x2(sum01, pack_f32x2(p0, p1));
+                    sum23 = add_f32x2(sum23, pack_f32x2(p2, p3));
+                    r[i / 2] = pack_16x2<F16>(p0, p1);
+                    r[i / 2 + 1] = pack_16x2<F16>(p2, p3);
+                }
+                if (t >= 2) {  // this warpgroup's last P has been read
+                    ok = mbar_wait_warp(b_own_pv, ((t >> 1) - 1) & 1, abortp);
                     if (!ok) break;
                     tc_fence_after();
                 }
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                    for (int i = half * 64; i < half * 64 + 64; i += 4) {
-                        float x0, x1, x2, x3;
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), c22, nm2), x0, x1);
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), c22, nm2), x2, x3);
-                        const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
-                        sum01 = add_f32x2(sum01, pack_f32x2(p0, p1));
-                        sum23 = add_f32x2(sum23, pack_f32x2(p2, p3));
-                        r[i / 2] = pack_16x2<F16>(p0, p1);
-                        r[i / 2 + 1] = pack_16x2<F16>(p2, p3);
-                    }
-                    tmem_st32(t_p + half * 32, &r[half * 32]);
-                    tc_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&bars.p_half[x][half]));
-                }
+                tmem_st32(t_p, r);
+                tmem_st32(t_p + 32, r + 32);
                 float s0, s1, s2, s3;
                 unpack_f32x2(sum01, s0, s1);
                 unpack_f32x2(sum23, s2, s3);
-                l = l * alpha + ((s0 + s1) + (s2 + s3));
-                ++n_s;
+                l += (s0 + s1) + (s2 + s3);
+                tc_wait_st();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&bars.p_ready[x]));
             }
             if (!ok) break;
-            ok = mbar_wait_warp(smem_u32(&bars.e_taken[x]), (n_e & 1) ^ 1, abortp);
+            const uint32_t last = g + n - 1;
+            if constexpr (!C::kOwnO) {
+                if ((last & 1) != (uint32_t)x) {  // the other warpgroup had the last tile: its reference is the item's
+                    float m_end;
+                    ok = take_reference(&mref[x ^ 1][tw], ((last >> 1) + 1) & 3u, abortp, m_end);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    taken = true;
+                    if (m_ref != m_end) l *= ex2_approx(m_ref - m_end);
+                }
+            }
+            ok = mbar_wait_warp(smem_u32(&bars.e_taken), (n_it & 1) ^ 1, abortp);
             if (!ok) break;
-            fin_m[x][tw] = m_ref;
-            fin_l[x][tw] = l;
-            mbar_arrive(smem_u32(&bars.e_ready[x]));
-            ++n_e;
+            lfin[x][tw] = l;
+            if constexpr (C::kOwnO)
+                mref[x][tw] = __float_as_uint(m_ref);
+            else if ((last & 1) == (uint32_t)x)
+                mfin[tw] = m_ref;
+            mbar_arrive(smem_u32(&bars.e_ready));
+            ++n_it;
+            g += n;
         }
     }
 
     tc_fence_before();
     __syncthreads();
     if (tid == 0 && abort_flag) atomicExch(&g_window_status, (int)BSA_ERR_DEVICE_TIMEOUT);
-    if (warp == 13) tmem_dealloc(tmem, kTmemCols);
+    if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 
 template <int D, bool F16>
 cudaError_t launch_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, Params p, cudaStream_t stream) {
     CUtensorMap tq, tk, tv;
-    if (!encode_view_map(&tq, Q, a.g.N, a.g.heads, a.g.batch, D, kSlotRows, F16) ||
+    if (!encode_view_map(&tq, Q, a.g.N, a.g.heads, a.g.batch, D, kWinT, F16) ||
         !encode_view_map(&tk, K, a.g.N_kv, a.g.heads_kv, a.g.batch, D, kWinT, F16) ||
         !encode_view_map(&tv, V, a.g.N_kv, a.g.heads_kv, a.g.batch, D, kWinT, F16))
         return cudaErrorInvalidValue;
@@ -622,7 +620,7 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     p.o_batch = O->batch; p.o_head = O->head; p.o_row = O->row;
     p.LSE = LSE;
     p.scale_log2 = a.scale * 1.4426950408889634f;
-    p.n_qt = (a.g.N + kCtaRows - 1) / kCtaRows;
+    p.n_qt = (a.g.N + kWinT - 1) / kWinT;
     const int64_t items = (int64_t)p.n_qt * a.g.batch * a.g.heads;
     if (items > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
     p.n_items = (int)items;

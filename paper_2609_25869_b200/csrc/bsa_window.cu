@@ -6,17 +6,16 @@
 // around the diagonal and the sinks' tiles, computed from the rows' positions (no list, no mask in memory).  Bounds on a
 // row's columns are applied only in tiles that some row does not see whole.
 //   warps 0-3 / 4-7 : softmax warpgroups (thread = row); tile t belongs to warpgroup t mod 2, and S and P buffer t mod 2 with it
-//   warp 8 : Q and K producer   warp 9 : Q K^T issuer   warp 10 : P V issuer   warp 11 : V producer   warps 12-15 : epilogue
+//   warp 8 : Q and K producer   warp 9 : Q K^T issuer   warp 10 : P V issuer   warp 11 : V producer
+//   warps 12-15 : references: each row's running maximum, the accumulator's rescaling, and the epilogue
 // Work per tile: 4 * 128 * 128 * d flops (1024 clk at d = 128) and 128 * 128 exponentials (1024 clk at 16 per clk and SM): at
-// d = 128 the tensor pipe and the special-function unit bind together, at d = 64 the latter alone.  A warpgroup's softmax takes
-// about 2000 clk of a tile (maxima, exponentials, their latencies), so two must run at once and neither may wait for
-// products: S and P have their own columns, Q K^T runs two tiles ahead.
-// (Measured against 256 rows per CTA with a slot of 128 per warpgroup and P in the place of S, which reads K and V from shared
-// memory half as often: 115200 tokens, 24 heads, window 8191, d = 128: 12.1 ms; a slot's softmax, P V and Q K^T then follow each
-// other, 4400 clk per tile and slot.)
-// d = 128: tensor memory has room for one accumulator, so both warpgroups follow one reference maximum per row, handed from tile to
-// tile through shared memory.  d = 64: each has an accumulator and a reference of its own, joined by the epilogue.
-// Tensor-memory columns: S0 0, S1 128, O 256 (d = 64: O0 256, O1 320), P0 384, P1 448.
+// d = 128 the tensor pipe and the special-function unit bind together, at d = 64 the latter alone.  A warpgroup takes longer
+// than that over a tile (latencies), so two must run at once and neither may wait: S and P have their own columns, Q K^T runs
+// two tiles ahead, and the maxima are found by a third warpgroup while the tile in front is still in the softmax.  That also
+// makes one reference maximum per row for both warpgroups, and one accumulator.
+// On one GPU, 25088 keys for 4736 rows, d = 128, 12 heads: 256 rows per CTA, a slot of 128 per warpgroup with P in the place of S (so that a
+// slot's softmax, P V and Q K^T follow each other) 900 TFLOP/s; 128 rows, warpgroups finding the maxima themselves 1100.
+// Tensor-memory columns: S0 0, S1 128, O 256, P0 384, P1 448.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -38,11 +37,10 @@ constexpr float kRescale = 8.0f;  // log2 units: P stays below 2^8 between resca
 
 template <int D>
 struct Cfg {
-    static constexpr bool kOwnO = (D == 64);              // an accumulator per softmax warpgroup
     static constexpr int kTile = kWinT * D * 2;           // bytes of a 128-row tile of Q, K or V
     static constexpr int kK = (D == 64) ? 4 : 2, kV = (D == 64) ? 4 : 3;  // tiles in the rings
     static constexpr int kSmem = (2 + kK + kV) * kTile;   // two Q tiles
-    static constexpr uint32_t kS0 = 0, kS1 = 128, kO0 = 256, kO1 = kOwnO ? 320 : 256, kP0 = 384, kP1 = 448;
+    static constexpr uint32_t kS0 = 0, kS1 = 128, kO = 256, kP0 = 384, kP1 = 448;
 };
 
 struct Params {
@@ -59,7 +57,7 @@ struct Params {
 struct __align__(8) Barriers {
     uint64_t q_full[2], q_empty[2];
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
-    uint64_t s_full[2], s_free[2], p_ready[2], pv_done[2];
+    uint64_t s_full[2], s_free[2], ref_ready[2], p_ready[2], pv_done[2];
     uint64_t o_full, o_free, e_ready, e_taken;
 };
 
@@ -120,37 +118,20 @@ struct Ring {
     }
 };
 
-__device__ __forceinline__ float row_max(const uint32_t (&r)[kWinT]) {
-    float m0 = -INFINITY, m1 = m0, m2 = m0, m3 = m0;
+// P in the place of the scores: exp2(s * c2 + neg_m), rounded and packed by pairs; its unrounded sum.
+template <bool F16>
+__device__ __forceinline__ void exp_keys(uint32_t (&r)[kWinT], uint64_t c22, uint64_t neg_m2, uint64_t& sum01, uint64_t& sum23) {
 #pragma unroll
-    for (int i = 0; i < kWinT; i += 8) {
-        m0 = max3(m0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-        m1 = max3(m1, __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-        m2 = max3(m2, __uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
-        m3 = max3(m3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
+    for (int i = 0; i < kWinT; i += 4) {
+        float x0, x1, x2, x3;
+        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), c22, neg_m2), x0, x1);
+        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), c22, neg_m2), x2, x3);
+        const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
+        sum01 = add_f32x2(sum01, pack_f32x2(p0, p1));
+        sum23 = add_f32x2(sum23, pack_f32x2(p2, p3));
+        r[i / 2] = pack_16x2<F16>(p0, p1);
+        r[i / 2 + 1] = pack_16x2<F16>(p2, p3);
     }
-    return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-}
-
-// A word of a row's reference: the value's two lowest mantissa bits make room for (publish index + 1) mod 4, so that one read
-// tells whether the value is the one that is waited for.  False: the wait expired.
-__device__ __forceinline__ bool take_reference(volatile uint32_t* slot, uint32_t tag, volatile uint32_t* abortp, float& m) {
-    uint32_t word = *slot;
-    long long t0 = 0;
-    for (uint32_t spins = 1; (word & 3u) != tag; ++spins) {
-        if ((spins & 63u) == 0) {
-            if (*abortp) return false;
-            const long long now = clock64();
-            if (t0 == 0) t0 = now;
-            if (now - t0 > *reinterpret_cast<volatile long long*>(&g_wait_limit_cycles)) {
-                *abortp = 1;
-                return false;
-            }
-        }
-        word = *slot;
-    }
-    m = __uint_as_float(word & ~3u);
-    return true;
 }
 
 template <int D, bool F16>
@@ -164,9 +145,8 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     uint8_t* sK = sQ + 2 * C::kTile;
     uint8_t* sV = sK + C::kK * C::kTile;
     __shared__ Barriers bars;
-    __shared__ uint32_t mref[2][kWinT];  // d = 128: [publishing warpgroup][row]; d = 64: an item's references, plain
-    __shared__ float lfin[2][kWinT];     // an item's row sums, by warpgroup (d = 128: in its final reference)
-    __shared__ float mfin[kWinT];        // d = 128: that reference (log2 domain)
+    __shared__ float mref[2][kWinT];               // [tile mod 2][row]: the tile's reference maximum (log2 domain)
+    __shared__ float lfin[2][kWinT];  // [warpgroup][row]: an item's row sums, in its last reference
     __shared__ uint32_t tmem_base_s, abort_flag;
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -181,6 +161,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             mbar_init(smem_u32(&bars.q_empty[i]), 1);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
             mbar_init(smem_u32(&bars.s_free[i]), 128);
+            mbar_init(smem_u32(&bars.ref_ready[i]), 128);
             mbar_init(smem_u32(&bars.p_ready[i]), 128);
             mbar_init(smem_u32(&bars.pv_done[i]), 1);
         }
@@ -196,7 +177,6 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         mbar_init(smem_u32(&bars.e_taken), 128);
         fence_mbar_init();
     }
-    if (tid < 2 * kWinT) (&mref[0][0])[tid] = 0u;  // a tag that matches no first publish
     if (warp == 9) {
         tmem_alloc(smem_u32(&tmem_base_s), kTmemCols);
         tmem_relinquish();
@@ -214,19 +194,79 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     Item it;
 
     if (warp >= 12) {
-        // =========================== epilogue ===========================
+        // =========================== references and epilogue ===========================
         reg_dec<80>();
         const int tw = tid & 127;
-        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        uint32_t n_it = 0, g = 0;  // items with tiles, tiles so far
-        for (int k = 0; load_item(p, k, it); ++k) {
-            const int row = it.row0 + tw;
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_lane + C::kO;
+        const float c2 = p.scale_log2;
+        uint32_t n_it = 0, g = 0;  // items finished (with tiles), tiles in front of the item
+        // The reference of tile j of an item (running index t), from `m` of the tile before.
+        auto reference = [&](const Item& w, int j, uint32_t t, float& m) -> bool {
+            const uint32_t x = t & 1;
+            const int key0 = w.tiles.tile(j) * kWinT;
+            const bool full = tile_is_full(p.g, w.range, key0);
+            if (!mbar_wait_warp(smem_u32(&bars.s_full[x]), (t >> 1) & 1, abortp)) return false;
+            tc_fence_after();
+            float m0 = -INFINITY, m1 = m0, m2 = m0, m3 = m0;
+#pragma unroll
+            for (int c = 0; c < kWinT / 32; ++c) {
+                uint32_t r[32];
+                tmem_ld32(t_lane + (x ? C::kS1 : C::kS0) + c * 32, r);
+                tc_wait_ld();
+                if (!full) {
+                    const RowMask mk = row_mask(p.g, w.seq, w.seq.start + w.row0 + tw, key0 + c * 32);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) r[i] = (i < mk.hi && (i >= mk.lo || i < mk.sink)) ? r[i] : 0xff800000u;  // -inf
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    m0 = max3(m0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+                    m1 = max3(m1, __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                    m2 = max3(m2, __uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
+                    m3 = max3(m3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
+                }
+            }
+            const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * c2;
+            const float m_old = m;
+            if (mx > m + kRescale) m = mx;
+            const bool moved = m != m_old && m_old != -INFINITY;
+            if (j > 0 && __any_sync(0xffffffffu, moved)) {  // the accumulator follows, once all products before are in it
+                if (!mbar_wait_warp(smem_u32(&bars.pv_done[x ^ 1]), ((t - 1) >> 1) & 1, abortp)) return false;
+                tc_fence_after();
+                const float alpha = moved ? ex2_approx(m_old - m) : 1.f;
+#pragma unroll 1
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(t_o + c * 32, o);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                    tmem_st32(t_o + c * 32, o);
+                }
+                tc_wait_st();
+            }
+            mref[x][tw] = m;
+            tc_fence_before();
+            mbar_arrive(smem_u32(&bars.ref_ready[x]));
+            return true;
+        };
+        bool more = load_item(p, 0, it), ok = true, begun = false;  // begun: this item's first reference is out
+        float m = -INFINITY;
+        for (int k = 0; more; ++k) {
+            const Item w = it;
+            const int row = w.row0 + tw;
             const bool row_ok = row < p.g.N;
-            const int pos = it.seq.start + row;
-            const bool seen = pos >= 0 && pos < it.seq.len;
-            uint16_t* orow = p.O + (long long)it.b * p.o_batch + (long long)it.h * p.o_head + (long long)row * p.o_row;
-            float* lse_out = p.LSE + ((long long)it.b * p.g.heads + it.h) * p.g.N + row;
-            const int n = it.tiles.count();
+            const int pos = w.seq.start + row;
+            const bool seen = pos >= 0 && pos < w.seq.len;
+            uint16_t* orow = p.O + (long long)w.b * p.o_batch + (long long)w.h * p.o_head + (long long)row * p.o_row;
+            float* lse_out = p.LSE + ((long long)w.b * p.g.heads + w.h) * p.g.N + row;
+            const int n = w.tiles.count();
+            for (int j = begun ? 1 : 0; ok && j < n; ++j) ok = reference(w, j, g + j, m);
+            if (!ok) break;
+            g += (uint32_t)n;
+            more = load_item(p, k + 1, it);
+            begun = false;
+            float m_next = -INFINITY;
             if (n == 0) {  // no row of the tile sees anything
                 if (row_ok) {
 #pragma unroll
@@ -235,61 +275,39 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 }
                 continue;
             }
-            if (!mbar_wait_warp(smem_u32(&bars.e_ready), n_it & 1, abortp)) break;
-            // warpgroup a had the item's first tile: an item's bits do not depend on its place among the CTA's
-            const uint32_t a = g & 1u;
-            float l, m, wa = 1.f, wb = 0.f;
-            if constexpr (C::kOwnO) {
-                const float ma = __uint_as_float(mref[a][tw]), mb = __uint_as_float(mref[a ^ 1u][tw]);
-                m = fmaxf(ma, mb);
-                wa = ma == -INFINITY ? 0.f : ex2_approx(ma - m);
-                wb = mb == -INFINITY ? 0.f : ex2_approx(mb - m);
-                l = fmaf(lfin[a ^ 1u][tw], wb, lfin[a][tw] * wa);
-            } else {
-                l = lfin[a][tw] + lfin[a ^ 1u][tw];
-                m = mfin[tw];
+            // the next item's first tile comes before this item's end: one warpgroup has work until the accumulator is drained
+            if (more && it.tiles.count() > 0) {
+                ok = reference(it, 0, g, m_next);
+                if (!ok) break;
+                begun = true;
             }
+            if (!mbar_wait_warp(smem_u32(&bars.e_ready), n_it & 1, abortp)) break;
+            const float l = lfin[0][tw] + lfin[1][tw];
             mbar_arrive(smem_u32(&bars.e_taken));
             const bool any = seen && l > 0.f;
             const float inv = any ? 1.f / l : 0.f;
             if (row_ok) *lse_out = any ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
+            m = m_next;
             if (!mbar_wait_warp(smem_u32(&bars.o_full), n_it & 1, abortp)) break;
             ++n_it;
-            g += (uint32_t)n;
             tc_fence_after();
-            constexpr int CW = C::kOwnO ? 16 : 32;
-            const float sa = inv * wa, sb = inv * wb;
 #pragma unroll 1
-            for (int c = 0; c < D / CW; ++c) {
-                uint32_t o[CW];
-                if constexpr (C::kOwnO) {
-                    uint32_t ob[CW];
-                    tmem_ld16(t_lane + (a ? C::kO1 : C::kO0) + c * CW, o);
-                    tmem_ld16(t_lane + (a ? C::kO0 : C::kO1) + c * CW, ob);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < CW; ++e) {
-                        const float v = __uint_as_float(o[e]) * sa;
-                        o[e] = __float_as_uint(n > 1 ? fmaf(__uint_as_float(ob[e]), sb, v) : v);  // (one tile: the other is stale)
-                    }
-                } else {
-                    tmem_ld32(t_lane + C::kO0 + c * CW, o);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < CW; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * sa);
-                }
-                if (c == D / CW - 1) {  // drained: the next item's first P V may overwrite it
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld32(t_o + c * 32, o);
+                tc_wait_ld();
+                if (c == D / 32 - 1) {  // drained: the next item's first P V may overwrite it
                     tc_fence_before();
                     mbar_arrive(smem_u32(&bars.o_free));
                 }
                 if (row_ok) {
 #pragma unroll
-                    for (int q = 0; q < CW / 8; ++q) {
+                    for (int q = 0; q < 4; ++q) {
                         uint32_t v[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            v[e] = seen ? pack_16x2<F16>(__uint_as_float(o[q * 8 + 2 * e]), __uint_as_float(o[q * 8 + 2 * e + 1])) : 0u;
-                        *reinterpret_cast<uint4*>(orow + c * CW + q * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+                            v[e] = seen ? pack_16x2<F16>(__uint_as_float(o[q * 8 + 2 * e]) * inv, __uint_as_float(o[q * 8 + 2 * e + 1]) * inv) : 0u;
+                        *reinterpret_cast<uint4*>(orow + c * 32 + q * 8) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
             }
@@ -390,8 +408,8 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t v0 = descV + (uint64_t)((ring.stage * C::kTile) >> 4);
-                    const uint32_t d_o = tmem + ((g & 1) ? C::kO1 : C::kO0), a_p = tmem + ((g & 1) ? C::kP1 : C::kP0);
-                    const uint32_t keep = j >= (C::kOwnO ? 2 : 1);
+                    const uint32_t d_o = tmem + C::kO, a_p = tmem + ((g & 1) ? C::kP1 : C::kP0);
+                    const uint32_t keep = j > 0;
                     if (leader) {
 #pragma unroll
                         for (int kk = 0; kk < kWinT / 16; ++kk)
@@ -409,11 +427,11 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         reg_inc<192>();
         const int x = warp >> 2, tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t t_s = t_lane + (x ? C::kS1 : C::kS0), t_p = t_lane + (x ? C::kP1 : C::kP0), t_o = t_lane + (x ? C::kO1 : C::kO0);
-        const uint32_t b_s = smem_u32(&bars.s_full[x]), b_own_pv = smem_u32(&bars.pv_done[x]), b_other_pv = smem_u32(&bars.pv_done[x ^ 1]);
+        const uint32_t t_s = t_lane + (x ? C::kS1 : C::kS0), t_p = t_lane + (x ? C::kP1 : C::kP0);
+        const uint32_t b_ref = smem_u32(&bars.ref_ready[x]), b_pv = smem_u32(&bars.pv_done[x]);
         const float c2 = p.scale_log2;
+        const uint64_t c22 = pack_f32x2(c2, c2);
         uint32_t g = 0, n_it = 0;
-        bool taken = x == 0;  // d = 128: the publish of the tile in front of this warpgroup's next one has been read, or there is none
         bool ok = true;
         for (int k = 0; ok && load_item(p, k, it); ++k) {
             const int n = it.tiles.count();
@@ -423,16 +441,18 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             for (int j = ((g & 1) == (uint32_t)x) ? 0 : 1; j < n; j += 2) {
                 const uint32_t t = g + j;
                 const int key0 = it.tiles.tile(j) * kWinT;
-                ok = mbar_wait_warp(b_s, (t >> 1) & 1, abortp);
+                const bool full = tile_is_full(p.g, it.range, key0);
+                ok = mbar_wait_warp(b_ref, (t >> 1) & 1, abortp);  // (which is behind s_full)
                 if (!ok) break;
                 tc_fence_after();
+                const float m = mref[x][tw];
                 uint32_t r[kWinT];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, &r[c * 32]);
                 tc_wait_ld();
                 tc_fence_before();
                 mbar_arrive(smem_u32(&bars.s_free[x]));
-                if (!tile_is_full(p.g, it.range, key0)) {
+                if (!full) {
                     const RowMask mk = row_mask(p.g, it.seq, pos, key0);
 #pragma unroll
                     for (int i = 0; i < kWinT; ++i)
@@ -452,60 +472,16 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                         fence_proxy_async_smem();
                     }
                 }
-                const float mx = row_max(r) * c2;
-                float m_old = m_ref;  // d = 128: the reference after tile t - 1, which the other warpgroup had
-                if constexpr (!C::kOwnO) {
-                    if (!taken) {
-                        ok = take_reference(&mref[x ^ 1][tw], (((t - 1) >> 1) + 1) & 3u, abortp, m_old);
-                        if (j == 0) m_old = -INFINITY;  // (of the item before: read only so that its slot may be written again)
-                    } else if (j == 0) {
-                        m_old = -INFINITY;
-                    }
-                    taken = false;
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
+                if (m_ref != m) {
+                    l *= ex2_approx(m_ref - m);  // (m_ref = -inf: l is zero)
+                    m_ref = m;
                 }
-                float m_new = m_old;
-                if (mx > m_old + kRescale) m_new = __uint_as_float(__float_as_uint(mx) & ~3u);
-                if constexpr (!C::kOwnO) *reinterpret_cast<volatile uint32_t*>(&mref[x][tw]) = __float_as_uint(m_new) | (((t >> 1) + 1) & 3u);
-                const bool moved = m_new != m_old && m_old != -INFINITY;
-                if (j > 0 && __any_sync(0xffffffffu, moved)) {  // the accumulator follows, once all products before are in it
-                    ok = C::kOwnO ? mbar_wait_warp(b_own_pv, ((t >> 1) - 1) & 1, abortp) : mbar_wait_warp(b_other_pv, ((t - 1) >> 1) & 1, abortp);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (!C::kOwnO || j >= 2) {
-                        const float alpha = moved ? ex2_approx(m_old - m_new) : 1.f;
-#pragma unroll 1
-                        for (int c = 0; c < D / 16; ++c) {
-                            uint32_t o[16];
-                            tmem_ld16(t_o + c * 16, o);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                            tmem_st16(t_o + c * 16, o);
-                        }
-                    }
-                }
-                if (m_ref != m_new) {
-                    l *= ex2_approx(m_ref - m_new);  // (m_ref = -inf: l is zero)
-                    m_ref = m_new;
-                }
-                const float neg_m = (m_new == -INFINITY) ? 0.f : -m_new;
-                const uint64_t c22 = pack_f32x2(c2, c2), nm2 = pack_f32x2(neg_m, neg_m);
+                const float neg_m = (m == -INFINITY) ? 0.f : -m;
+                const uint64_t nm2 = pack_f32x2(neg_m, neg_m);
                 uint64_t sum01 = pack_f32x2(0.f, 0.f), sum23 = sum01;
-#pragma unroll
-                for (int i = 0; i < kWinT; i += 4) {
-                    float x0, x1, x2, x3;
-                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), c22, nm2), x0, x1);
-                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), c22, nm2), x2, x3);
-                    const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
-                    sum01 = add_f32x2(sum01, pack_f32x2(p0, p1));
-                    sum23 = add_f32x2(sum23, pack_f32x2(p2, p3));
-                    r[i / 2] = pack_16x2<F16>(p0, p1);
-                    r[i / 2 + 1] = pack_16x2<F16>(p2, p3);
-                }
+                exp_keys<F16>(r, c22, nm2, sum01, sum23);
                 if (t >= 2) {  // this warpgroup's last P has been read
-                    ok = mbar_wait_warp(b_own_pv, ((t >> 1) - 1) & 1, abortp);
+                    ok = mbar_wait_warp(b_pv, ((t >> 1) - 1) & 1, abortp);
                     if (!ok) break;
                     tc_fence_after();
                 }
@@ -521,23 +497,16 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             }
             if (!ok) break;
             const uint32_t last = g + n - 1;
-            if constexpr (!C::kOwnO) {
-                if ((last & 1) != (uint32_t)x) {  // the other warpgroup had the last tile: its reference is the item's
-                    float m_end;
-                    ok = take_reference(&mref[x ^ 1][tw], ((last >> 1) + 1) & 3u, abortp, m_end);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    taken = true;
-                    if (m_ref != m_end) l *= ex2_approx(m_ref - m_end);
-                }
+            if ((last & 1) != (uint32_t)x) {  // the other warpgroup had the last tile
+                // (its reference stays in place until both warpgroups have arrived below)
+                ok = mbar_wait_warp(smem_u32(&bars.ref_ready[x ^ 1]), (last >> 1) & 1, abortp);
+                if (!ok) break;
+                const float m = mref[x ^ 1][tw];
+                if (m_ref != m) l *= ex2_approx(m_ref - m);
             }
             ok = mbar_wait_warp(smem_u32(&bars.e_taken), (n_it & 1) ^ 1, abortp);
             if (!ok) break;
             lfin[x][tw] = l;
-            if constexpr (C::kOwnO)
-                mref[x][tw] = __float_as_uint(m_ref);
-            else if ((last & 1) == (uint32_t)x)
-                mfin[tw] = m_ref;
             mbar_arrive(smem_u32(&bars.e_ready));
             ++n_it;
             g += n;

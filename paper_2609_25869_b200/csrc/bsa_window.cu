@@ -208,16 +208,12 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             if (!mbar_wait_warp(smem_u32(&bars.s_full[x]), (t >> 1) & 1, abortp)) return false;
             tc_fence_after();
             float m0 = -INFINITY, m1 = m0, m2 = m0, m3 = m0;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < kWinT / 32; ++c) {
                 uint32_t r[32];
                 tmem_ld32(t_lane + (x ? C::kS1 : C::kS0) + c * 32, r);
                 tc_wait_ld();
-                if (!full) {
-                    const RowMask mk = row_mask(p.g, w.seq, w.seq.start + w.row0 + tw, key0 + c * 32);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) r[i] = (i < mk.hi && (i >= mk.lo || i < mk.sink)) ? r[i] : 0xff800000u;  // -inf
-                }
+                if (!full) hide(r, row_bits(p.g, w.seq, w.seq.start + w.row0 + tw, key0 + c * 32));
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
                     m0 = max3(m0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
@@ -453,10 +449,8 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 tc_fence_before();
                 mbar_arrive(smem_u32(&bars.s_free[x]));
                 if (!full) {
-                    const RowMask mk = row_mask(p.g, it.seq, pos, key0);
 #pragma unroll
-                    for (int i = 0; i < kWinT; ++i)
-                        r[i] = (i < mk.hi && (i >= mk.lo || i < mk.sink)) ? r[i] : 0xff800000u;  // -inf
+                    for (int c = 0; c < 4; ++c) hide(r + c * 32, row_bits(p.g, it.seq, pos, key0 + c * 32));
                     // V rows that no row of this tile sees may hold anything: their weight is zero, which times NaN would not be
                     const int from = it.range.hi - key0, below = it.range.lo - key0;
                     if (from < kWinT || (below > 0 && p.g.sinks - key0 < below)) {

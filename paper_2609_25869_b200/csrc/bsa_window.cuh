@@ -82,17 +82,16 @@ __device__ __forceinline__ TileSpan join(const TileSpan& a, const TileSpan& b) {
     return t;
 }
 
-// Row i's view of a tile that starts at key0, as bounds on the column: it sees c < hi with c >= lo or c < sink.
-struct RowMask {
-    int lo, hi, sink;
-};
-__device__ __forceinline__ RowMask row_mask(const WindowGeom& g, const Sequence& s, int pos, int key0) {
-    RowMask m;
-    const bool seen = pos >= 0 && pos < s.len;
-    m.hi = (seen ? min(s.len, pos + g.right + 1) : 0) - key0;
-    m.lo = pos - g.left - key0;
-    m.sink = g.sinks - key0;
-    return m;
+// What the row at `pos` sees of the 32 keys from key0 on, one bit each.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t row_bits(const WindowGeom& g, const Sequence& s, int pos, int key0) {
+    const int hi = (pos >= 0 && pos < s.len) ? min(s.len, pos + g.right + 1) : 0;
+    return bits_below(hi - key0) & (~bits_below(pos - g.left - key0) | bits_below(g.sinks - key0));
+}
+// Hidden scores become -inf: two instructions each (a test of the two bounds branched, 7000 clk a tile).
+__device__ __forceinline__ void hide(uint32_t* r, uint32_t bits) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = (bits & (1u << i)) ? r[i] : 0xff800000u;
 }
 
 // ---- host side (bsa_window.cu) ----

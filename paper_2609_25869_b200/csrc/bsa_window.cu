@@ -535,7 +535,14 @@ cudaError_t launch_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view
 
 }  // namespace
 
-cudaError_t window_status_word(int** out) { return cudaGetSymbolAddress(reinterpret_cast<void**>(out), g_window_status); }
+cudaError_t window_status_word(int device, int** out) {
+    static std::atomic<int*> word[kMaxDevices];
+    *out = word[device].load(std::memory_order_acquire);
+    if (*out) return cudaSuccess;
+    const cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(out), g_window_status);
+    if (e == cudaSuccess) word[device].store(*out, std::memory_order_release);
+    return e;
+}
 
 bsa_status_t window_args(const bsa_window_desc_t* t, WindowArgs* a) {
     if (!t || t->batch < 1 || t->heads < 1 || t->heads_kv < 1 || t->N < 1 || t->N_kv < 1 || t->heads % t->heads_kv) return BSA_ERR_INVALID_ARG;
@@ -589,6 +596,15 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     p.n_items = (int)items;
     p.longest_first = a.g.left >= a.g.N_kv;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
+    // Up to 32 rows per key head share their keys in one pass of the kernel for few rows.
+    if ((int64_t)a.g.N * a.g.group <= 32) {
+        const cudaError_t e = launch_window_rows(a, *Q, *K, *V, *O, LSE, stream);
+        if (e != cudaSuccess) {
+            set_cuda_err(e, "bsa_window_forward");
+            return BSA_ERR_CUDA;
+        }
+        return BSA_OK;
+    }
     const cudaError_t e = a.d == 64 ? (a.f16 ? launch_rows<64, true>(a, *Q, *K, *V, p, stream) : launch_rows<64, false>(a, *Q, *K, *V, p, stream))
                                     : (a.f16 ? launch_rows<128, true>(a, *Q, *K, *V, p, stream) : launch_rows<128, false>(a, *Q, *K, *V, p, stream));
     if (e != cudaSuccess) {
@@ -602,7 +618,10 @@ extern "C" bsa_status_t bsa_window_status(int* status_out) {
     if (!status_out) return BSA_ERR_INVALID_ARG;
     int* word = nullptr;
     int v = 0;
-    cudaError_t e = window_status_word(&word);
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess && device >= kMaxDevices) return BSA_ERR_CUDA;
+    if (e == cudaSuccess) e = window_status_word(device, &word);
     if (e == cudaSuccess) e = cudaMemcpy(&v, word, sizeof v, cudaMemcpyDeviceToHost);
     if (e == cudaSuccess && v != 0) e = cudaMemset(word, 0, sizeof v);
     if (e != cudaSuccess) {

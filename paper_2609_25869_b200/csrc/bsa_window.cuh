@@ -7,8 +7,8 @@
 
 namespace bsa {
 
-// Set by kernels whose bounded wait expired; read by bsa_window_status.  One word per device.
-cudaError_t window_status_word(int** out);
+// The device's word that kernels set whose bounded wait expired; read by bsa_window_status.
+cudaError_t window_status_word(int device, int** out);
 
 constexpr int kWinT = 128;             // rows and keys of a tile
 constexpr int kWinNoLimit = 1 << 29;   // left or right where there is no limit: beyond every position
@@ -104,5 +104,8 @@ struct WindowArgs {
 };
 // Checks a description and fills `a` in; the current device becomes the call's.
 bsa_status_t window_args(const bsa_window_desc_t* t, WindowArgs* a);
+// Forward for few rows (bsa_window_rows.cu).
+cudaError_t launch_window_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
+                               float* LSE, cudaStream_t stream);
 
 }  // namespace bsa

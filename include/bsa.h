@@ -418,6 +418,11 @@ typedef struct bsa_window_desc {
 } bsa_window_desc_t;
 BSA_API bsa_status_t bsa_window_forward(const bsa_window_desc_t* desc, const bsa_view_t* Q, const bsa_view_t* K,
                                         const bsa_view_t* V, const bsa_view_t* O, float* LSE_dev, void* stream);
+BSA_API int64_t bsa_window_workspace_bytes(const bsa_window_desc_t* desc); /* 0 for a description that the calls refuse */
+BSA_API bsa_status_t bsa_window_backward(const bsa_window_desc_t* desc, const bsa_view_t* Q, const bsa_view_t* K,
+                                         const bsa_view_t* V, const bsa_view_t* O, const float* LSE_dev, const bsa_view_t* dO,
+                                         const bsa_view_t* dQ, const bsa_view_t* dK, const bsa_view_t* dV, void* workspace_dev,
+                                         int64_t workspace_bytes, void* stream);
 /* The current device's status word of the windowed kernels, and clears it: 0, or BSA_ERR_DEVICE_TIMEOUT if a bounded wait of any of
  * their calls has expired since the last look (that call's outputs are undefined then).  Synchronises the device. */
 BSA_API bsa_status_t bsa_window_status(int* status_out);

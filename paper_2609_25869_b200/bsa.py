@@ -99,6 +99,9 @@ def lib() -> ctypes.CDLL:
     L.bsa_mask_stats_noalloc.argtypes = [vp, i32, i32, i32, vp, vp]
     L.bsa_rope.argtypes = [ctypes.c_char_p] * 5 + [vp]
     L.bsa_window_forward.argtypes = [ctypes.c_char_p] * 5 + [vp, vp]
+    L.bsa_window_backward.argtypes = [ctypes.c_char_p] * 5 + [vp] + [ctypes.c_char_p] * 4 + [vp, i64, vp]
+    L.bsa_window_workspace_bytes.argtypes = [ctypes.c_char_p]
+    L.bsa_window_workspace_bytes.restype = i64
     L.bsa_window_status.argtypes = [ctypes.POINTER(ctypes.c_int)]
     L.bsa_plan_get_info.argtypes = [vp, ctypes.POINTER(PlanInfo)]
     L.bsa_plan_export_csr.argtypes = [vp, vp, vp]
@@ -508,6 +511,33 @@ def window_forward(Q, K, V, *, left: int, right: int = 0, sinks: int = 0, q_star
     _check(_on_device(Q.device, lambda st: lib().bsa_window_forward(desc, vq, vk, vv, vo, LSE.data_ptr(), st), stream),
            "bsa_window_forward")
     return O, LSE
+
+
+def window_backward(Q, K, V, O, LSE, dO, *, left: int, right: int = 0, sinks: int = 0, q_start=None, kv_len=None,
+                    scale: float = 0.0, layout: str = "hnd", dQ=None, dK=None, dV=None, stream=None):
+    """``bsa_window_backward``: ``(dQ, dK, dV)`` of ``window_forward`` from its inputs, its outputs and the gradient ``dO`` of
+    ``O``; arguments as there.  dK and dV are summed over the query heads that share a key head.  The workspace comes from
+    torch's allocator on the current stream; with ``stream`` given, that one has to be the tensors' as torch knows it."""
+    import torch
+    desc, vq, vk, vv, shape = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, layout)
+    nhd = LAYOUTS[layout] == 1
+    if O.shape != Q.shape or dO.shape != Q.shape:
+        raise ValueError("O and dO have to have the shape of Q")
+    if tuple(LSE.shape) != shape or LSE.dtype is not torch.float32 or LSE.device != Q.device or not LSE.is_contiguous():
+        raise ValueError(f"LSE has to be a contiguous fp32 tensor {shape} on the device of Q")
+    dQ = torch.empty_like(Q) if dQ is None else dQ
+    dK = torch.empty_like(K) if dK is None else dK
+    dV = torch.empty_like(V) if dV is None else dV
+    if dQ.shape != Q.shape or dK.shape != K.shape or dV.shape != K.shape:
+        raise ValueError("gradients have to have the shapes of their tensors")
+    views = [_view(t, nhd, Q, n)[4] for t, n in ((O, "O"), (dO, "dO"), (dQ, "dQ"), (dK, "dK"), (dV, "dV"))]
+
+    def call(st):
+        n = lib().bsa_window_workspace_bytes(desc)
+        ws = torch.empty(n, dtype=torch.uint8, device=Q.device)
+        return lib().bsa_window_backward(desc, vq, vk, vv, views[0], LSE.data_ptr(), *views[1:], ws.data_ptr(), n, st)
+    _check(_on_device(Q.device, call, stream), "bsa_window_backward")
+    return dQ, dK, dV
 
 
 def window_status() -> int:

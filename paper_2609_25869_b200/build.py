@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbsa.so")
 SOURCES = ["bsa_api.cu", "bsa_planner.cu", "bsa_attention.cu", "bsa_attention_rb.cu", "bsa_noalloc.cu",
-           "bsa_rope.cu", "bsa_window.cu", "bsa_window_rows.cu", "bsa_lut.cpp"]
+           "bsa_rope.cu", "bsa_window.cu", "bsa_window_rows.cu", "bsa_window_bwd.cu",
+           "bsa_lut.cpp"]
 
 
 def _stale() -> bool:

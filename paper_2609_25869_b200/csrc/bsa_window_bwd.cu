@@ -3,7 +3,7 @@
 //   P = exp(S - LSE),  D_i = sum dO * O,  dV = P^T dO,  dS = P * (dO V^T - D),  dQ = scale dS K,  dK = scale dS^T Q
 //
 // Three kernels:
-//   rows   : D of every row, and LSE in the exp2 domain (+inf for rows that see nothing: their P is zero)
+//   delta  : D of every row, and LSE in the exp2 domain
 //   dQ     : a CTA owns 128 query rows and walks over the key tiles that they see      (S, dO V^T, dS K: three products a tile)
 //   dK, dV : a CTA owns 128 keys and walks over the query tiles, of every head that shares the keys, that see them, with the
 //            scores transposed so that P^T and dS^T, where they are computed, are the products' left operands in tensor memory
@@ -12,8 +12,7 @@
 // in global memory, in an order that changes from run to run, or keep partial sums of one of them per tile of the other.  Here
 // every gradient is summed in tensor memory by one CTA.  Only the keys of the first tokens, seen by every query, are cut into
 // several shares of their queries, whose sums are added up in a fixed order by a fourth kernel.
-// In both kernels eight softmax warps share a tile by columns (thread = row of the tile, 64 columns each), one warp copies, one
-// issues the products.
+// In both kernels eight softmax warps (thread = row of a tile), one warp that copies and one that issues the products.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -36,8 +35,8 @@ struct BwdParams {
     WindowGeom g;
     float scale, scale_log2;
     int n_pad;             // N rounded up to whole tiles
-    const float* lse2;     // [batch * heads][n_pad]
-    const float* delta;
+    const float* neg_lse2;   // [batch * heads][n_pad]: -LSE in the exp2 domain (-inf for rows that see nothing: their P is zero)
+    const float* neg_delta;  // -D
     uint16_t* dQ;
     uint16_t* dK;
     uint16_t* dV;
@@ -50,12 +49,12 @@ struct BwdParams {
 };
 
 struct __align__(8) DqBarriers {
-    uint64_t q_full, k_full[4], k_empty[4], v_full[2], v_empty[2];
-    uint64_t s_full[2], s_free[2], dp_full, ds_ready, acc_full;
+    uint64_t q_full, k_full[3], k_empty[3], v_full[2], v_empty[2];
+    uint64_t s_full[2], s_free, dp_full[2], ds_ready[2], acc_full;  // (one s_full for each of its readers)
 };
 struct __align__(8) DkvBarriers {
     uint64_t kv_full, q_full[4], q_empty[4], o_full[4], o_empty[4];
-    uint64_t s_full, dp_full, p_ready, ds_ready, acc_full;
+    uint64_t s_full, dp_full, p_ready[2], ds_ready, acc_full;
 };
 
 __device__ __forceinline__ void let_copies_land() {
@@ -113,12 +112,12 @@ __device__ __forceinline__ void store_row(uint32_t t_acc, float f, bool zero, ui
     }
 }
 
-// ------------------------------------------------------------------------------------------ rows
+// ------------------------------------------------------------------------------------------ delta
 // Eight lanes a row.  Bound by memory: O and dO are read once.
 template <int D, bool F16>
 __global__ void __launch_bounds__(256) window_delta_kernel(const WindowGeom g, const uint16_t* O, const uint16_t* dO, long long o_batch,
                                                           long long o_head, long long o_row, long long d_batch, long long d_head,
-                                                          long long d_row, const float* LSE, float* lse2, float* delta, int n_pad) {
+                                                          long long d_row, const float* LSE, float* neg_lse2, float* neg_delta, int n_pad) {
     const int bh = blockIdx.y, b = bh / g.heads, h = bh - b * g.heads;
     const int row = blockIdx.x * 32 + (threadIdx.x >> 3), l8 = threadIdx.x & 7;
     const Sequence seq = load_sequence(g, b);
@@ -148,8 +147,8 @@ __global__ void __launch_bounds__(256) window_delta_kernel(const WindowGeom g, c
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     sum += __shfl_xor_sync(0xffffffffu, sum, 4);
     if (l8 == 0 && row < n_pad) {
-        delta[(long long)bh * n_pad + row] = sum;
-        lse2[(long long)bh * n_pad + row] = seen ? LSE[(long long)bh * g.N + row] * 1.4426950408889634f : INFINITY;
+        neg_delta[(long long)bh * n_pad + row] = -sum;
+        neg_lse2[(long long)bh * n_pad + row] = seen ? LSE[(long long)bh * g.N + row] * -1.4426950408889634f : -INFINITY;
     }
 }
 
@@ -159,7 +158,7 @@ struct DqCfg {
     static constexpr int kTile = kWinT * D * 2;
     static constexpr int kK = 3, kV = 2;
     static constexpr int kSmem = (2 + kK + kV) * kTile;  // Q, dO, rings of K and V
-    static constexpr uint32_t kS0 = 0, kS1 = 128, kDP = 256, kDQ = 384;
+    static constexpr uint32_t kS = 0, kDP0 = 128, kDP1 = 256, kDQ = 384;
 };
 
 template <int D, bool F16>
@@ -212,10 +211,10 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             mbar_init(smem_u32(&bars.v_full[i]), 1);
             mbar_init(smem_u32(&bars.v_empty[i]), 1);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
-            mbar_init(smem_u32(&bars.s_free[i]), 256);
+            mbar_init(smem_u32(&bars.dp_full[i]), 1);
+            mbar_init(smem_u32(&bars.ds_ready[i]), 128);
         }
-        mbar_init(smem_u32(&bars.dp_full), 1);
-        mbar_init(smem_u32(&bars.ds_ready), 256);
+        mbar_init(smem_u32(&bars.s_free), 128);
         mbar_init(smem_u32(&bars.acc_full), 1);
         fence_mbar_init();
     }
@@ -252,7 +251,8 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             if (!ok) let_copies_land();
         }
     } else if (warp == 9) {
-        // Order: S(0), dP(0), S(1); then for every tile i: dQ(i) behind its dS, dP(i + 1) in the place of that dS, S(i + 2).
+        // Tile i belongs to softmax warpgroup i mod 2 and has dP buffer i mod 2, where its dS goes as well; S has one buffer, free
+        // as soon as it has been read.  Order: S(0), dP(0), S(1), dP(1); then for every tile i: S(i + 2), dQ(i) behind its dS, dP(i + 2).
         constexpr uint32_t idesc_s = make_idesc_f32(kWinT, kWinT, 0, 0, F16), idesc_dq = make_idesc_f32(kWinT, D, 0, 1, F16);
         const uint64_t descQ = make_smem_desc_sw128(smem_u32(sQ), 16, 1024), descG = make_smem_desc_sw128(smem_u32(sG), 16, 1024);
         const uint64_t descK = make_smem_desc_sw128(smem_u32(sK), 16, 1024), descV = make_smem_desc_sw128(smem_u32(sV), 16, 1024);
@@ -268,98 +268,106 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             }
         };
         auto issue_s = [&](int j) -> bool {
-            if (j >= 2 && !mbar_wait_warp(smem_u32(&bars.s_free[j & 1]), ((j >> 1) - 1) & 1, abortp)) return false;
+            if (j >= 1 && !mbar_wait_warp(smem_u32(&bars.s_free), (j - 1) & 1, abortp)) return false;
             if (!mbar_wait_warp(smem_u32(&bars.k_full[rs.stage]), rs.phase, abortp)) return false;
             tc_fence_after();
             if (leader) {
-                product(tmem + ((j & 1) ? C::kS1 : C::kS0), descQ, descK + (uint64_t)((rs.stage * C::kTile) >> 4));
+                product(tmem + C::kS, descQ, descK + (uint64_t)((rs.stage * C::kTile) >> 4));
                 mma_commit(smem_u32(&bars.s_full[j & 1]));
             }
             rs.advance<C::kK>();
             return true;
         };
-        auto issue_dp = [&]() -> bool {
+        auto issue_dp = [&](int j) -> bool {
             if (!mbar_wait_warp(smem_u32(&bars.v_full[rv.stage]), rv.phase, abortp)) return false;
             tc_fence_after();
             if (leader) {
-                product(tmem + C::kDP, descG, descV + (uint64_t)((rv.stage * C::kTile) >> 4));
-                mma_commit(smem_u32(&bars.dp_full));
+                product(tmem + ((j & 1) ? C::kDP1 : C::kDP0), descG, descV + (uint64_t)((rv.stage * C::kTile) >> 4));
+                mma_commit(smem_u32(&bars.dp_full[j & 1]));
                 mma_commit(smem_u32(&bars.v_empty[rv.stage]));
             }
             rv.advance<C::kV>();
             return true;
         };
-        ok = ok && issue_s(0) && issue_dp();
-        if (ok && n > 1) ok = issue_s(1);
+        ok = ok && issue_s(0) && issue_dp(0);
+        if (ok && n > 1) ok = issue_s(1) && issue_dp(1);
         for (int i = 0; ok && i < n; ++i) {
-            ok = mbar_wait_warp(smem_u32(&bars.ds_ready), i & 1, abortp);
+            if (i + 2 < n) ok = issue_s(i + 2);
+            ok = ok && mbar_wait_warp(smem_u32(&bars.ds_ready[i & 1]), (i >> 1) & 1, abortp);
             if (!ok) break;
             tc_fence_after();
             if (leader) {
                 const uint64_t k0 = descKt + (uint64_t)((rq.stage * C::kTile) >> 4);
+                const uint32_t a_ds = tmem + ((i & 1) ? C::kDP1 : C::kDP0);
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
-                    mma_ts(tmem + C::kDQ, tmem + C::kDP + (kk < 4 ? kk * 8 : 64 + (kk - 4) * 8), k0 + (uint64_t)(kk * 128), idesc_dq,
-                           (i > 0 || kk > 0) ? 1u : 0u);
+                    mma_ts(tmem + C::kDQ, a_ds + kk * 8, k0 + (uint64_t)(kk * 128), idesc_dq, (i > 0 || kk > 0) ? 1u : 0u);
                 mma_commit(smem_u32(&bars.k_empty[rq.stage]));
                 if (i == n - 1) mma_commit(smem_u32(&bars.acc_full));
             }
             rq.advance<C::kK>();
-            if (i + 1 < n) ok = issue_dp();
-            if (ok && i + 2 < n) ok = issue_s(i + 2);
+            if (i + 2 < n) ok = issue_dp(i + 2);
         }
     } else {
         const int x = warp >> 2, tw = tid & 127;
-        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_dp = t_lane + C::kDP + x * 64;
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_dp = t_lane + (x ? C::kDP1 : C::kDP0);
         const int row = row0 + tw, pos = seq.start + row;
-        const float c2 = p.scale_log2;
-        const float neg_lse = -__ldg(p.lse2 + (long long)bh * p.n_pad + row), del = __ldg(p.delta + (long long)bh * p.n_pad + row);
+        const float neg_lse = __ldg(p.neg_lse2 + (long long)bh * p.n_pad + row), neg_del = __ldg(p.neg_delta + (long long)bh * p.n_pad + row);
+        const uint64_t c22 = pack_f32x2(p.scale_log2, p.scale_log2), nl2 = pack_f32x2(neg_lse, neg_lse), nd2 = pack_f32x2(neg_del, neg_del);
         bool ok = true;
-        for (int i = 0; i < n; ++i) {
+        for (int i = x; i < n; i += 2) {
             const int key0 = tiles.tile(i) * kWinT;
             const bool full = tile_is_full(p.g, range, key0);
-            ok = mbar_wait_warp(smem_u32(&bars.s_full[i & 1]), (i >> 1) & 1, abortp);
+            ok = mbar_wait_warp(smem_u32(&bars.s_full[x]), (i >> 1) & 1, abortp);
             if (!ok) break;
             tc_fence_after();
-            uint32_t r[64];
-            tmem_ld32(t_lane + ((i & 1) ? C::kS1 : C::kS0) + x * 64, r);
-            tmem_ld32(t_lane + ((i & 1) ? C::kS1 : C::kS0) + x * 64 + 32, r + 32);
+            uint32_t r[kWinT];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(t_lane + C::kS + c * 32, r + c * 32);
             tc_wait_ld();
             tc_fence_before();
-            mbar_arrive(smem_u32(&bars.s_free[i & 1]));
+            mbar_arrive(smem_u32(&bars.s_free));
 #pragma unroll
-            for (int c = 0; c < 64; ++c) r[c] = __float_as_uint(ex2_approx(fmaf(__uint_as_float(r[c]), c2, neg_lse)));
-            uint32_t bits[2] = {0xffffffffu, 0xffffffffu};
+            for (int c = 0; c < kWinT; c += 2) {
+                float a, e;
+                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), c22, nl2), a, e);
+                r[c] = __float_as_uint(ex2_approx(a));
+                r[c + 1] = __float_as_uint(ex2_approx(e));
+            }
             if (!full) {
-                bits[0] = row_bits(p.g, seq, pos, key0 + x * 64);
-                bits[1] = row_bits(p.g, seq, pos, key0 + x * 64 + 32);
                 // K rows that no row here sees may hold anything: their dS is zero, which times NaN would not be
                 const int key = key0 + tw;
-                if (x == 0 && (key >= range.hi || (key < range.lo && key >= p.g.sinks))) zero_row<D>(sK + (i % C::kK) * C::kTile, tw);
+                if (key >= range.hi || (key < range.lo && key >= p.g.sinks)) zero_row<D>(sK + (i % C::kK) * C::kTile, tw);
                 fence_proxy_async_smem();
             }
-            ok = mbar_wait_warp(smem_u32(&bars.dp_full), i & 1, abortp);
+            ok = mbar_wait_warp(smem_u32(&bars.dp_full[x]), (i >> 1) & 1, abortp);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < 4; ++c) {
                 uint32_t d[32];
                 tmem_ld32(t_dp + c * 32, d);
                 tc_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) d[e] = __float_as_uint((__uint_as_float(d[e]) - del) * __uint_as_float(r[c * 32 + e]));
+                for (int e = 0; e < 32; e += 2) {
+                    float u, v;
+                    unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), nd2),
+                                           pack_f32x2(__uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]))), u, v);
+                    d[e] = __float_as_uint(u);
+                    d[e + 1] = __float_as_uint(v);
+                }
                 if (!full) {
+                    const uint32_t bits = row_bits(p.g, seq, pos, key0 + c * 32);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) d[e] = (bits[c] & (1u << e)) ? d[e] : 0u;
+                    for (int e = 0; e < 32; ++e) d[e] = (bits & (1u << e)) ? d[e] : 0u;
                 }
 #pragma unroll
-                for (int e = 0; e < 16; ++e) r[c * 32 + e] = pack_16x2<F16>(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+                for (int e = 0; e < 16; ++e) d[e] = pack_16x2<F16>(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+                tmem_st16(t_dp + c * 16, d);  // over columns that have been read
             }
-            tmem_st16(t_dp, r);
-            tmem_st16(t_dp + 16, r + 32);
             tc_wait_st();
             tc_fence_before();
-            mbar_arrive(smem_u32(&bars.ds_ready));
+            mbar_arrive(smem_u32(&bars.ds_ready[x]));
         }
         if (ok && mbar_wait_warp(smem_u32(&bars.acc_full), 0, abortp)) {
             tc_fence_after();
@@ -466,7 +474,8 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         mbar_init(smem_u32(&bars.s_full), 1);
         mbar_init(smem_u32(&bars.dp_full), 1);
-        mbar_init(smem_u32(&bars.p_ready), 256);
+        mbar_init(smem_u32(&bars.p_ready[0]), 256);
+        mbar_init(smem_u32(&bars.p_ready[1]), 256);
         mbar_init(smem_u32(&bars.ds_ready), 256);
         mbar_init(smem_u32(&bars.acc_full), 1);
         fence_mbar_init();
@@ -498,8 +507,8 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const long long at = ((long long)b * p.g.heads + h) * p.n_pad + row;
                 mbar_arrive_expect_tx(bar, C::kTile + C::kRows);
                 tma_load_rows(smem_u32(sQ) + ring.stage * C::kTile, &tmQ, bar, row, h, b);
-                bulk_load(rows, p.lse2 + at, kWinT * 4, bar);
-                bulk_load(rows + kWinT * 4, p.delta + at, kWinT * 4, bar);
+                bulk_load(rows, p.neg_lse2 + at, kWinT * 4, bar);
+                bulk_load(rows + kWinT * 4, p.neg_delta + at, kWinT * 4, bar);
                 ok = mbar_wait(smem_u32(&bars.o_empty[ring.stage]), ring.phase ^ 1, abortp);
                 if (!ok) break;
                 mbar_arrive_expect_tx(smem_u32(&bars.o_full[ring.stage]), C::kTile);
@@ -545,13 +554,23 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         next.advance<C::kQ>();
         for (int i = 0; ok && i < n; ++i) {
-            ok = mbar_wait_warp(smem_u32(&bars.p_ready), i & 1, abortp);
-            if (!ok) break;
-            tc_fence_after();
-            if (leader) {
-                gradient(tmem + C::kDV, tmem + C::kS, descGt + (uint64_t)((cur.stage * C::kTile) >> 4), i == 0);
-                mma_commit(smem_u32(&bars.o_empty[cur.stage]));
+            const uint64_t g0 = descGt + (uint64_t)((cur.stage * C::kTile) >> 4);
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                ok = ok && mbar_wait_warp(smem_u32(&bars.p_ready[part]), i & 1, abortp);
+                if (!ok) break;
+                tc_fence_after();
+                if (leader) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int kk = (e >> 1) * 4 + part * 2 + (e & 1);  // 16 query rows, of either warpgroup's 64
+                        mma_ts(tmem + C::kDV, tmem + C::kS + (kk < 4 ? kk * 8 : 64 + (kk - 4) * 8), g0 + (uint64_t)(kk * 128), idesc_g,
+                               (i > 0 || part > 0 || e > 0) ? 1u : 0u);
+                    }
+                }
             }
+            if (!ok) break;
+            if (leader) mma_commit(smem_u32(&bars.o_empty[cur.stage]));
             if (i + 1 < n) {
                 ok = mbar_wait_warp(smem_u32(&bars.q_full[next.stage]), next.phase, abortp);
                 if (!ok) break;
@@ -594,7 +613,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             const bool full = rows_ok && key0 + kWinT <= seq.len && key0 + kWinT - 1 <= pos0 + p.g.right &&
                               (pos0 + kWinT - 1 <= key0 + p.g.left || key0 + kWinT <= p.g.sinks);
             const float4* lse = reinterpret_cast<const float4*>(sR + ring.stage * C::kRows) + x * 16;
-            const float4* del = lse + kWinT / 4;
+            const float4* del = lse + kWinT / 4;  // (both negated)
             ok = mbar_wait_warp(smem_u32(&bars.q_full[ring.stage]), ring.phase, abortp) && mbar_wait_warp(smem_u32(&bars.s_full), i & 1, abortp);
             if (!ok) break;
             tc_fence_after();
@@ -602,20 +621,11 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             tmem_ld32(t_s, r);
             tmem_ld32(t_s + 32, r + 32);
             tc_wait_ld();
-#pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 l = lse[c / 4];
-                r[c] = __float_as_uint(ex2_approx(fmaf(__uint_as_float(r[c]), c2, -l.x)));
-                r[c + 1] = __float_as_uint(ex2_approx(fmaf(__uint_as_float(r[c + 1]), c2, -l.y)));
-                r[c + 2] = __float_as_uint(ex2_approx(fmaf(__uint_as_float(r[c + 2]), c2, -l.z)));
-                r[c + 3] = __float_as_uint(ex2_approx(fmaf(__uint_as_float(r[c + 3]), c2, -l.w)));
-            }
+            const uint64_t c22 = pack_f32x2(c2, c2);
             uint32_t bits[2] = {0xffffffffu, 0xffffffffu};
             if (!full) {
                 bits[0] = key_bits(p.g, seq, key, row0 + x * 64);
                 bits[1] = key_bits(p.g, seq, key, row0 + x * 64 + 32);
-#pragma unroll
-                for (int c = 0; c < 64; ++c) r[c] = (bits[c >> 5] & (1u << (c & 31))) ? r[c] : 0u;
                 if (!rows_ok) {  // rows at no position may hold anything: their weight is zero, which times NaN would not be
                     ok = mbar_wait_warp(smem_u32(&bars.o_full[ring.stage]), ring.phase, abortp);
                     if (!ok) break;
@@ -623,15 +633,32 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     fence_proxy_async_smem();
                 }
             }
-            {
-                uint32_t q[32];
+            // P goes out in two parts of 32 columns: the first part's products run beside the second's exponentials
 #pragma unroll
-                for (int e = 0; e < 32; ++e) q[e] = pack_16x2<F16>(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
-                tmem_st32(t_s, q);
+            for (int part = 0; part < 2; ++part) {
+#pragma unroll
+                for (int c = part * 32; c < part * 32 + 32; c += 4) {
+                    const float4 l = lse[c / 4];
+                    float a0, a1, a2, a3;
+                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), c22, pack_f32x2(l.x, l.y)), a0, a1);
+                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c + 2]), __uint_as_float(r[c + 3])), c22, pack_f32x2(l.z, l.w)), a2, a3);
+                    r[c] = __float_as_uint(ex2_approx(a0));
+                    r[c + 1] = __float_as_uint(ex2_approx(a1));
+                    r[c + 2] = __float_as_uint(ex2_approx(a2));
+                    r[c + 3] = __float_as_uint(ex2_approx(a3));
+                }
+                if (!full) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) r[part * 32 + c] = (bits[part] & (1u << c)) ? r[part * 32 + c] : 0u;
+                }
+                uint32_t q[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) q[e] = pack_16x2<F16>(__uint_as_float(r[part * 32 + 2 * e]), __uint_as_float(r[part * 32 + 2 * e + 1]));
+                tmem_st16(t_s + part * 16, q);
+                tc_wait_st();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&bars.p_ready[part]));
             }
-            tc_wait_st();
-            tc_fence_before();
-            mbar_arrive(smem_u32(&bars.p_ready));
             ok = mbar_wait_warp(smem_u32(&bars.dp_full), i & 1, abortp);
             if (!ok) break;
             tc_fence_after();
@@ -643,10 +670,15 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
                     const float4 l = del[c * 8 + e / 4];
-                    d[e] = __float_as_uint((__uint_as_float(d[e]) - l.x) * __uint_as_float(r[c * 32 + e]));
-                    d[e + 1] = __float_as_uint((__uint_as_float(d[e + 1]) - l.y) * __uint_as_float(r[c * 32 + e + 1]));
-                    d[e + 2] = __float_as_uint((__uint_as_float(d[e + 2]) - l.z) * __uint_as_float(r[c * 32 + e + 2]));
-                    d[e + 3] = __float_as_uint((__uint_as_float(d[e + 3]) - l.w) * __uint_as_float(r[c * 32 + e + 3]));
+                    float a0, a1, a2, a3;
+                    unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pack_f32x2(l.x, l.y)),
+                                           pack_f32x2(__uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]))), a0, a1);
+                    unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])), pack_f32x2(l.z, l.w)),
+                                           pack_f32x2(__uint_as_float(r[c * 32 + e + 2]), __uint_as_float(r[c * 32 + e + 3]))), a2, a3);
+                    d[e] = __float_as_uint(a0);
+                    d[e + 1] = __float_as_uint(a1);
+                    d[e + 2] = __float_as_uint(a2);
+                    d[e + 3] = __float_as_uint(a3);
                 }
                 if (!full) {
 #pragma unroll
@@ -812,8 +844,8 @@ extern "C" bsa_status_t bsa_window_backward(const bsa_window_desc_t* t, const bs
     float* lse2 = reinterpret_cast<float*>(ws + l.lse2);
     float* delta = reinterpret_cast<float*>(ws + l.delta);
     p.n_pad = l.n_pad;
-    p.lse2 = lse2;
-    p.delta = delta;
+    p.neg_lse2 = lse2;
+    p.neg_delta = delta;
     p.partial = reinterpret_cast<float*>(ws + l.partial);
     p.dQ = static_cast<uint16_t*>(dQ->data);
     p.dK = static_cast<uint16_t*>(dK->data);

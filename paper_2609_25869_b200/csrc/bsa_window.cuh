@@ -94,6 +94,21 @@ __device__ __forceinline__ void hide(uint32_t* r, uint32_t bits) {
     for (int i = 0; i < 32; ++i) r[i] = (bits & (1u << i)) ? r[i] : 0xff800000u;
 }
 
+// Division of non-negative ints by a constant of the call: the items of a persistent CTA are decoded on its critical path.
+struct Divisor {
+    uint32_t d, mul, shift;
+    Divisor() = default;
+    explicit Divisor(int n) : d((uint32_t)n), mul(0), shift(0) {
+        while ((1ull << shift) < d) ++shift;  // n / d = (n + n * mul / 2^32) / 2^shift
+        mul = (uint32_t)((((1ull << shift) - d) << 32) / d + 1);
+    }
+    __device__ __forceinline__ int div(int n, int& rest) const {
+        const uint32_t q = (__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift;
+        rest = n - (int)(q * d);
+        return (int)q;
+    }
+};
+
 // ---- host side (bsa_window.cu) ----
 struct WindowArgs {
     WindowGeom g;

@@ -41,20 +41,24 @@ struct BwdParams {
     uint16_t* dK;
     uint16_t* dV;
     long long q_batch, q_head, q_row, k_batch, k_head, k_row, v_batch, v_head, v_row;  // strides of the gradients
-    int n_qt, n_kt;        // tiles of a sequence
+    int n_dq, n_dkv;       // items of the two kernels
     int longest_first;
-    int sink_tiles, sink_shares;  // key tiles in front that are cut into shares (0: none)
+    Divisor qt, heads, bh, heads_kv, group;  // query tiles of a sequence, heads, batch x heads, key heads, heads that share a key head
+    Divisor kt, bhk, shares, shared;        // key tiles of a sequence that are not cut into shares, batch x key heads, shares of a tile and of a
+                                            // sequence's tiles
+    int sink_tiles, sink_shares;            // key tiles in front that are cut into shares (0: none)
+    int wide_q, wide_k, wide_v;             // gradients whose rows lie on 32-byte boundaries
     float* partial;        // [batch * heads_kv][sink_tiles][sink_shares][dV, dK][128][D]
     int* status;
 };
 
 struct __align__(8) DqBarriers {
-    uint64_t q_full, k_full[3], k_empty[3], v_full[2], v_empty[2];
-    uint64_t s_full[2], s_free, dp_full[2], ds_ready[2], acc_full;  // (one s_full for each of its readers)
+    uint64_t q_full, q_empty, k_full[4], k_empty[4], v_full, v_empty;
+    uint64_t s_full[2], s_free, dp_full[2], ds_ready[2], acc_full, acc_free;  // (one s_full for each of its readers)
 };
 struct __align__(8) DkvBarriers {
-    uint64_t kv_full, q_full[4], q_empty[4], o_full[4], o_empty[4];
-    uint64_t s_full, dp_full, p_ready[2], ds_ready, acc_full;
+    uint64_t kv_full, kv_empty, q_full[2], q_empty[2], o_full[2], o_empty[2];
+    uint64_t s_full, dp_full, p_ready[2], ds_ready, acc_full, acc_free;
 };
 
 __device__ __forceinline__ void let_copies_land() {
@@ -78,9 +82,10 @@ struct Ring {
         }
     }
 };
-template <int R>
-__device__ __forceinline__ void reg_inc() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R));
+// The k-th item of a persistent CTA, dealt in alternating directions (the longest items come first).
+__device__ __forceinline__ int item_index(int k) {
+    const int G = gridDim.x;
+    return k * G + ((k & 1) ? (G - 1 - (int)blockIdx.x) : (int)blockIdx.x);
 }
 
 // Row `row` of a tile in shared memory becomes zero (its 64-column sub-tiles, whatever the swizzle).
@@ -92,23 +97,25 @@ __device__ __forceinline__ void zero_row(uint8_t* tile, int row) {
         for (int c = 0; c < 8; ++c) reinterpret_cast<uint4*>(tile + s * SUB + row * 128)[c] = make_uint4(0, 0, 0, 0);
 }
 
-// A row of an accumulator, times `f`, to global memory in the element type.
-template <int D, bool F16>
-__device__ __forceinline__ void store_row(uint32_t t_acc, float f, bool zero, uint16_t* out) {
+// Columns [c0 * 32, c1 * 32) of a row of an accumulator, times `f`, to global memory in the element type; out null: nowhere.
+template <bool F16>
+__device__ __forceinline__ void store_row(uint32_t t_acc, int c0, int c1, float f, bool zero, uint16_t* out, int wide) {
 #pragma unroll 1
-    for (int c = 0; c < D / 32; ++c) {
+    for (int c = c0; c < c1; ++c) {
         uint32_t o[32];
         tmem_ld32(t_acc + c * 32, o);
         tc_wait_ld();
-        if (!out) continue;
+        if (out) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            uint32_t v[4];
+            for (int q = 0; q < 2; ++q) {
+                uint32_t v[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = zero ? 0u : pack_16x2<F16>(__uint_as_float(o[q * 8 + 2 * e]) * f, __uint_as_float(o[q * 8 + 2 * e + 1]) * f);
-            *reinterpret_cast<uint4*>(out + c * 32 + q * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+                for (int e = 0; e < 8; ++e)
+                    v[e] = zero ? 0u : pack_16x2<F16>(__uint_as_float(o[q * 16 + 2 * e]) * f, __uint_as_float(o[q * 16 + 2 * e + 1]) * f);
+                st_global_v8_or_2v4(out + c * 32 + q * 16, v, wide);
+            }
         }
+        __syncwarp();
     }
 }
 
@@ -156,10 +163,34 @@ __global__ void __launch_bounds__(256) window_delta_kernel(const WindowGeom g, c
 template <int D>
 struct DqCfg {
     static constexpr int kTile = kWinT * D * 2;
-    static constexpr int kK = 3, kV = 2;
-    static constexpr int kSmem = (2 + kK + kV) * kTile;  // Q, dO, rings of K and V
+    static constexpr int kK = 4;                       // K tiles in the ring (a tile lives from its S to its dQ, two tiles later); V has one
+    static constexpr int kSmem = (2 + kK + 1) * kTile;  // Q, dO, K, V
     static constexpr uint32_t kS = 0, kDP0 = 128, kDP1 = 256, kDQ = 384;
 };
+
+struct DqItem {
+    int b, h, hk, row0;
+    Sequence seq;
+    KeyRange range;
+    TileSpan tiles;
+};
+__device__ __forceinline__ bool load_item(const BwdParams& p, int k, DqItem& it) {
+    const int idx = item_index(k);
+    if (idx >= p.n_dq) return false;
+    int bh, qt;
+    if (p.longest_first)
+        qt = (int)p.qt.d - 1 - p.bh.div(idx, bh);
+    else
+        bh = p.qt.div(idx, qt);
+    it.b = p.heads.div(bh, it.h);
+    int rest;
+    it.hk = p.group.div(it.h, rest);
+    it.row0 = qt * kWinT;
+    it.seq = load_sequence(p.g, it.b);
+    it.range = key_range(p.g, it.seq, it.row0, it.row0 + kWinT);
+    it.tiles = tile_span(it.range);
+    return true;
+}
 
 template <int D, bool F16>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -178,44 +209,24 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         if (tid == 0) atomicExch(p.status, (int)BSA_ERR_CUDA);
         return;
     }
-    int bh, qt;
-    if (p.longest_first) {
-        const int n_bh = p.g.batch * p.g.heads;
-        qt = p.n_qt - 1 - (int)blockIdx.x / n_bh;
-        bh = (int)blockIdx.x % n_bh;
-    } else {
-        bh = (int)blockIdx.x / p.n_qt;
-        qt = (int)blockIdx.x % p.n_qt;
-    }
-    const int b = bh / p.g.heads, h = bh - b * p.g.heads, hk = h / p.g.group, row0 = qt * kWinT;
-    const Sequence seq = load_sequence(p.g, b);
-    const KeyRange range = key_range(p.g, seq, row0, row0 + kWinT);
-    const TileSpan tiles = tile_span(range);
-    const int n = tiles.count();
-    if (n == 0) {  // nothing is seen: zero gradient
-        const int row = row0 + tid;
-        if (tid < kWinT && row < p.g.N) {
-            uint4* o = reinterpret_cast<uint4*>(p.dQ + (long long)b * p.q_batch + (long long)h * p.q_head + (long long)row * p.q_row);
-            for (int c = 0; c < D / 8; ++c) o[c] = make_uint4(0, 0, 0, 0);
-        }
-        return;
-    }
     if (tid == 0) {
         abort_flag = 0;
         mbar_init(smem_u32(&bars.q_full), 1);
+        mbar_init(smem_u32(&bars.q_empty), 1);
+        mbar_init(smem_u32(&bars.v_full), 1);
+        mbar_init(smem_u32(&bars.v_empty), 1);
         for (int i = 0; i < C::kK; ++i) {
             mbar_init(smem_u32(&bars.k_full[i]), 1);
             mbar_init(smem_u32(&bars.k_empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&bars.v_full[i]), 1);
-            mbar_init(smem_u32(&bars.v_empty[i]), 1);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
             mbar_init(smem_u32(&bars.dp_full[i]), 1);
             mbar_init(smem_u32(&bars.ds_ready[i]), 128);
         }
         mbar_init(smem_u32(&bars.s_free), 128);
         mbar_init(smem_u32(&bars.acc_full), 1);
+        mbar_init(smem_u32(&bars.acc_free), 256);
         fence_mbar_init();
     }
     if (warp == 9) {
@@ -227,39 +238,53 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
     volatile uint32_t* abortp = &abort_flag;
+    DqItem it;
 
     if (warp == 8) {
         if (lane == 0) {
-            Ring rk, rv;
-            mbar_arrive_expect_tx(smem_u32(&bars.q_full), 2 * C::kTile);
-            tma_load_rows(smem_u32(sQ), &tmQ, smem_u32(&bars.q_full), row0, h, b);
-            tma_load_rows(smem_u32(sG), &tmG, smem_u32(&bars.q_full), row0, h, b);
+            Ring rk;
+            uint32_t n_q = 0, n_v = 0;
             bool ok = true;
-            for (int j = 0; j < n; ++j) {
-                const int key0 = tiles.tile(j) * kWinT;
-                ok = mbar_wait(smem_u32(&bars.k_empty[rk.stage]), rk.phase ^ 1, abortp);
+            for (int k = 0; ok && load_item(p, k, it); ++k) {
+                const int n = it.tiles.count();
+                if (n == 0) continue;
+                auto copy_k = [&](int j) -> bool {
+                    if (!mbar_wait(smem_u32(&bars.k_empty[rk.stage]), rk.phase ^ 1, abortp)) return false;
+                    mbar_arrive_expect_tx(smem_u32(&bars.k_full[rk.stage]), C::kTile);
+                    tma_load_rows(smem_u32(sK) + rk.stage * C::kTile, &tmK, smem_u32(&bars.k_full[rk.stage]), it.tiles.tile(j) * kWinT, it.hk, it.b);
+                    rk.advance<C::kK>();
+                    return true;
+                };
+                ok = mbar_wait(smem_u32(&bars.q_empty), (n_q & 1) ^ 1, abortp);
                 if (!ok) break;
-                mbar_arrive_expect_tx(smem_u32(&bars.k_full[rk.stage]), C::kTile);
-                tma_load_rows(smem_u32(sK) + rk.stage * C::kTile, &tmK, smem_u32(&bars.k_full[rk.stage]), key0, hk, b);
-                rk.advance<C::kK>();
-                ok = mbar_wait(smem_u32(&bars.v_empty[rv.stage]), rv.phase ^ 1, abortp);
-                if (!ok) break;
-                mbar_arrive_expect_tx(smem_u32(&bars.v_full[rv.stage]), C::kTile);
-                tma_load_rows(smem_u32(sV) + rv.stage * C::kTile, &tmV, smem_u32(&bars.v_full[rv.stage]), key0, hk, b);
-                rv.advance<C::kV>();
+                mbar_arrive_expect_tx(smem_u32(&bars.q_full), 2 * C::kTile);
+                tma_load_rows(smem_u32(sQ), &tmQ, smem_u32(&bars.q_full), it.row0, it.h, it.b);
+                tma_load_rows(smem_u32(sG), &tmG, smem_u32(&bars.q_full), it.row0, it.h, it.b);
+                ++n_q;
+                ok = copy_k(0);
+                for (int j = 0; ok && j < n; ++j) {  // K a tile ahead of V
+                    if (j + 1 < n) ok = copy_k(j + 1);
+                    ok = ok && mbar_wait(smem_u32(&bars.v_empty), (n_v & 1) ^ 1, abortp);
+                    if (!ok) break;
+                    mbar_arrive_expect_tx(smem_u32(&bars.v_full), C::kTile);
+                    tma_load_rows(smem_u32(sV), &tmV, smem_u32(&bars.v_full), it.tiles.tile(j) * kWinT, it.hk, it.b);
+                    ++n_v;
+                }
             }
             if (!ok) let_copies_land();
         }
     } else if (warp == 9) {
-        // Tile i belongs to softmax warpgroup i mod 2 and has dP buffer i mod 2, where its dS goes as well; S has one buffer, free
-        // as soon as it has been read.  Order: S(0), dP(0), S(1), dP(1); then for every tile i: S(i + 2), dQ(i) behind its dS, dP(i + 2).
+        // Tile t (counted over the CTA's items) belongs to softmax warpgroup t mod 2 and has dP buffer t mod 2, where its dS goes as
+        // well; S has one buffer, free as soon as it has been read.  Order within an item: S(0), dP(0), S(1), dP(1); then for every
+        // tile i: S(i + 2), dQ(i) behind its dS, dP(i + 2).
         constexpr uint32_t idesc_s = make_idesc_f32(kWinT, kWinT, 0, 0, F16), idesc_dq = make_idesc_f32(kWinT, D, 0, 1, F16);
         const uint64_t descQ = make_smem_desc_sw128(smem_u32(sQ), 16, 1024), descG = make_smem_desc_sw128(smem_u32(sG), 16, 1024);
         const uint64_t descK = make_smem_desc_sw128(smem_u32(sK), 16, 1024), descV = make_smem_desc_sw128(smem_u32(sV), 16, 1024);
         const uint64_t descKt = make_smem_desc_sw128(smem_u32(sK), SUB, 1024);
         const bool leader = elect_one();
-        Ring rs, rv, rq;  // K of the next S, V of the next dP, K of the next dQ
-        bool ok = mbar_wait_warp(smem_u32(&bars.q_full), 0, abortp);
+        Ring rs, rq;  // K of the next S and of the next dQ
+        uint32_t n_it = 0, n_v = 0, g = 0;
+        bool ok = true;
         auto product = [&](uint32_t d, uint64_t a, uint64_t b0) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
@@ -267,114 +292,144 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 mma_ss(d, a + off, b0 + off, idesc_s, kk > 0);
             }
         };
-        auto issue_s = [&](int j) -> bool {
-            if (j >= 1 && !mbar_wait_warp(smem_u32(&bars.s_free), (j - 1) & 1, abortp)) return false;
+        auto issue_s = [&](uint32_t t) -> bool {
+            if (t >= 1 && !mbar_wait_warp(smem_u32(&bars.s_free), (t - 1) & 1, abortp)) return false;
             if (!mbar_wait_warp(smem_u32(&bars.k_full[rs.stage]), rs.phase, abortp)) return false;
             tc_fence_after();
             if (leader) {
                 product(tmem + C::kS, descQ, descK + (uint64_t)((rs.stage * C::kTile) >> 4));
-                mma_commit(smem_u32(&bars.s_full[j & 1]));
+                mma_commit(smem_u32(&bars.s_full[t & 1]));
             }
             rs.advance<C::kK>();
             return true;
         };
-        auto issue_dp = [&](int j) -> bool {
-            if (!mbar_wait_warp(smem_u32(&bars.v_full[rv.stage]), rv.phase, abortp)) return false;
+        auto issue_dp = [&](uint32_t t, bool last) -> bool {
+            if (!mbar_wait_warp(smem_u32(&bars.v_full), n_v & 1, abortp)) return false;
+            ++n_v;
             tc_fence_after();
             if (leader) {
-                product(tmem + ((j & 1) ? C::kDP1 : C::kDP0), descG, descV + (uint64_t)((rv.stage * C::kTile) >> 4));
-                mma_commit(smem_u32(&bars.dp_full[j & 1]));
-                mma_commit(smem_u32(&bars.v_empty[rv.stage]));
+                product(tmem + ((t & 1) ? C::kDP1 : C::kDP0), descG, descV);
+                mma_commit(smem_u32(&bars.dp_full[t & 1]));
+                mma_commit(smem_u32(&bars.v_empty));
+                if (last) mma_commit(smem_u32(&bars.q_empty));  // (its S is in front of it)
             }
-            rv.advance<C::kV>();
             return true;
         };
-        ok = ok && issue_s(0) && issue_dp(0);
-        if (ok && n > 1) ok = issue_s(1) && issue_dp(1);
-        for (int i = 0; ok && i < n; ++i) {
-            if (i + 2 < n) ok = issue_s(i + 2);
-            ok = ok && mbar_wait_warp(smem_u32(&bars.ds_ready[i & 1]), (i >> 1) & 1, abortp);
-            if (!ok) break;
-            tc_fence_after();
-            if (leader) {
-                const uint64_t k0 = descKt + (uint64_t)((rq.stage * C::kTile) >> 4);
-                const uint32_t a_ds = tmem + ((i & 1) ? C::kDP1 : C::kDP0);
+        for (int k = 0; ok && load_item(p, k, it); ++k) {
+            const int n = it.tiles.count();
+            if (n == 0) continue;
+            ok = mbar_wait_warp(smem_u32(&bars.q_full), n_it & 1, abortp);
+            ok = ok && issue_s(g) && issue_dp(g, n == 1);
+            if (ok && n > 1) ok = issue_s(g + 1) && issue_dp(g + 1, n == 2);
+            for (int i = 0; ok && i < n; ++i) {
+                const uint32_t t = g + i;
+                if (i + 2 < n) ok = issue_s(t + 2);
+                if (ok && i == 0) ok = mbar_wait_warp(smem_u32(&bars.acc_free), (n_it & 1) ^ 1, abortp);  // the last item's gradient is out
+                ok = ok && mbar_wait_warp(smem_u32(&bars.ds_ready[t & 1]), (t >> 1) & 1, abortp);
+                if (!ok) break;
+                tc_fence_after();
+                if (leader) {
+                    const uint64_t k0 = descKt + (uint64_t)((rq.stage * C::kTile) >> 4);
+                    const uint32_t a_ds = tmem + ((t & 1) ? C::kDP1 : C::kDP0);
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    mma_ts(tmem + C::kDQ, a_ds + kk * 8, k0 + (uint64_t)(kk * 128), idesc_dq, (i > 0 || kk > 0) ? 1u : 0u);
-                mma_commit(smem_u32(&bars.k_empty[rq.stage]));
-                if (i == n - 1) mma_commit(smem_u32(&bars.acc_full));
+                    for (int kk = 0; kk < 8; ++kk)
+                        mma_ts(tmem + C::kDQ, a_ds + kk * 8, k0 + (uint64_t)(kk * 128), idesc_dq, (i > 0 || kk > 0) ? 1u : 0u);
+                    mma_commit(smem_u32(&bars.k_empty[rq.stage]));
+                    if (i == n - 1) mma_commit(smem_u32(&bars.acc_full));
+                }
+                rq.advance<C::kK>();
+                if (i + 2 < n) ok = issue_dp(t + 2, i + 3 == n);
             }
-            rq.advance<C::kK>();
-            if (i + 2 < n) ok = issue_dp(i + 2);
+            g += (uint32_t)n;
+            ++n_it;
         }
     } else {
         const int x = warp >> 2, tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_dp = t_lane + (x ? C::kDP1 : C::kDP0);
-        const int row = row0 + tw, pos = seq.start + row;
-        const float neg_lse = __ldg(p.neg_lse2 + (long long)bh * p.n_pad + row), neg_del = __ldg(p.neg_delta + (long long)bh * p.n_pad + row);
-        const uint64_t c22 = pack_f32x2(p.scale_log2, p.scale_log2), nl2 = pack_f32x2(neg_lse, neg_lse), nd2 = pack_f32x2(neg_del, neg_del);
-        bool ok = true;
-        for (int i = x; i < n; i += 2) {
-            const int key0 = tiles.tile(i) * kWinT;
-            const bool full = tile_is_full(p.g, range, key0);
-            ok = mbar_wait_warp(smem_u32(&bars.s_full[x]), (i >> 1) & 1, abortp);
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t r[kWinT];
+        const uint64_t c22 = pack_f32x2(p.scale_log2, p.scale_log2);
+        uint32_t g = 0, n_it = 0;
+        bool ok = true, more = load_item(p, 0, it);
+        auto row_value = [&](const float* v) { return __ldg(v + ((long long)it.b * p.g.heads + it.h) * p.n_pad + it.row0 + tw); };
+        float neg_lse = more ? row_value(p.neg_lse2) : 0.f, neg_del = more ? row_value(p.neg_delta) : 0.f;
+        for (int k = 0; ok && more; ++k) {
+            const int n = it.tiles.count();
+            const int row = it.row0 + tw, pos = it.seq.start + row;
+            const bool seen = pos >= 0 && pos < it.seq.len;
+            uint16_t* out = row < p.g.N ? p.dQ + (long long)it.b * p.q_batch + (long long)it.h * p.q_head + (long long)row * p.q_row : nullptr;
+            const uint64_t nl2 = pack_f32x2(neg_lse, neg_lse), nd2 = pack_f32x2(neg_del, neg_del);
+            for (int i = ((g & 1) == (uint32_t)x) ? 0 : 1; i < n; i += 2) {
+                const uint32_t t = g + i;
+                const int key0 = it.tiles.tile(i) * kWinT;
+                const bool full = tile_is_full(p.g, it.range, key0);
+                ok = mbar_wait_warp(smem_u32(&bars.s_full[x]), (t >> 1) & 1, abortp);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t r[kWinT];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(t_lane + C::kS + c * 32, r + c * 32);
-            tc_wait_ld();
-            tc_fence_before();
-            mbar_arrive(smem_u32(&bars.s_free));
-#pragma unroll
-            for (int c = 0; c < kWinT; c += 2) {
-                float a, e;
-                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), c22, nl2), a, e);
-                r[c] = __float_as_uint(ex2_approx(a));
-                r[c + 1] = __float_as_uint(ex2_approx(e));
-            }
-            if (!full) {
-                // K rows that no row here sees may hold anything: their dS is zero, which times NaN would not be
-                const int key = key0 + tw;
-                if (key >= range.hi || (key < range.lo && key >= p.g.sinks)) zero_row<D>(sK + (i % C::kK) * C::kTile, tw);
-                fence_proxy_async_smem();
-            }
-            ok = mbar_wait_warp(smem_u32(&bars.dp_full[x]), (i >> 1) & 1, abortp);
-            if (!ok) break;
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t d[32];
-                tmem_ld32(t_dp + c * 32, d);
+                for (int c = 0; c < 4; ++c) tmem_ld32(t_lane + C::kS + c * 32, r + c * 32);
                 tc_wait_ld();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&bars.s_free));
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    float u, v;
-                    unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), nd2),
-                                           pack_f32x2(__uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]))), u, v);
-                    d[e] = __float_as_uint(u);
-                    d[e + 1] = __float_as_uint(v);
+                for (int c = 0; c < kWinT; c += 2) {
+                    float a, e;
+                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), c22, nl2), a, e);
+                    r[c] = __float_as_uint(ex2_approx(a));
+                    r[c + 1] = __float_as_uint(ex2_approx(e));
                 }
                 if (!full) {
-                    const uint32_t bits = row_bits(p.g, seq, pos, key0 + c * 32);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) d[e] = (bits & (1u << e)) ? d[e] : 0u;
+                    // K rows that no row here sees may hold anything: their dS is zero, which times NaN would not be
+                    const int key = key0 + tw;
+                    if (key >= it.range.hi || (key < it.range.lo && key >= p.g.sinks)) zero_row<D>(sK + (t % C::kK) * C::kTile, tw);
+                    fence_proxy_async_smem();
                 }
+                ok = mbar_wait_warp(smem_u32(&bars.dp_full[x]), (t >> 1) & 1, abortp);
+                if (!ok) break;
+                tc_fence_after();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) d[e] = pack_16x2<F16>(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
-                tmem_st16(t_dp + c * 16, d);  // over columns that have been read
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t d[32];
+                    tmem_ld32(t_dp + c * 32, d);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float u, v;
+                        unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), nd2),
+                                               pack_f32x2(__uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]))), u, v);
+                        d[e] = __float_as_uint(u);
+                        d[e + 1] = __float_as_uint(v);
+                    }
+                    if (!full) {
+                        const uint32_t bits = row_bits(p.g, it.seq, pos, key0 + c * 32);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) d[e] = (bits & (1u << e)) ? d[e] : 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) d[e] = pack_16x2<F16>(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+                    tmem_st16(t_dp + c * 16, d);  // over columns that have been read
+                }
+                tc_wait_st();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&bars.ds_ready[x]));
             }
-            tc_wait_st();
-            tc_fence_before();
-            mbar_arrive(smem_u32(&bars.ds_ready[x]));
-        }
-        if (ok && mbar_wait_warp(smem_u32(&bars.acc_full), 0, abortp)) {
-            tc_fence_after();
-            if (x == 0) {
-                const bool seen = pos >= 0 && pos < seq.len;
-                store_row<D, F16>(t_lane + C::kDQ, p.scale, !seen,
-                                  row < p.g.N ? p.dQ + (long long)b * p.q_batch + (long long)h * p.q_head + (long long)row * p.q_row : nullptr);
+            if (!ok) break;
+            more = load_item(p, k + 1, it);
+            if (more) {  // under way while the accumulator is waited for
+                neg_lse = row_value(p.neg_lse2);
+                neg_del = row_value(p.neg_delta);
+            }
+            if (n > 0) {
+                ok = mbar_wait_warp(smem_u32(&bars.acc_full), n_it & 1, abortp);
+                if (!ok) break;
+                ++n_it;
+                g += (uint32_t)n;
+                tc_fence_after();
+            }
+            // either warpgroup stores half of the columns (nothing seen, n = 0: zeros)
+            store_row<F16>(t_lane + C::kDQ, x * (D / 64), (x + 1) * (D / 64), p.scale, !seen || n == 0, out, p.wide_q);
+            if (n > 0) {
+                tc_fence_before();
+                mbar_arrive(smem_u32(&bars.acc_free));
             }
         }
     }
@@ -388,7 +443,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 template <int D>
 struct DkvCfg {
     static constexpr int kTile = kWinT * D * 2;
-    static constexpr int kQ = 2;  // tiles in the rings of Q and of dO
+    static constexpr int kQ = 2;                 // tiles in the rings of Q and of dO
     static constexpr int kRows = 2 * kWinT * 4;  // bytes of a Q tile's LSE and D
     static constexpr int kSmem = (2 + 2 * kQ) * kTile + kQ * kRows;
     static constexpr uint32_t kS = 0, kDP = 128, kDV = 256, kDK = 384;
@@ -416,6 +471,59 @@ __device__ __forceinline__ uint32_t key_bits(const WindowGeom& g, const Sequence
     return bits_below(to + 1 - s.start - q0) & ~bits_below(from - s.start - q0);
 }
 
+struct DkvItem {
+    int b, hk, bh, kt, share, shares;
+    Sequence seq;
+    int key0, t0, per_head;  // query tiles t0 .. t0 + per_head - 1 of every head
+    int head, tile, n;       // the first of this item's n tiles: head (of those that share the key head), tile behind t0
+};
+// Items: the shares of the sinks' tiles first (the longest), then the other tiles, a sequence's neighbours side by side.
+__device__ __forceinline__ bool load_item(const BwdParams& p, int k, DkvItem& it) {
+    int idx = item_index(k);
+    if (idx >= p.n_dkv) return false;
+    const int n_shared = (int)p.bhk.d * p.sink_tiles * p.sink_shares;
+    if (idx < n_shared) {
+        it.bh = p.shared.div(idx, idx);
+        it.kt = p.shares.div(idx, it.share);
+        it.shares = p.sink_shares;
+    } else {
+        idx -= n_shared;
+        it.share = 0;
+        it.shares = 1;
+        if (p.longest_first)  // the first keys are seen by the most rows
+            it.kt = p.bhk.div(idx, it.bh);
+        else
+            it.bh = p.kt.div(idx, it.kt);
+        it.kt += p.sink_tiles;
+    }
+    it.b = p.heads_kv.div(it.bh, it.hk);
+    it.seq = load_sequence(p.g, it.b);
+    it.key0 = it.kt * kWinT;
+    const RowSpan span = row_span(p.g, it.seq, it.key0);
+    it.t0 = span.t0;
+    it.per_head = span.t1 - span.t0;
+    it.n = it.per_head * p.g.group;
+    it.head = it.tile = 0;
+    if (it.shares > 1 && it.n > 0) {
+        const int all = it.n, first = (int)((long long)all * it.share / it.shares);
+        it.n = (int)((long long)all * (it.share + 1) / it.shares) - first;
+        it.head = first / it.per_head;
+        it.tile = first - it.head * it.per_head;
+    }
+    return true;
+}
+// Walks over an item's tiles.
+struct Cursor {
+    int head, tile;
+    __device__ __forceinline__ explicit Cursor(const DkvItem& it) : head(it.head), tile(it.tile) {}
+    __device__ __forceinline__ void next(const DkvItem& it) {
+        if (++tile == it.per_head) {
+            tile = 0;
+            ++head;
+        }
+    }
+};
+
 template <int D, bool F16>
 __global__ void __launch_bounds__(kThreads, 1)
 window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -426,7 +534,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     uint8_t* sV = sK + C::kTile;
     uint8_t* sQ = sV + C::kTile;
     uint8_t* sG = sQ + C::kQ * C::kTile;
-    uint8_t* sR = sG + C::kQ * C::kTile;  // [stage][LSE, D][128]
+    uint8_t* sR = sG + C::kQ * C::kTile;  // [stage][-LSE, -D][128]
     __shared__ DkvBarriers bars;
     __shared__ uint32_t tmem_base_s, abort_flag;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -434,38 +542,10 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (tid == 0) atomicExch(p.status, (int)BSA_ERR_CUDA);
         return;
     }
-    // Items: the shares of the sinks' tiles first (the longest), then the other tiles, a sequence's neighbours side by side.
-    const int n_bh = p.g.batch * p.g.heads_kv, n_shared = p.sink_tiles * p.sink_shares;
-    int bh, kt, share = 0, shares = 1;
-    {
-        int idx = blockIdx.x;
-        if (idx < n_bh * n_shared) {
-            bh = idx / n_shared;
-            idx -= bh * n_shared;
-            kt = idx / p.sink_shares;
-            share = idx - kt * p.sink_shares;
-            shares = p.sink_shares;
-        } else {
-            idx -= n_bh * n_shared;
-            const int per = p.n_kt - p.sink_tiles;
-            if (p.longest_first) {  // the first keys are seen by the most rows
-                kt = p.sink_tiles + idx / n_bh;
-                bh = idx % n_bh;
-            } else {
-                bh = idx / per;
-                kt = p.sink_tiles + idx % per;
-            }
-        }
-    }
-    const int b = bh / p.g.heads_kv, hk = bh - b * p.g.heads_kv, key0 = kt * kWinT;
-    const Sequence seq = load_sequence(p.g, b);
-    const RowSpan span = row_span(p.g, seq, key0);
-    const int per_head = span.t1 - span.t0, all = per_head * p.g.group;
-    const int first = (int)((long long)all * share / shares), last = (int)((long long)all * (share + 1) / shares), n = last - first;
-
     if (tid == 0) {
         abort_flag = 0;
         mbar_init(smem_u32(&bars.kv_full), 1);
+        mbar_init(smem_u32(&bars.kv_empty), 1);
         for (int i = 0; i < C::kQ; ++i) {
             mbar_init(smem_u32(&bars.q_full[i]), 1);
             mbar_init(smem_u32(&bars.q_empty[i]), 1);
@@ -478,6 +558,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         mbar_init(smem_u32(&bars.p_ready[1]), 256);
         mbar_init(smem_u32(&bars.ds_ready), 256);
         mbar_init(smem_u32(&bars.acc_full), 1);
+        mbar_init(smem_u32(&bars.acc_free), 256);
         fence_mbar_init();
     }
     if (warp == 9) {
@@ -489,30 +570,37 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
     volatile uint32_t* abortp = &abort_flag;
-    auto head_of = [&](int i) { return hk * p.g.group + (first + i) / per_head; };
-    auto row_of = [&](int i) { return (span.t0 + (first + i) % per_head) * kWinT; };
+    DkvItem it;
 
     if (warp == 8) {
-        if (lane == 0 && n > 0) {
-            mbar_arrive_expect_tx(smem_u32(&bars.kv_full), 2 * C::kTile);
-            tma_load_rows(smem_u32(sK), &tmK, smem_u32(&bars.kv_full), key0, hk, b);
-            tma_load_rows(smem_u32(sV), &tmV, smem_u32(&bars.kv_full), key0, hk, b);
+        if (lane == 0) {
             Ring ring;
+            uint32_t n_it = 0;
             bool ok = true;
-            for (int i = 0; i < n; ++i, ring.advance<C::kQ>()) {
-                const int h = head_of(i), row = row_of(i);
-                ok = mbar_wait(smem_u32(&bars.q_empty[ring.stage]), ring.phase ^ 1, abortp);
+            for (int k = 0; ok && load_item(p, k, it); ++k) {
+                if (it.n == 0) continue;
+                ok = mbar_wait(smem_u32(&bars.kv_empty), (n_it & 1) ^ 1, abortp);
                 if (!ok) break;
-                const uint32_t bar = smem_u32(&bars.q_full[ring.stage]), rows = smem_u32(sR) + ring.stage * C::kRows;
-                const long long at = ((long long)b * p.g.heads + h) * p.n_pad + row;
-                mbar_arrive_expect_tx(bar, C::kTile + C::kRows);
-                tma_load_rows(smem_u32(sQ) + ring.stage * C::kTile, &tmQ, bar, row, h, b);
-                bulk_load(rows, p.neg_lse2 + at, kWinT * 4, bar);
-                bulk_load(rows + kWinT * 4, p.neg_delta + at, kWinT * 4, bar);
-                ok = mbar_wait(smem_u32(&bars.o_empty[ring.stage]), ring.phase ^ 1, abortp);
-                if (!ok) break;
-                mbar_arrive_expect_tx(smem_u32(&bars.o_full[ring.stage]), C::kTile);
-                tma_load_rows(smem_u32(sG) + ring.stage * C::kTile, &tmG, smem_u32(&bars.o_full[ring.stage]), row, h, b);
+                ++n_it;
+                mbar_arrive_expect_tx(smem_u32(&bars.kv_full), 2 * C::kTile);
+                tma_load_rows(smem_u32(sK), &tmK, smem_u32(&bars.kv_full), it.key0, it.hk, it.b);
+                tma_load_rows(smem_u32(sV), &tmV, smem_u32(&bars.kv_full), it.key0, it.hk, it.b);
+                Cursor at(it);
+                for (int i = 0; i < it.n; ++i, ring.advance<C::kQ>(), at.next(it)) {
+                    const int h = it.hk * p.g.group + at.head, row = (it.t0 + at.tile) * kWinT;
+                    ok = mbar_wait(smem_u32(&bars.q_empty[ring.stage]), ring.phase ^ 1, abortp);
+                    if (!ok) break;
+                    const uint32_t bar = smem_u32(&bars.q_full[ring.stage]), rows = smem_u32(sR) + ring.stage * C::kRows;
+                    const long long from = ((long long)it.b * p.g.heads + h) * p.n_pad + row;
+                    mbar_arrive_expect_tx(bar, C::kTile + C::kRows);
+                    tma_load_rows(smem_u32(sQ) + ring.stage * C::kTile, &tmQ, bar, row, h, it.b);
+                    bulk_load(rows, p.neg_lse2 + from, kWinT * 4, bar);
+                    bulk_load(rows + kWinT * 4, p.neg_delta + from, kWinT * 4, bar);
+                    ok = mbar_wait(smem_u32(&bars.o_empty[ring.stage]), ring.phase ^ 1, abortp);
+                    if (!ok) break;
+                    mbar_arrive_expect_tx(smem_u32(&bars.o_full[ring.stage]), C::kTile);
+                    tma_load_rows(smem_u32(sG) + ring.stage * C::kTile, &tmG, smem_u32(&bars.o_full[ring.stage]), row, h, it.b);
+                }
             }
             if (!ok) let_copies_land();
         }
@@ -525,6 +613,9 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const uint64_t descQ = make_smem_desc_sw128(smem_u32(sQ), 16, 1024), descG = make_smem_desc_sw128(smem_u32(sG), 16, 1024);
         const uint64_t descQt = make_smem_desc_sw128(smem_u32(sQ), SUB, 1024), descGt = make_smem_desc_sw128(smem_u32(sG), SUB, 1024);
         const bool leader = elect_one();
+        Ring cur, next;  // of the tile whose gradients, and of the one whose scores come next
+        uint32_t n_it = 0, t = 0;
+        bool ok = true;
         auto product = [&](uint32_t d, uint64_t a, uint64_t b0) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
@@ -532,189 +623,198 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 mma_ss(d, a + off, b0 + off, idesc_s, kk > 0);
             }
         };
-        auto gradient = [&](uint32_t d, uint32_t a, uint64_t b0, bool begin) {
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk)
-                mma_ts(d, a + (kk < 4 ? kk * 8 : 64 + (kk - 4) * 8), b0 + (uint64_t)(kk * 128), idesc_g, (begin && kk == 0) ? 0u : 1u);
-        };
-        Ring cur, next;
-        bool ok = n > 0 && mbar_wait_warp(smem_u32(&bars.kv_full), 0, abortp) && mbar_wait_warp(smem_u32(&bars.q_full[0]), 0, abortp);
-        if (ok) {
+        auto issue_s = [&]() -> bool {
+            if (!mbar_wait_warp(smem_u32(&bars.q_full[next.stage]), next.phase, abortp)) return false;
             tc_fence_after();
             if (leader) {
-                product(tmem + C::kS, descK, descQ);
+                product(tmem + C::kS, descK, descQ + (uint64_t)((next.stage * C::kTile) >> 4));
                 mma_commit(smem_u32(&bars.s_full));
             }
-            ok = mbar_wait_warp(smem_u32(&bars.o_full[0]), 0, abortp);
-            tc_fence_after();
-            if (ok && leader) {
-                product(tmem + C::kDP, descV, descG);
-                mma_commit(smem_u32(&bars.dp_full));
-            }
-        }
-        next.advance<C::kQ>();
-        for (int i = 0; ok && i < n; ++i) {
-            const uint64_t g0 = descGt + (uint64_t)((cur.stage * C::kTile) >> 4);
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                ok = ok && mbar_wait_warp(smem_u32(&bars.p_ready[part]), i & 1, abortp);
-                if (!ok) break;
-                tc_fence_after();
-                if (leader) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int kk = (e >> 1) * 4 + part * 2 + (e & 1);  // 16 query rows, of either warpgroup's 64
-                        mma_ts(tmem + C::kDV, tmem + C::kS + (kk < 4 ? kk * 8 : 64 + (kk - 4) * 8), g0 + (uint64_t)(kk * 128), idesc_g,
-                               (i > 0 || part > 0 || e > 0) ? 1u : 0u);
-                    }
-                }
-            }
-            if (!ok) break;
-            if (leader) mma_commit(smem_u32(&bars.o_empty[cur.stage]));
-            if (i + 1 < n) {
-                ok = mbar_wait_warp(smem_u32(&bars.q_full[next.stage]), next.phase, abortp);
-                if (!ok) break;
-                tc_fence_after();
-                if (leader) {
-                    product(tmem + C::kS, descK, descQ + (uint64_t)((next.stage * C::kTile) >> 4));
-                    mma_commit(smem_u32(&bars.s_full));
-                }
-            }
-            ok = mbar_wait_warp(smem_u32(&bars.ds_ready), i & 1, abortp);
-            if (!ok) break;
+            return true;
+        };
+        auto issue_dp = [&](bool last) -> bool {
+            if (!mbar_wait_warp(smem_u32(&bars.o_full[next.stage]), next.phase, abortp)) return false;
             tc_fence_after();
             if (leader) {
-                gradient(tmem + C::kDK, tmem + C::kDP, descQt + (uint64_t)((cur.stage * C::kTile) >> 4), i == 0);
-                mma_commit(smem_u32(&bars.q_empty[cur.stage]));
-                if (i == n - 1) mma_commit(smem_u32(&bars.acc_full));
+                product(tmem + C::kDP, descV, descG + (uint64_t)((next.stage * C::kTile) >> 4));
+                mma_commit(smem_u32(&bars.dp_full));
+                if (last) mma_commit(smem_u32(&bars.kv_empty));  // (its S is in front of it)
             }
-            if (i + 1 < n) {
-                ok = mbar_wait_warp(smem_u32(&bars.o_full[next.stage]), next.phase, abortp);
+            next.advance<C::kQ>();
+            return true;
+        };
+        for (int k = 0; ok && load_item(p, k, it); ++k) {
+            const int n = it.n;
+            if (n == 0) continue;
+            ok = mbar_wait_warp(smem_u32(&bars.kv_full), n_it & 1, abortp);
+            ok = ok && issue_s() && issue_dp(n == 1);
+            ok = ok && mbar_wait_warp(smem_u32(&bars.acc_free), (n_it & 1) ^ 1, abortp);  // the last item's gradients are out
+            ++n_it;
+            for (int i = 0; ok && i < n; ++i, ++t) {
+                const uint64_t g0 = descGt + (uint64_t)((cur.stage * C::kTile) >> 4), q0 = descQt + (uint64_t)((cur.stage * C::kTile) >> 4);
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    ok = ok && mbar_wait_warp(smem_u32(&bars.p_ready[part]), t & 1, abortp);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (leader) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int kk = (e >> 1) * 4 + part * 2 + (e & 1);  // 16 query rows, of either warpgroup's 64
+                            mma_ts(tmem + C::kDV, tmem + C::kS + (kk < 4 ? kk * 8 : 64 + (kk - 4) * 8), g0 + (uint64_t)(kk * 128), idesc_g,
+                                   (i > 0 || part > 0 || e > 0) ? 1u : 0u);
+                        }
+                    }
+                }
+                if (!ok) break;
+                if (leader) mma_commit(smem_u32(&bars.o_empty[cur.stage]));
+                if (i + 1 < n) ok = issue_s();
+                ok = ok && mbar_wait_warp(smem_u32(&bars.ds_ready), t & 1, abortp);
                 if (!ok) break;
                 tc_fence_after();
                 if (leader) {
-                    product(tmem + C::kDP, descV, descG + (uint64_t)((next.stage * C::kTile) >> 4));
-                    mma_commit(smem_u32(&bars.dp_full));
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        mma_ts(tmem + C::kDK, tmem + C::kDP + (kk < 4 ? kk * 8 : 64 + (kk - 4) * 8), q0 + (uint64_t)(kk * 128), idesc_g,
+                               (i > 0 || kk > 0) ? 1u : 0u);
+                    mma_commit(smem_u32(&bars.q_empty[cur.stage]));
+                    if (i == n - 1) mma_commit(smem_u32(&bars.acc_full));
                 }
+                if (i + 1 < n) ok = issue_dp(i + 2 == n);
+                cur.advance<C::kQ>();
             }
-            cur.advance<C::kQ>();
-            next.advance<C::kQ>();
         }
     } else {
-        const int x = warp >> 2, tw = tid & 127, key = key0 + tw;
+        // A tile is shared by columns: warpgroup x takes query rows 64 x .. 64 x + 63 of it, thread = key.
+        const int x = warp >> 2, tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t t_s = t_lane + C::kS + x * 64, t_dp = t_lane + C::kDP + x * 64;
         const float c2 = p.scale_log2;
+        uint32_t t = 0, n_it = 0;
         bool ok = true;
         Ring ring;
-        for (int i = 0; i < n; ++i, ring.advance<C::kQ>()) {
-            const int row0 = row_of(i), pos0 = seq.start + row0;
-            const bool rows_ok = pos0 >= 0 && pos0 + kWinT <= seq.len;
-            const bool full = rows_ok && key0 + kWinT <= seq.len && key0 + kWinT - 1 <= pos0 + p.g.right &&
-                              (pos0 + kWinT - 1 <= key0 + p.g.left || key0 + kWinT <= p.g.sinks);
-            const float4* lse = reinterpret_cast<const float4*>(sR + ring.stage * C::kRows) + x * 16;
-            const float4* del = lse + kWinT / 4;  // (both negated)
-            ok = mbar_wait_warp(smem_u32(&bars.q_full[ring.stage]), ring.phase, abortp) && mbar_wait_warp(smem_u32(&bars.s_full), i & 1, abortp);
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t r[64];
-            tmem_ld32(t_s, r);
-            tmem_ld32(t_s + 32, r + 32);
-            tc_wait_ld();
-            const uint64_t c22 = pack_f32x2(c2, c2);
-            uint32_t bits[2] = {0xffffffffu, 0xffffffffu};
-            if (!full) {
-                bits[0] = key_bits(p.g, seq, key, row0 + x * 64);
-                bits[1] = key_bits(p.g, seq, key, row0 + x * 64 + 32);
-                if (!rows_ok) {  // rows at no position may hold anything: their weight is zero, which times NaN would not be
-                    ok = mbar_wait_warp(smem_u32(&bars.o_full[ring.stage]), ring.phase, abortp);
-                    if (!ok) break;
-                    if (pos0 + tw < 0 || pos0 + tw >= seq.len) zero_row<D>((x ? sQ : sG) + ring.stage * C::kTile, tw);
-                    fence_proxy_async_smem();
-                }
-            }
-            // P goes out in two parts of 32 columns: the first part's products run beside the second's exponentials
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-#pragma unroll
-                for (int c = part * 32; c < part * 32 + 32; c += 4) {
-                    const float4 l = lse[c / 4];
-                    float a0, a1, a2, a3;
-                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), c22, pack_f32x2(l.x, l.y)), a0, a1);
-                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c + 2]), __uint_as_float(r[c + 3])), c22, pack_f32x2(l.z, l.w)), a2, a3);
-                    r[c] = __float_as_uint(ex2_approx(a0));
-                    r[c + 1] = __float_as_uint(ex2_approx(a1));
-                    r[c + 2] = __float_as_uint(ex2_approx(a2));
-                    r[c + 3] = __float_as_uint(ex2_approx(a3));
-                }
+        for (int k = 0; ok && load_item(p, k, it); ++k) {
+            const int n = it.n, key0 = it.key0, key = key0 + tw;
+            const Sequence seq = it.seq;
+            Cursor at(it);
+            for (int i = 0; i < n; ++i, ++t, ring.advance<C::kQ>(), at.next(it)) {
+                const int row0 = (it.t0 + at.tile) * kWinT, pos0 = seq.start + row0;
+                const bool rows_ok = pos0 >= 0 && pos0 + kWinT <= seq.len;
+                const bool full = rows_ok && key0 + kWinT <= seq.len && key0 + kWinT - 1 <= pos0 + p.g.right &&
+                                  (pos0 + kWinT - 1 <= key0 + p.g.left || key0 + kWinT <= p.g.sinks);
+                const float4* lse = reinterpret_cast<const float4*>(sR + ring.stage * C::kRows) + x * 16;
+                const float4* del = lse + kWinT / 4;  // (both negated)
+                ok = mbar_wait_warp(smem_u32(&bars.q_full[ring.stage]), ring.phase, abortp) && mbar_wait_warp(smem_u32(&bars.s_full), t & 1, abortp);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t r[64];
+                tmem_ld32(t_s, r);
+                tmem_ld32(t_s + 32, r + 32);
+                tc_wait_ld();
+                const uint64_t c22 = pack_f32x2(c2, c2);
+                uint32_t bits[2] = {0xffffffffu, 0xffffffffu};
                 if (!full) {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) r[part * 32 + c] = (bits[part] & (1u << c)) ? r[part * 32 + c] : 0u;
+                    bits[0] = key_bits(p.g, seq, key, row0 + x * 64);
+                    bits[1] = key_bits(p.g, seq, key, row0 + x * 64 + 32);
+                    if (!rows_ok) {  // rows at no position may hold anything: their weight is zero, which times NaN would not be
+                        ok = mbar_wait_warp(smem_u32(&bars.o_full[ring.stage]), ring.phase, abortp);
+                        if (!ok) break;
+                        if (pos0 + tw < 0 || pos0 + tw >= seq.len) zero_row<D>((x ? sQ : sG) + ring.stage * C::kTile, tw);
+                        fence_proxy_async_smem();
+                    }
                 }
-                uint32_t q[16];
+                // P goes out in two parts of 32 columns: the first part's products run beside the second's exponentials
 #pragma unroll
-                for (int e = 0; e < 16; ++e) q[e] = pack_16x2<F16>(__uint_as_float(r[part * 32 + 2 * e]), __uint_as_float(r[part * 32 + 2 * e + 1]));
-                tmem_st16(t_s + part * 16, q);
+                for (int part = 0; part < 2; ++part) {
+#pragma unroll
+                    for (int c = part * 32; c < part * 32 + 32; c += 4) {
+                        const float4 l = lse[c / 4];
+                        float a0, a1, a2, a3;
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), c22, pack_f32x2(l.x, l.y)), a0, a1);
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c + 2]), __uint_as_float(r[c + 3])), c22, pack_f32x2(l.z, l.w)), a2, a3);
+                        r[c] = __float_as_uint(ex2_approx(a0));
+                        r[c + 1] = __float_as_uint(ex2_approx(a1));
+                        r[c + 2] = __float_as_uint(ex2_approx(a2));
+                        r[c + 3] = __float_as_uint(ex2_approx(a3));
+                    }
+                    if (!full) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) r[part * 32 + c] = (bits[part] & (1u << c)) ? r[part * 32 + c] : 0u;
+                    }
+                    uint32_t q[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) q[e] = pack_16x2<F16>(__uint_as_float(r[part * 32 + 2 * e]), __uint_as_float(r[part * 32 + 2 * e + 1]));
+                    tmem_st16(t_s + part * 16, q);
+                    tc_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&bars.p_ready[part]));
+                }
+                ok = mbar_wait_warp(smem_u32(&bars.dp_full), t & 1, abortp);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t d[32];
+                    tmem_ld32(t_dp + c * 32, d);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 l = del[c * 8 + e / 4];
+                        float a0, a1, a2, a3;
+                        unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pack_f32x2(l.x, l.y)),
+                                               pack_f32x2(__uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]))), a0, a1);
+                        unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])), pack_f32x2(l.z, l.w)),
+                                               pack_f32x2(__uint_as_float(r[c * 32 + e + 2]), __uint_as_float(r[c * 32 + e + 3]))), a2, a3);
+                        d[e] = __float_as_uint(a0);
+                        d[e + 1] = __float_as_uint(a1);
+                        d[e + 2] = __float_as_uint(a2);
+                        d[e + 3] = __float_as_uint(a3);
+                    }
+                    if (!full) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) d[e] = (bits[c] & (1u << e)) ? d[e] : 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) r[c * 32 + e] = pack_16x2<F16>(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+                }
+                tmem_st16(t_dp, r);
+                tmem_st16(t_dp + 16, r + 32);
                 tc_wait_st();
                 tc_fence_before();
-                mbar_arrive(smem_u32(&bars.p_ready[part]));
+                mbar_arrive(smem_u32(&bars.ds_ready));
             }
-            ok = mbar_wait_warp(smem_u32(&bars.dp_full), i & 1, abortp);
             if (!ok) break;
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t d[32];
-                tmem_ld32(t_dp + c * 32, d);
-                tc_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 l = del[c * 8 + e / 4];
-                    float a0, a1, a2, a3;
-                    unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pack_f32x2(l.x, l.y)),
-                                           pack_f32x2(__uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]))), a0, a1);
-                    unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])), pack_f32x2(l.z, l.w)),
-                                           pack_f32x2(__uint_as_float(r[c * 32 + e + 2]), __uint_as_float(r[c * 32 + e + 3]))), a2, a3);
-                    d[e] = __float_as_uint(a0);
-                    d[e + 1] = __float_as_uint(a1);
-                    d[e + 2] = __float_as_uint(a2);
-                    d[e + 3] = __float_as_uint(a3);
-                }
-                if (!full) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) d[e] = (bits[c] & (1u << e)) ? d[e] : 0u;
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) r[c * 32 + e] = pack_16x2<F16>(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+            if (n > 0) {
+                ok = mbar_wait_warp(smem_u32(&bars.acc_full), n_it & 1, abortp);
+                if (!ok) break;
+                ++n_it;
+                tc_fence_after();
             }
-            tmem_st16(t_dp, r);
-            tmem_st16(t_dp + 16, r + 32);
-            tc_wait_st();
-            tc_fence_before();
-            mbar_arrive(smem_u32(&bars.ds_ready));
-        }
-        // Warps 0-3 write dV, warps 4-7 dK.
-        if (n > 0) ok = ok && mbar_wait_warp(smem_u32(&bars.acc_full), 0, abortp);
-        tc_fence_after();
-        if (ok) {
+            // Warps 0-3 write dV, warps 4-7 dK.
             const uint32_t t_acc = t_lane + (x ? C::kDK : C::kDV);
-            if (shares > 1) {
-                float* out = p.partial + ((((long long)bh * p.sink_tiles + kt) * shares + share) * 2 + x) * kWinT * D + tw * D;
+            if (it.shares > 1) {
+                float* out = p.partial + ((((long long)it.bh * p.sink_tiles + it.kt) * it.shares + it.share) * 2 + x) * kWinT * D + tw * D;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
-                    if (n > 0) {
-                        tmem_ld32(t_acc + c * 32, o);
-                        tc_wait_ld();
-                    }
+                    tmem_ld32(t_acc + c * 32, o);
+                    tc_wait_ld();
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        reinterpret_cast<uint4*>(out + c * 32)[q] = n > 0 ? make_uint4(o[q * 4], o[q * 4 + 1], o[q * 4 + 2], o[q * 4 + 3]) : make_uint4(0, 0, 0, 0);
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = n > 0 ? o[q * 8 + e] : 0u;
+                        st_global_v8(out + c * 32 + q * 8, v);
+                    }
                 }
             } else {
-                uint16_t* out = x ? p.dK + (long long)b * p.k_batch + (long long)hk * p.k_head + (long long)key * p.k_row
-                                  : p.dV + (long long)b * p.v_batch + (long long)hk * p.v_head + (long long)key * p.v_row;
-                store_row<D, F16>(t_acc, x ? p.scale : 1.f, n == 0, key < p.g.N_kv ? out : nullptr);
+                uint16_t* out = x ? p.dK + (long long)it.b * p.k_batch + (long long)it.hk * p.k_head + (long long)key * p.k_row
+                                  : p.dV + (long long)it.b * p.v_batch + (long long)it.hk * p.v_head + (long long)key * p.v_row;
+                store_row<F16>(t_acc, 0, D / 32, x ? p.scale : 1.f, n == 0, key < p.g.N_kv ? out : nullptr, x ? p.wide_k : p.wide_v);
+            }
+            if (n > 0) {
+                tc_fence_before();
+                mbar_arrive(smem_u32(&bars.acc_free));
             }
         }
     }
@@ -800,9 +900,8 @@ cudaError_t launch(const WindowArgs& a, const Layout& l, const bsa_view_t& Q, co
     }
     window_delta_kernel<D, F16><<<dim3((unsigned)(l.n_pad / 32), (unsigned)(g.batch * g.heads)), 256, 0, stream>>>(
         g, static_cast<const uint16_t*>(O.data), static_cast<const uint16_t*>(G.data), O.batch, O.head, O.row, G.batch, G.head, G.row, LSE, lse2, delta, l.n_pad);
-    dq<<<(unsigned)(l.n_qt * g.batch * g.heads), kThreads, DqCfg<D>::kSmem, stream>>>(tq, tk, tv, tg, p);
-    const unsigned items = (unsigned)(g.batch * g.heads_kv) * (unsigned)(l.sink_tiles * l.sink_shares + (l.n_kt - l.sink_tiles));
-    dkv<<<items, kThreads, DkvCfg<D>::kSmem, stream>>>(tq, tk, tv, tg, p);
+    dq<<<p.n_dq < a.num_sms ? p.n_dq : a.num_sms, kThreads, DqCfg<D>::kSmem, stream>>>(tq, tk, tv, tg, p);
+    dkv<<<p.n_dkv < a.num_sms ? p.n_dkv : a.num_sms, kThreads, DkvCfg<D>::kSmem, stream>>>(tq, tk, tv, tg, p);
     count_launch(3);
     if (l.sink_tiles) {
         window_sink_sum_kernel<D, F16><<<dim3((unsigned)(l.sink_tiles * kWinT * D / 8 / 256), (unsigned)(g.batch * g.heads_kv), 2), 256, 0, stream>>>(p);
@@ -853,8 +952,24 @@ extern "C" bsa_status_t bsa_window_backward(const bsa_window_desc_t* t, const bs
     p.q_batch = dQ->batch; p.q_head = dQ->head; p.q_row = dQ->row;
     p.k_batch = dK->batch; p.k_head = dK->head; p.k_row = dK->row;
     p.v_batch = dV->batch; p.v_head = dV->head; p.v_row = dV->row;
-    p.n_qt = l.n_qt;
-    p.n_kt = l.n_kt;
+    p.n_dq = l.n_qt * a.g.batch * a.g.heads;
+    p.n_dkv = a.g.batch * a.g.heads_kv * (l.sink_tiles * l.sink_shares + (l.n_kt - l.sink_tiles));
+    p.qt = Divisor(l.n_qt);
+    p.heads = Divisor(a.g.heads);
+    p.bh = Divisor(a.g.batch * a.g.heads);
+    p.heads_kv = Divisor(a.g.heads_kv);
+    p.group = Divisor(a.g.group);
+    p.kt = Divisor(l.n_kt > l.sink_tiles ? l.n_kt - l.sink_tiles : 1);
+    p.bhk = Divisor(a.g.batch * a.g.heads_kv);
+    p.shares = Divisor(l.sink_shares);
+    p.shared = Divisor(l.sink_tiles > 0 ? l.sink_tiles * l.sink_shares : 1);
+    const auto wide = [&](const bsa_view_t* v, int64_t heads, int64_t rows) {
+        const auto on32 = [](int64_t n, int64_t stride) { return n == 1 || stride % 16 == 0; };
+        return (reinterpret_cast<uintptr_t>(v->data) & 31) == 0 && on32(a.g.batch, v->batch) && on32(heads, v->head) && on32(rows, v->row);
+    };
+    p.wide_q = wide(dQ, a.g.heads, a.g.N);
+    p.wide_k = wide(dK, a.g.heads_kv, a.g.N_kv);
+    p.wide_v = wide(dV, a.g.heads_kv, a.g.N_kv);
     p.longest_first = a.g.left >= a.g.N_kv;
     p.sink_tiles = l.sink_tiles;
     p.sink_shares = l.sink_shares;

@@ -49,7 +49,7 @@ struct Params {
     long long o_batch, o_head, o_row;
     float* LSE;
     float scale_log2;  // scale * log2(e)
-    int n_qt;          // 128-row tiles of a sequence
+    Divisor qt, heads, bh, group;  // 128-row tiles of a sequence, heads, batch x heads, heads that share a key head
     int n_items;
     int longest_first; // no left limit: later tiles are longer
 };
@@ -62,7 +62,7 @@ struct __align__(8) Barriers {
 };
 
 struct Item {
-    int b, h, row0;
+    int b, h, hk, row0;
     Sequence seq;
     KeyRange range;
     TileSpan tiles;
@@ -75,15 +75,13 @@ __device__ __forceinline__ bool load_item(const Params& p, int k, Item& it) {
     if (idx >= p.n_items) return false;
     int bh, qt;
     if (p.longest_first) {
-        const int n_bh = p.g.batch * p.g.heads;
-        qt = p.n_qt - 1 - idx / n_bh;
-        bh = idx % n_bh;
+        qt = (int)p.qt.d - 1 - p.bh.div(idx, bh);
     } else {
-        bh = idx / p.n_qt;
-        qt = idx % p.n_qt;
+        bh = p.qt.div(idx, qt);
     }
-    it.b = bh / p.g.heads;
-    it.h = bh - it.b * p.g.heads;
+    int rest;
+    it.b = p.heads.div(bh, it.h);
+    it.hk = p.group.div(it.h, rest);
     it.row0 = qt * kWinT;
     it.seq = load_sequence(p.g, it.b);
     it.range = key_range(p.g, it.seq, it.row0, it.row0 + kWinT);
@@ -316,7 +314,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             uint32_t n_q = 0;
             bool ok = true;
             for (int k = 0; ok && load_item(p, k, it); ++k) {
-                const int n = it.tiles.count(), hk = it.h / p.g.group;
+                const int n = it.tiles.count(), hk = it.hk;
                 if (n == 0) continue;
                 const uint32_t qb = n_q & 1;
                 ok = mbar_wait(smem_u32(&bars.q_empty[qb]), ((n_q >> 1) & 1) ^ 1, abortp);
@@ -338,7 +336,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             Ring ring;
             bool ok = true;
             for (int k = 0; ok && load_item(p, k, it); ++k) {
-                const int n = it.tiles.count(), hk = it.h / p.g.group;
+                const int n = it.tiles.count(), hk = it.hk;
                 for (int j = 0; j < n; ++j, ring.advance<C::kV>()) {
                     ok = mbar_wait(smem_u32(&bars.v_empty[ring.stage]), ring.phase ^ 1, abortp);
                     if (!ok) break;
@@ -451,18 +449,11 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 if (!full) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) hide(r + c * 32, row_bits(p.g, it.seq, pos, key0 + c * 32));
-                    // V rows that no row of this tile sees may hold anything: their weight is zero, which times NaN would not be
                     const int from = it.range.hi - key0, below = it.range.lo - key0;
                     if (from < kWinT || (below > 0 && p.g.sinks - key0 < below)) {
                         ok = mbar_wait_warp(smem_u32(&bars.v_full[t % C::kV]), (t / C::kV) & 1, abortp);
                         if (!ok) break;
-                        if (tw >= from || (tw < below && key0 + tw >= p.g.sinks)) {
-                            uint4* v = reinterpret_cast<uint4*>(sV + (t % C::kV) * C::kTile + tw * 128);
-#pragma unroll
-                            for (int s = 0; s < D / 64; ++s)
-#pragma unroll
-                                for (int c = 0; c < 8; ++c) v[s * (SUB / 16) + c] = make_uint4(0, 0, 0, 0);
-                        }
+                        zero_unseen_keys<D>(sV + (t % C::kV) * C::kTile, p.g, it.range, key0, tw);
                         fence_proxy_async_smem();
                     }
                 }
@@ -590,8 +581,12 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     p.o_batch = O->batch; p.o_head = O->head; p.o_row = O->row;
     p.LSE = LSE;
     p.scale_log2 = a.scale * 1.4426950408889634f;
-    p.n_qt = (a.g.N + kWinT - 1) / kWinT;
-    const int64_t items = (int64_t)p.n_qt * a.g.batch * a.g.heads;
+    const int n_qt = (a.g.N + kWinT - 1) / kWinT;
+    p.qt = Divisor(n_qt);
+    p.heads = Divisor(a.g.heads);
+    p.bh = Divisor(a.g.batch * a.g.heads);
+    p.group = Divisor(a.g.group);
+    const int64_t items = (int64_t)n_qt * a.g.batch * a.g.heads;
     if (items > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
     p.n_items = (int)items;
     p.longest_first = a.g.left >= a.g.N_kv;

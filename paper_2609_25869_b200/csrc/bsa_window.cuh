@@ -94,6 +94,22 @@ __device__ __forceinline__ void hide(uint32_t* r, uint32_t bits) {
     for (int i = 0; i < 32; ++i) r[i] = (bits & (1u << i)) ? r[i] : 0xff800000u;
 }
 
+// Rows of a tile in shared memory that no row of the CTA sees may hold anything, and a weight of zero times NaN would not be zero:
+// they become zero themselves (all their 64-column sub-tiles, whatever the swizzle).  128 threads, eight to a row, so that a warp's stores
+// fall into different banks (with a row to a thread a window's edge tile took 2000 clk more); the caller fences.
+template <int D>
+__device__ __forceinline__ void zero_rows(uint8_t* tile, int from, int to, int thread) {
+    for (int row = max(from, 0) + (thread >> 3); row < min(to, kWinT); row += 16)
+#pragma unroll
+        for (int s = 0; s < D / 64; ++s)
+            *reinterpret_cast<uint4*>(tile + s * (kWinT * 128) + row * 128 + (thread & 7) * 16) = make_uint4(0, 0, 0, 0);
+}
+template <int D>
+__device__ __forceinline__ void zero_unseen_keys(uint8_t* tile, const WindowGeom& g, const KeyRange& k, int key0, int thread) {
+    zero_rows<D>(tile, g.sinks - key0, k.lo - key0, thread);
+    zero_rows<D>(tile, k.hi - key0, kWinT, thread);
+}
+
 // Division of non-negative ints by a constant of the call: the items of a persistent CTA are decoded on its critical path.
 struct Divisor {
     uint32_t d, mul, shift;

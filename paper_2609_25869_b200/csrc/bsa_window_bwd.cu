@@ -88,15 +88,6 @@ __device__ __forceinline__ int item_index(int k) {
     return k * G + ((k & 1) ? (G - 1 - (int)blockIdx.x) : (int)blockIdx.x);
 }
 
-// Row `row` of a tile in shared memory becomes zero (its 64-column sub-tiles, whatever the swizzle).
-template <int D>
-__device__ __forceinline__ void zero_row(uint8_t* tile, int row) {
-#pragma unroll
-    for (int s = 0; s < D / 64; ++s)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) reinterpret_cast<uint4*>(tile + s * SUB + row * 128)[c] = make_uint4(0, 0, 0, 0);
-}
-
 // Columns [c0 * 32, c1 * 32) of a row of an accumulator, times `f`, to global memory in the element type; out null: nowhere.
 template <bool F16>
 __device__ __forceinline__ void store_row(uint32_t t_acc, int c0, int c1, float f, bool zero, uint16_t* out, int wide) {
@@ -378,9 +369,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                     r[c + 1] = __float_as_uint(ex2_approx(e));
                 }
                 if (!full) {
-                    // K rows that no row here sees may hold anything: their dS is zero, which times NaN would not be
-                    const int key = key0 + tw;
-                    if (key >= it.range.hi || (key < it.range.lo && key >= p.g.sinks)) zero_row<D>(sK + (t % C::kK) * C::kTile, tw);
+                    zero_unseen_keys<D>(sK + (t % C::kK) * C::kTile, p.g, it.range, key0, tw);
                     fence_proxy_async_smem();
                 }
                 ok = mbar_wait_warp(smem_u32(&bars.dp_full[x]), (t >> 1) & 1, abortp);
@@ -716,10 +705,12 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 if (!full) {
                     bits[0] = key_bits(p.g, seq, key, row0 + x * 64);
                     bits[1] = key_bits(p.g, seq, key, row0 + x * 64 + 32);
-                    if (!rows_ok) {  // rows at no position may hold anything: their weight is zero, which times NaN would not be
+                    if (!rows_ok) {  // rows at no position
                         ok = mbar_wait_warp(smem_u32(&bars.o_full[ring.stage]), ring.phase, abortp);
                         if (!ok) break;
-                        if (pos0 + tw < 0 || pos0 + tw >= seq.len) zero_row<D>((x ? sQ : sG) + ring.stage * C::kTile, tw);
+                        uint8_t* rows = (x ? sQ : sG) + ring.stage * C::kTile;
+                        zero_rows<D>(rows, 0, -pos0, tw);
+                        zero_rows<D>(rows, seq.len - pos0, kWinT, tw);
                         fence_proxy_async_smem();
                     }
                 }

@@ -186,6 +186,9 @@ bool view_ok(const bsa_view_t* v, int64_t batch, int64_t heads, int64_t rows) {
 
 using namespace bsa;
 
+// the binding packs them as bytes
+static_assert(sizeof(bsa_view_t) == 32 && sizeof(bsa_rope_desc_t) == 136 && sizeof(bsa_window_desc_t) == 80, "layout of the C structs");
+
 extern "C" bsa_status_t bsa_rope(const bsa_rope_desc_t* t, const bsa_view_t* Q, const bsa_view_t* K, const bsa_view_t* Q_out,
                                  const bsa_view_t* K_out, void* stream_v) {
     if (!t || t->batch < 1 || t->heads < 1 || t->heads_kv < 0 || t->N < 1 || t->d < 1 || t->n_axes < 1 || t->n_axes > BSA_MAX_AXES)

@@ -34,6 +34,10 @@ __device__ int g_window_status = 0;
 constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;
 constexpr float kRescale = 8.0f;  // log2 units: P stays below 2^8 between rescales
+// Half: P is computed 2^7 times as large, up to 2^15 (half ends at 2^16).  A row's largest weight is at least its reference's, so what
+// half loses below 2^-14 of P is below 2^-21 of it.
+template <bool F16>
+constexpr float kShift = F16 ? 7.0f : 0.0f;
 
 template <int D>
 struct Cfg {
@@ -280,7 +284,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             mbar_arrive(smem_u32(&bars.e_taken));
             const bool any = seen && l > 0.f;
             const float inv = any ? 1.f / l : 0.f;
-            if (row_ok) *lse_out = any ? fmaf(m, 0.6931471805599453f, logf(l)) : -INFINITY;
+            if (row_ok) *lse_out = any ? fmaf(m - kShift<F16>, 0.6931471805599453f, logf(l)) : -INFINITY;
             m = m_next;
             if (!mbar_wait_warp(smem_u32(&bars.o_full), n_it & 1, abortp)) break;
             ++n_it;
@@ -461,7 +465,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     l *= ex2_approx(m_ref - m);  // (m_ref = -inf: l is zero)
                     m_ref = m;
                 }
-                const float neg_m = (m == -INFINITY) ? 0.f : -m;
+                const float neg_m = (m == -INFINITY) ? 0.f : kShift<F16> - m;
                 const uint64_t nm2 = pack_f32x2(neg_m, neg_m);
                 uint64_t sum01 = pack_f32x2(0.f, 0.f), sum23 = sum01;
                 exp_keys<F16>(r, c22, nm2, sum01, sum23);

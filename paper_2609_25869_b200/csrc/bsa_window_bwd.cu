@@ -30,13 +30,19 @@ namespace {
 constexpr int kThreads = 320;  // warps 0-7: softmax, 8: copies, 9: products
 constexpr uint32_t kTmemCols = 512;
 constexpr int SUB = kWinT * 128;  // bytes of a [128 rows][64 columns] sub-tile
+// Half: P, at most one and over a window of thousands of keys mostly below 2^-14, where half loses bits, is computed 2^14 times as large
+// (half ends at 2^16); dV is scaled back at its end.  dS keeps its size: it follows dO, whose scale is the caller's.
+template <bool F16>
+constexpr float kShift = F16 ? 14.0f : 0.0f;
+template <bool F16>
+constexpr float kUnshift = F16 ? 1.0f / 16384.0f : 1.0f;
 
 struct BwdParams {
     WindowGeom g;
     float scale, scale_log2;
     int n_pad;             // N rounded up to whole tiles
-    const float* neg_lse2;   // [batch * heads][n_pad]: -LSE in the exp2 domain (-inf for rows that see nothing: their P is zero)
-    const float* neg_delta;  // -D
+    const float* neg_lse2;   // [batch * heads][n_pad]: kShift - LSE in the exp2 domain (-inf for rows that see nothing: their P is zero)
+    const float* neg_delta;  // -D * kUnshift: what is multiplied with the larger P is that much smaller
     uint16_t* dQ;
     uint16_t* dK;
     uint16_t* dV;
@@ -145,8 +151,8 @@ __global__ void __launch_bounds__(256) window_delta_kernel(const WindowGeom g, c
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     sum += __shfl_xor_sync(0xffffffffu, sum, 4);
     if (l8 == 0 && row < n_pad) {
-        neg_delta[(long long)bh * n_pad + row] = -sum;
-        neg_lse2[(long long)bh * n_pad + row] = seen ? LSE[(long long)bh * g.N + row] * -1.4426950408889634f : -INFINITY;
+        neg_delta[(long long)bh * n_pad + row] = -sum * kUnshift<F16>;
+        neg_lse2[(long long)bh * n_pad + row] = seen ? fmaf(LSE[(long long)bh * g.N + row], -1.4426950408889634f, kShift<F16>) : -INFINITY;
     }
 }
 
@@ -337,7 +343,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     } else {
         const int x = warp >> 2, tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_dp = t_lane + (x ? C::kDP1 : C::kDP0);
-        const uint64_t c22 = pack_f32x2(p.scale_log2, p.scale_log2);
+        const uint64_t c22 = pack_f32x2(p.scale_log2, p.scale_log2), unshift2 = pack_f32x2(kUnshift<F16>, kUnshift<F16>);
         uint32_t g = 0, n_it = 0;
         bool ok = true, more = load_item(p, 0, it);
         auto row_value = [&](const float* v) { return __ldg(v + ((long long)it.b * p.g.heads + it.h) * p.n_pad + it.row0 + tw); };
@@ -383,7 +389,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
                         float u, v;
-                        unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), nd2),
+                        unpack_f32x2(mul_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), unshift2, nd2),
                                                pack_f32x2(__uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]))), u, v);
                         d[e] = __float_as_uint(u);
                         d[e + 1] = __float_as_uint(v);
@@ -700,7 +706,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 tmem_ld32(t_s, r);
                 tmem_ld32(t_s + 32, r + 32);
                 tc_wait_ld();
-                const uint64_t c22 = pack_f32x2(c2, c2);
+                const uint64_t c22 = pack_f32x2(c2, c2), unshift2 = pack_f32x2(kUnshift<F16>, kUnshift<F16>);
                 uint32_t bits[2] = {0xffffffffu, 0xffffffffu};
                 if (!full) {
                     bits[0] = key_bits(p.g, seq, key, row0 + x * 64);
@@ -752,9 +758,9 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     for (int e = 0; e < 32; e += 4) {
                         const float4 l = del[c * 8 + e / 4];
                         float a0, a1, a2, a3;
-                        unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pack_f32x2(l.x, l.y)),
+                        unpack_f32x2(mul_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), unshift2, pack_f32x2(l.x, l.y)),
                                                pack_f32x2(__uint_as_float(r[c * 32 + e]), __uint_as_float(r[c * 32 + e + 1]))), a0, a1);
-                        unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])), pack_f32x2(l.z, l.w)),
+                        unpack_f32x2(mul_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])), unshift2, pack_f32x2(l.z, l.w)),
                                                pack_f32x2(__uint_as_float(r[c * 32 + e + 2]), __uint_as_float(r[c * 32 + e + 3]))), a2, a3);
                         d[e] = __float_as_uint(a0);
                         d[e + 1] = __float_as_uint(a1);
@@ -801,7 +807,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             } else {
                 uint16_t* out = x ? p.dK + (long long)it.b * p.k_batch + (long long)it.hk * p.k_head + (long long)key * p.k_row
                                   : p.dV + (long long)it.b * p.v_batch + (long long)it.hk * p.v_head + (long long)key * p.v_row;
-                store_row<F16>(t_acc, 0, D / 32, x ? p.scale : 1.f, n == 0, key < p.g.N_kv ? out : nullptr, x ? p.wide_k : p.wide_v);
+                store_row<F16>(t_acc, 0, D / 32, x ? p.scale : kUnshift<F16>, n == 0, key < p.g.N_kv ? out : nullptr, x ? p.wide_k : p.wide_v);
             }
             if (n > 0) {
                 tc_fence_before();
@@ -832,7 +838,7 @@ __global__ void __launch_bounds__(256) window_sink_sum_kernel(const __grid_const
         s[0] += a.x; s[1] += a.y; s[2] += a.z; s[3] += a.w;
         s[4] += c.x; s[5] += c.y; s[6] += c.z; s[7] += c.w;
     }
-    const float f = which ? p.scale : 1.f;
+    const float f = which ? p.scale : kUnshift<F16>;
     uint16_t* out = which ? p.dK + (long long)b * p.k_batch + (long long)hk * p.k_head + (long long)key * p.k_row
                           : p.dV + (long long)b * p.v_batch + (long long)hk * p.v_head + (long long)key * p.v_row;
     *reinterpret_cast<uint4*>(out + col) = make_uint4(pack_16x2<F16>(s[0] * f, s[1] * f), pack_16x2<F16>(s[2] * f, s[3] * f),

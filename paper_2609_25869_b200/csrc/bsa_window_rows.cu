@@ -29,6 +29,9 @@ constexpr int kSlot = 4096;
 constexpr int kSlots = kRing / kSlot;
 constexpr int kMaxCluster = 8;
 constexpr unsigned kAll = 0xffffffffu;
+// Half: P, at most one, is computed 2^15 times as large (half ends at 2^16), so that less of it falls below 2^-14.
+template <bool F16>
+constexpr float kShift = F16 ? 15.0f : 0.0f;
 
 struct RowsParams {
     WindowGeom g;
@@ -198,7 +201,7 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                 o[n][3] *= a_hi;
             }
         }
-        const float nm_lo = (m_lo == -INFINITY) ? 0.f : -m_lo, nm_hi = (m_hi == -INFINITY) ? 0.f : -m_hi;
+        const float nm_lo = (m_lo == -INFINITY) ? 0.f : kShift<F16> - m_lo, nm_hi = (m_hi == -INFINITY) ? 0.f : kShift<F16> - m_hi;
         uint32_t pa[KS_PV][4];  // P as the A operand of P V
 #pragma unroll
         for (int n = 0; n < NT_S; ++n) {
@@ -305,7 +308,7 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             const float inv = any ? 1.f / L : 0.f;
             *reinterpret_cast<uint32_t*>(p.O + (long long)b * p.o_batch + (long long)h * p.o_head + (long long)n * p.o_row + c) =
                 any ? pack_16x2<F16>(v0 * inv, v1 * inv) : 0u;
-            if (c == 0) p.LSE[((long long)b * p.g.heads + h) * p.g.N + n] = any ? fmaf(M, 0.6931471805599453f, logf(L)) : -INFINITY;
+            if (c == 0) p.LSE[((long long)b * p.g.heads + h) * p.g.N + n] = any ? fmaf(M - kShift<F16>, 0.6931471805599453f, logf(L)) : -INFINITY;
         }
     }
     if (threadIdx.x == 0 && abort_flag) atomicExch(p.status, (int)BSA_ERR_DEVICE_TIMEOUT);

@@ -376,56 +376,59 @@ _VIEW = struct.Struct("@Pqqq")                       # bsa_view_t
 _ROPE = struct.Struct("@4iq2i4i4idPPqq4i4i")         # bsa_rope_desc_t
 _WINDOW = struct.Struct("@4iqqqqqifPP")              # bsa_window_desc_t
 PAIRS = {"interleaved": 0, "halves": 1}  # BSA_PAIRS_*
+_PAD = ((0, 0, 0, 0), (0, 0, 0), (0, 0), (0,), ())  # of an array of BSA_MAX_AXES entries behind so many given ones
+_torch = None      # the module and its two element types, once a call has needed them
 _DTYPE_IDS: Dict = {}
 
 
-def _dtype_id(t, what: str) -> int:
-    if not _DTYPE_IDS:
+def _tensor_of(t, what: str):
+    """(type id, device index) of a call's first tensor."""
+    global _torch
+    if _torch is None:
         import torch
         _DTYPE_IDS.update({torch.bfloat16: 0, torch.float16: 1})
-    if not t.is_cuda or t.dtype not in _DTYPE_IDS:
+        _torch = torch
+    dt, dev = _DTYPE_IDS.get(t.dtype), t.get_device()
+    if dt is None or dev < 0:
         raise ValueError(f"{what} has to be a bf16 or fp16 CUDA tensor")
-    return _DTYPE_IDS[t.dtype]
+    return dt, dev
 
 
-def _view(t, nhd: bool, like, what: str):
+def _view(t, nhd: bool, dtype, dev: int, what: str):
     """(batch, heads, rows, d, packed bsa_view_t) of ``[heads, rows, d]`` / ``[batch, heads, rows, d]``, or of
-    ``[rows, heads, d]`` / ``[batch, rows, heads, d]`` with ``nhd``; of the type and on the device of ``like``."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 3:
+    ``[rows, heads, d]`` / ``[batch, rows, heads, d]`` with ``nhd``."""
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what} has to have the type and the device of Q")
+    shape = t.shape
+    if len(shape) == 4:
+        b, h, n, d = shape
+        sb, sh, sn, sd = t.stride()
+    elif len(shape) == 3:
         b, sb = 1, 0
         h, n, d = shape
-        sh, sn, sd = stride
-    elif len(shape) == 4:
-        b, h, n, d = shape
-        sb, sh, sn, sd = stride
+        sh, sn, sd = t.stride()
     else:
         raise ValueError(f"{what} has to have three or four dimensions")
-    if nhd:
-        h, n, sh, sn = n, h, sn, sh
-    if like is not None and (t.dtype is not like.dtype or t.device != like.device):
-        raise ValueError(f"{what} has to have the type and the device of Q")
     if sd != 1 and d > 1:
         raise ValueError(f"{what} has to be contiguous in its last dimension")
+    if nhd:
+        return b, n, h, d, _VIEW.pack(t.data_ptr(), sb, sn, sh)
     return b, h, n, d, _VIEW.pack(t.data_ptr(), sb, sh, sn)
 
 
-def _int32_ptr(t, shape, device, what: str) -> int:
-    import torch
-    if t is None:
-        return 0
-    if t.dtype is not torch.int32 or t.device != device or tuple(t.shape) not in shape or not t.is_contiguous():
-        raise ValueError(f"{what} has to be a contiguous int32 tensor {' or '.join(map(str, shape))} on the device of Q")
+def _int32_ptr(t, shapes, dev: int, what: str) -> int:
+    if t.dtype is not _torch.int32 or t.get_device() != dev or tuple(t.shape) not in shapes or not t.is_contiguous():
+        raise ValueError(f"{what} has to be a contiguous int32 tensor {' or '.join(map(str, shapes))} on the device of Q")
     return t.data_ptr()
 
 
-def _on_device(device, call, stream):
-    """``call(stream pointer)`` with ``device`` current, on ``stream`` or the device's current stream."""
-    import torch
-    if device.index == torch.cuda.current_device():
-        return call(_stream_ptr(stream))
-    with torch.cuda.device(device):
-        return call(_stream_ptr(stream))
+def _on_device(dev: int, call, stream):
+    """``call(stream pointer)`` with device ``dev`` current, on ``stream`` or the device's current stream."""
+    if dev != _torch._C._cuda_getDevice():
+        with _torch.cuda.device(dev):
+            return call(_stream_ptr(stream))
+    # (the handle alone, as in _stream_ptr)
+    return call((_torch._C._cuda_getCurrentRawStream(dev) or None) if stream is None else _stream_ptr(stream))
 
 
 def rope(Q, K=None, *, axes, positions=None, grid=None, first: int = 0, origin=None, theta: float = 10000.0, freq=None,
@@ -439,53 +442,62 @@ def rope(Q, K=None, *, axes, positions=None, grid=None, first: int = 0, origin=N
     ``first`` on stand on it row-major, ``origin`` added, and the others stay as they are.  ``freq``: the pairs' own
     frequencies instead of ``theta``'s.  ``inverse=True`` is the way back: gradients, or positions taken off.
     ``out``: the tensors to write (``(Q, K)`` themselves for in place), e.g. views of a cache."""
-    import torch
     nhd = LAYOUTS[layout] == 1
-    dt = _dtype_id(Q, "Q")
-    b, h, n, d, vq = _view(Q, nhd, None, "Q")
+    dt, dev = _tensor_of(Q, "Q")
+    dtype = Q.dtype
+    b, h, n, d, vq = _view(Q, nhd, dtype, dev, "Q")
     if out is None:
-        oq, ok = torch.empty_like(Q), None if K is None else torch.empty_like(K)
+        oq, ok = _torch.empty_like(Q), None if K is None else _torch.empty_like(K)
     else:
         oq, ok = (out, None) if K is None else out
         if oq.shape != Q.shape or (K is not None and ok.shape != K.shape):
             raise ValueError("out has to have the shapes of Q and K")
-    voq = _view(oq, nhd, Q, "out")[4]
+    voq = _view(oq, nhd, dtype, dev, "out")[4]
     hk, vk, vok = 0, None, None
     if K is not None:
-        bk, hk, nk, dk, vk = _view(K, nhd, Q, "K")
-        if (bk, nk, dk) != (b, n, d):
+        bk, hk, nk, dk, vk = _view(K, nhd, dtype, dev, "K")
+        if bk != b or nk != n or dk != d:
             raise ValueError("Q and K have to agree in batch, tokens and channels")
-        vok = _view(ok, nhd, Q, "out")[4]
+        vok = _view(ok, nhd, dtype, dev, "out")[4]
     na = len(axes)
     if not 1 <= na <= 4 or (positions is None) == (grid is None):
         raise ValueError("one to four axes, and either positions or a grid")
-    if grid is not None and (len(grid) != na or (origin is not None and len(origin) != na)):
-        raise ValueError("grid and origin have one entry per axis")
-    pos = _int32_ptr(positions, ((n, na), (1, n, na), (b, n, na)), Q.device, "positions")
-    per_batch = n * na if positions is not None and positions.dim() == 3 and positions.shape[0] > 1 else 0
-    freqs = None if freq is None else (ctypes.c_double * len(freq))(*freq)
-    if freq is not None and 2 * len(freq) != sum(axes):
-        raise ValueError("freq has one entry per pair of channels")
-    pad = (0,) * (4 - na)
+    pad = _PAD[na]
+    if grid is not None:
+        if len(grid) != na or (origin is not None and len(origin) != na):
+            raise ValueError("grid and origin have one entry per axis")
+        pos = per_batch = 0
+        where = (*grid, *pad, *origin, *pad) if origin is not None else (*grid, *pad, 0, 0, 0, 0)
+    else:
+        pos = _int32_ptr(positions, ((n, na), (1, n, na), (b, n, na)), dev, "positions")
+        per_batch = n * na if positions.dim() == 3 and positions.shape[0] > 1 else 0
+        where = (0, 0, 0, 0, 0, 0, 0, 0)
+    freqs = None
+    if freq is not None:
+        if 2 * len(freq) != sum(axes):
+            raise ValueError("freq has one entry per pair of channels")
+        freqs = (ctypes.c_double * len(freq))(*freq)
     desc = _ROPE.pack(b, h, hk, d, n, dt, na, *axes, *pad, PAIRS[pairs], shared_freq, inverse, 0, theta,
-                      0 if freqs is None else ctypes.addressof(freqs), pos, per_batch, first,
-                      *(grid or (0,) * na), *pad, *(origin or (0,) * na), *pad)
-    _check(_on_device(Q.device, lambda st: lib().bsa_rope(desc, vq, vk, voq, vok, st), stream), "bsa_rope")
+                      0 if freqs is None else ctypes.addressof(freqs), pos, per_batch, first, *where)
+    status = _on_device(dev, lambda st: lib().bsa_rope(desc, vq, vk, voq, vok, st), stream)
+    if status:
+        _check(status, "bsa_rope")
     return oq if K is None else (oq, ok)
 
 
-def _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, layout):
-    """(packed bsa_window_desc_t, packed views of Q, K, V, shape of LSE): what forward and backward check alike."""
-    nhd = LAYOUTS[layout] == 1
-    dt = _dtype_id(Q, "Q")
-    b, h, n, d, vq = _view(Q, nhd, None, "Q")
-    bk, hk, nk, dk, vk = _view(K, nhd, Q, "K")
-    if V.shape != K.shape or bk != b or dk != d or Q.dim() != K.dim():
+def _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, nhd):
+    """(packed bsa_window_desc_t, packed views of Q, K, V, shape of LSE, device): what forward and backward check alike."""
+    dt, dev = _tensor_of(Q, "Q")
+    dtype = Q.dtype
+    b, h, n, d, vq = _view(Q, nhd, dtype, dev, "Q")
+    bk, hk, nk, dk, vk = _view(K, nhd, dtype, dev, "K")
+    if V.shape != K.shape or bk != b or dk != d or len(Q.shape) != len(K.shape):
         raise ValueError("K and V have to have one shape, and batch and channels of Q")
-    vv = _view(V, nhd, Q, "V")[4]
-    desc = _WINDOW.pack(b, h, hk, d, n, nk, left, right, sinks, dt, scale, _int32_ptr(q_start, ((b,),), Q.device, "q_start"),
-                        _int32_ptr(kv_len, ((b,),), Q.device, "kv_len"))
-    return desc, vq, vk, vv, ((b, h, n) if Q.dim() == 4 else (h, n))
+    vv = _view(V, nhd, dtype, dev, "V")[4]
+    desc = _WINDOW.pack(b, h, hk, d, n, nk, left, right, sinks, dt, scale,
+                        0 if q_start is None else _int32_ptr(q_start, ((b,),), dev, "q_start"),
+                        0 if kv_len is None else _int32_ptr(kv_len, ((b,),), dev, "kv_len"))
+    return desc, vq, vk, vv, ((b, h, n) if len(Q.shape) == 4 else (h, n)), dev
 
 
 def window_forward(Q, K, V, *, left: int, right: int = 0, sinks: int = 0, q_start=None, kv_len=None, scale: float = 0.0,
@@ -497,20 +509,26 @@ def window_forward(Q, K, V, *, left: int, right: int = 0, sinks: int = 0, q_star
     (``layout="nhd"``: heads behind tokens); any strides that are multiples of 8 elements.  ``q_start``, ``kv_len``: int32
     CUDA tensors ``[batch]``, each sequence's first query position and its number of keys (default: the queries are the last N
     of N_kv positions).  LSE is fp32 ``[batch, heads, N]`` (``[heads, N]``) in either layout."""
-    import torch
-    desc, vq, vk, vv, shape = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, layout)
+    nhd = LAYOUTS[layout] == 1
+    desc, vq, vk, vv, shape, dev = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, nhd)
     if O is None:
-        O = torch.empty_like(Q)
+        O = _torch.empty_like(Q)
     elif O.shape != Q.shape:
         raise ValueError("O has to have the shape of Q")
     if LSE is None:
-        LSE = Q.new_empty(shape, dtype=torch.float32)
-    elif tuple(LSE.shape) != shape or LSE.dtype is not torch.float32 or LSE.device != Q.device or not LSE.is_contiguous():
-        raise ValueError(f"LSE has to be a contiguous fp32 tensor {shape} on the device of Q")
-    vo = _view(O, LAYOUTS[layout] == 1, Q, "O")[4]
-    _check(_on_device(Q.device, lambda st: lib().bsa_window_forward(desc, vq, vk, vv, vo, LSE.data_ptr(), st), stream),
-           "bsa_window_forward")
+        LSE = Q.new_empty(shape, dtype=_torch.float32)
+    else:
+        _check_lse(LSE, shape, dev)
+    vo = _view(O, nhd, Q.dtype, dev, "O")[4]
+    status = _on_device(dev, lambda st: lib().bsa_window_forward(desc, vq, vk, vv, vo, LSE.data_ptr(), st), stream)
+    if status:
+        _check(status, "bsa_window_forward")
     return O, LSE
+
+
+def _check_lse(LSE, shape, dev: int):
+    if tuple(LSE.shape) != shape or LSE.dtype is not _torch.float32 or LSE.get_device() != dev or not LSE.is_contiguous():
+        raise ValueError(f"LSE has to be a contiguous fp32 tensor {shape} on the device of Q")
 
 
 def window_backward(Q, K, V, O, LSE, dO, *, left: int, right: int = 0, sinks: int = 0, q_start=None, kv_len=None,
@@ -518,25 +536,22 @@ def window_backward(Q, K, V, O, LSE, dO, *, left: int, right: int = 0, sinks: in
     """``bsa_window_backward``: ``(dQ, dK, dV)`` of ``window_forward`` from its inputs, its outputs and the gradient ``dO`` of
     ``O``; arguments as there.  dK and dV are summed over the query heads that share a key head.  The workspace comes from
     torch's allocator on the current stream; with ``stream`` given, that one has to be the tensors' as torch knows it."""
-    import torch
-    desc, vq, vk, vv, shape = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, layout)
     nhd = LAYOUTS[layout] == 1
+    desc, vq, vk, vv, shape, dev = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, nhd)
     if O.shape != Q.shape or dO.shape != Q.shape:
         raise ValueError("O and dO have to have the shape of Q")
-    if tuple(LSE.shape) != shape or LSE.dtype is not torch.float32 or LSE.device != Q.device or not LSE.is_contiguous():
-        raise ValueError(f"LSE has to be a contiguous fp32 tensor {shape} on the device of Q")
-    dQ = torch.empty_like(Q) if dQ is None else dQ
-    dK = torch.empty_like(K) if dK is None else dK
-    dV = torch.empty_like(V) if dV is None else dV
+    _check_lse(LSE, shape, dev)
+    empty = _torch.empty_like
+    dQ, dK, dV = empty(Q) if dQ is None else dQ, empty(K) if dK is None else dK, empty(V) if dV is None else dV
     if dQ.shape != Q.shape or dK.shape != K.shape or dV.shape != K.shape:
         raise ValueError("gradients have to have the shapes of their tensors")
-    views = [_view(t, nhd, Q, n)[4] for t, n in ((O, "O"), (dO, "dO"), (dQ, "dQ"), (dK, "dK"), (dV, "dV"))]
+    views = [_view(t, nhd, Q.dtype, dev, n)[4] for t, n in ((O, "O"), (dO, "dO"), (dQ, "dQ"), (dK, "dK"), (dV, "dV"))]
 
     def call(st):
         n = lib().bsa_window_workspace_bytes(desc)
-        ws = torch.empty(n, dtype=torch.uint8, device=Q.device)
+        ws = _torch.empty(n, dtype=_torch.uint8, device=Q.device)
         return lib().bsa_window_backward(desc, vq, vk, vv, views[0], LSE.data_ptr(), *views[1:], ws.data_ptr(), n, st)
-    _check(_on_device(Q.device, call, stream), "bsa_window_backward")
+    _check(_on_device(dev, call, stream), "bsa_window_backward")
     return dQ, dK, dV
 
 

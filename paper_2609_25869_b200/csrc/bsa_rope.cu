@@ -254,8 +254,8 @@ extern "C" bsa_status_t bsa_rope(const bsa_rope_desc_t* t, const bsa_view_t* Q, 
             if (t->freq_host) f = (long double)t->freq_host[pair];
             if (!isfinite(f)) return BSA_ERR_INVALID_ARG;
             long double turns = f * 0.159154943091895335768883763372514362L;
-            turns -= floorl(turns);  // whole turns change nothing at whole positions
-            const long double units = roundl(turns * 18446744073709551616.0L);
+            if (!(turns >= 0.0L && turns < 1.0L)) turns -= floorl(turns);  // whole turns change nothing at whole positions
+            const long double units = turns * 18446744073709551616.0L + 0.5L;
             p.freq[pair] = units >= 18446744073709551616.0L ? 0ull : (unsigned long long)units;
             p.axis[pair] = (unsigned char)a;
         }

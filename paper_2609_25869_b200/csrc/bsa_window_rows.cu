@@ -52,9 +52,9 @@ __device__ __forceinline__ uint32_t map_to_rank(uint32_t smem, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float2 ld_cluster(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
     return v;
 }
 
@@ -66,7 +66,7 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[kWarps][2 * kSlots];  // K slots, then V slots: the copy has landed
     __shared__ float wm[kWarps][kRows], wl[kWarps][kRows];      // the warps' maxima (log2 domain) and sums
-    __shared__ float cm[kRows], cl[kRows];                      // the CTA's
+    __shared__ __align__(8) float2 cml[kRows];                  // the CTA's
     __shared__ uint32_t abort_flag;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, t = lane & 3;
     const int C = gridDim.x, rank = blockIdx.x;
@@ -75,6 +75,8 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     const uint32_t bK = smem_u32(&bars[warp][0]), bV = bK + kSlots * 8;
     if (threadIdx.x == 0) abort_flag = 0;
     if (lane == 0) {
+        prefetch_tensormap(&tmK);
+        prefetch_tensormap(&tmV);
         for (int i = 0; i < 2 * kSlots; ++i) mbar_init(bK + i * 8, 1);
         fence_mbar_init();
     }
@@ -267,8 +269,7 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         float M = -INFINITY, L = 0.f;
         for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w][r]);
         for (int w = 0; w < kWarps; ++w) L += wm[w][r] == -INFINITY ? 0.f : wl[w][r] * ex2_approx(wm[w][r] - M);
-        cm[r] = M;
-        cl[r] = L;
+        cml[r] = make_float2(M, L);
     }
     __syncthreads();
     float* sum = reinterpret_cast<float*>(smem);  // the CTA's rows, in the place of warp 0's
@@ -281,24 +282,25 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     // ---- join the CTAs of the cluster; each writes its share of the outputs ----
     if (C > 1) cluster_sync(); else __syncthreads();
     const int per = kRows * D / C;  // (C divides it)
-    const uint32_t a_sum = smem_u32(sum), a_cm = smem_u32(cm), a_cl = smem_u32(cl);
+    const uint32_t a_sum = smem_u32(sum), a_ml = smem_u32(cml);
     for (int i = rank * per + 2 * threadIdx.x; i < (rank + 1) * per; i += 2 * kWarps * 32) {
         const int r = i / D, c = (i - r * D) ^ ((r & 7) << 3);  // element i of the stored order is column c
-        float mr[kMaxCluster], M = -INFINITY;
+        float2 ml[kMaxCluster], v[kMaxCluster];
 #pragma unroll
-        for (int q = 0; q < kMaxCluster; ++q) {
-            mr[q] = q < C ? ld_cluster(map_to_rank(a_cm + r * 4, q)) : -INFINITY;
-            M = fmaxf(M, mr[q]);
+        for (int q = 0; q < kMaxCluster; ++q) {  // all loads on their way before the first is used (ranks beyond C: this one again)
+            const uint32_t from = q < C ? q : rank;
+            ml[q] = ld_cluster(map_to_rank(a_ml + r * 8, from));
+            v[q] = ld_cluster(map_to_rank(a_sum + i * 4, from));
         }
-        float L = 0.f, v0 = 0.f, v1 = 0.f;
+        float M = -INFINITY, L = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) M = fmaxf(M, ml[q].x);
 #pragma unroll
         for (int q = 0; q < kMaxCluster; ++q) {
-            if (q >= C || mr[q] == -INFINITY) continue;
-            const float f = ex2_approx(mr[q] - M);
-            L = fmaf(f, ld_cluster(map_to_rank(a_cl + r * 4, q)), L);
-            const uint32_t src = map_to_rank(a_sum + i * 4, q);
-            v0 = fmaf(f, ld_cluster(src), v0);
-            v1 = fmaf(f, ld_cluster(src + 4), v1);
+            const float f = (q >= C || ml[q].x == -INFINITY) ? 0.f : ex2_approx(ml[q].x - M);
+            L = fmaf(f, ml[q].y, L);
+            v0 = fmaf(f, v[q].x, v0);
+            v1 = fmaf(f, v[q].y, v1);
         }
         const int row = row0 + r;
         if (row < p.n_rows) {

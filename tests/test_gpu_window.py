@@ -345,8 +345,8 @@ def test_refusals():
     desc = bsa._WINDOW.pack(2, 4, 2, 64, 100, 200, 5, 0, 0, 0, 0.0, 0, 0)
     need = bsa.lib().bsa_window_workspace_bytes(desc)
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-    vs = [bsa._view(t, False, q, "")[4] for t in (q, k, v, O)]
-    gs = [bsa._view(t, False, q, "")[4] for t in (g, torch.empty_like(q), torch.empty_like(k), torch.empty_like(v))]
+    vs = [bsa._view(t, False, q.dtype, 0, "")[4] for t in (q, k, v, O)]
+    gs = [bsa._view(t, False, q.dtype, 0, "")[4] for t in (g, torch.empty_like(q), torch.empty_like(k), torch.empty_like(v))]
     call = lambda p, n: bsa.lib().bsa_window_backward(desc, *vs, L.data_ptr(), *gs, p, n, None)  # noqa: E731
     assert call(ws.data_ptr(), need - 1) == 1 and call(None, need) == 1 and call(ws.data_ptr() + 4, need) == 1
     assert call(ws.data_ptr(), need) == 0

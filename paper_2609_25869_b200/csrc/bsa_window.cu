@@ -7,7 +7,7 @@
 // row's columns are applied only in tiles that some row does not see whole.
 //   warps 0-3 / 4-7 : softmax warpgroups (thread = row); tile t belongs to warpgroup t mod 2, and S and P buffer t mod 2 with it
 //   warp 8 : Q and K producer   warp 9 : Q K^T issuer   warp 10 : P V issuer   warp 11 : V producer
-//   warps 12-15 : references: each row's running maximum, the accumulator's rescaling, and the epilogue
+//   warps 12-15 : references: each row's running maximum, the tiles' edges, the accumulator's rescaling, and the epilogue
 // Work per tile: 4 * 128 * 128 * d flops (1024 clk at d = 128) and 128 * 128 exponentials (1024 clk at 16 per clk and SM): at
 // d = 128 the tensor pipe and the special-function unit bind together, at d = 64 the latter alone.  A warpgroup takes longer
 // than that over a tile (latencies), so two must run at once and neither may wait: S and P have their own columns, Q K^T runs
@@ -52,10 +52,10 @@ struct Params {
     uint16_t* O;
     long long o_batch, o_head, o_row;
     float* LSE;
+    int o_wide;        // rows of O lie on 32-byte boundaries
     float scale_log2;  // scale * log2(e)
-    Divisor qt, heads, bh, group;  // 128-row tiles of a sequence, heads, batch x heads, heads that share a key head
-    int n_items;
-    int longest_first; // no left limit: later tiles are longer
+    ItemOrder order;       // 128-row tiles, from a sequence's last to its first
+    Divisor heads, group;  // heads; heads that share a key head
 };
 
 struct __align__(8) Barriers {
@@ -76,14 +76,9 @@ struct Item {
 __device__ __forceinline__ bool load_item(const Params& p, int k, Item& it) {
     const int G = gridDim.x;
     const int idx = k * G + ((k & 1) ? (G - 1 - (int)blockIdx.x) : (int)blockIdx.x);
-    if (idx >= p.n_items) return false;
-    int bh, qt;
-    if (p.longest_first) {
-        qt = (int)p.qt.d - 1 - p.bh.div(idx, bh);
-    } else {
-        bh = p.qt.div(idx, qt);
-    }
-    int rest;
+    if (idx >= p.order.n_items) return false;
+    int tile, rest;
+    const int bh = p.order.row_of(idx, tile), qt = p.order.n_tiles - 1 - tile;
     it.b = p.heads.div(bh, it.h);
     it.hk = p.group.div(it.h, rest);
     it.row0 = qt * kWinT;
@@ -120,11 +115,11 @@ struct Ring {
     }
 };
 
-// P in the place of the scores: exp2(s * c2 + neg_m), rounded and packed by pairs; its unrounded sum.
+// P of 32 keys in the place of their scores: exp2(s * c2 + neg_m), rounded and packed by pairs; its unrounded sum.
 template <bool F16>
-__device__ __forceinline__ void exp_keys(uint32_t (&r)[kWinT], uint64_t c22, uint64_t neg_m2, uint64_t& sum01, uint64_t& sum23) {
+__device__ __forceinline__ void exp_keys(uint32_t* r, uint64_t c22, uint64_t neg_m2, uint64_t& sum01, uint64_t& sum23) {
 #pragma unroll
-    for (int i = 0; i < kWinT; i += 4) {
+    for (int i = 0; i < 32; i += 4) {
         float x0, x1, x2, x3;
         unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), c22, neg_m2), x0, x1);
         unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), c22, neg_m2), x2, x3);
@@ -197,25 +192,33 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
 
     if (warp >= 12) {
         // =========================== references and epilogue ===========================
-        reg_dec<80>();
+        reg_dec<96>();
         const int tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_lane + C::kO;
         const float c2 = p.scale_log2;
         uint32_t n_it = 0, g = 0;  // items finished (with tiles), tiles in front of the item
-        // The reference of tile j of an item (running index t), from `m` of the tile before.
-        auto reference = [&](const Item& w, int j, uint32_t t, float& m) -> bool {
-            const uint32_t x = t & 1;
+        // The reference of tile j of an item (running index t) follows from `m`, that of the tile before, and its scores.  Where rows do
+        // not see the whole tile, this warpgroup writes the scores back with the hidden ones at -inf: the softmax warpgroups, whose loop is
+        // the kernel's bottleneck, have no edges.  Returns whether any row of the warp has moved to a new reference (m_old: the one before).
+        auto find = [&](const Item& w, int j, uint32_t t, float& m, float& m_old, bool& moved) -> bool {
+            const uint32_t t_s = t_lane + ((t & 1) ? C::kS1 : C::kS0);
             const int key0 = w.tiles.tile(j) * kWinT;
             const bool full = tile_is_full(p.g, w.range, key0);
-            if (!mbar_wait_warp(smem_u32(&bars.s_full[x]), (t >> 1) & 1, abortp)) return false;
+            if (!mbar_wait_warp(smem_u32(&bars.s_full[t & 1]), (t >> 1) & 1, abortp)) return false;
             tc_fence_after();
             float m0 = -INFINITY, m1 = m0, m2 = m0, m3 = m0;
 #pragma unroll 1
             for (int c = 0; c < kWinT / 32; ++c) {
                 uint32_t r[32];
-                tmem_ld32(t_lane + (x ? C::kS1 : C::kS0) + c * 32, r);
+                tmem_ld32(t_s + c * 32, r);
                 tc_wait_ld();
-                if (!full) hide(r, row_bits(p.g, w.seq, w.seq.start + w.row0 + tw, key0 + c * 32));
+                if (!full) {
+                    const uint32_t bits = row_bits(p.g, w.seq, w.seq.start + w.row0 + tw, key0 + c * 32);
+                    if (!__all_sync(0xffffffffu, bits == 0xffffffffu)) {
+                        hide(r, bits);
+                        tmem_st32(t_s + c * 32, r);
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
                     m0 = max3(m0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
@@ -224,14 +227,25 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     m3 = max3(m3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
                 }
             }
+            if (!full) {
+                if (w.range.hi - key0 < kWinT || w.range.lo - key0 > max(p.g.sinks - key0, 0)) {  // some keys are seen by no row
+                    if (!mbar_wait_warp(smem_u32(&bars.v_full[t % C::kV]), (t / C::kV) & 1, abortp)) return false;
+                    zero_unseen_keys<D>(sV + (t % C::kV) * C::kTile, p.g, w.range, key0, tw);
+                    fence_proxy_async_smem();
+                }
+                tc_wait_st();
+            }
             const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * c2;
-            const float m_old = m;
+            m_old = m;
             if (mx > m + kRescale) m = mx;
-            const bool moved = m != m_old && m_old != -INFINITY;
-            if (j > 0 && __any_sync(0xffffffffu, moved)) {  // the accumulator follows, once all products before are in it
-                if (!mbar_wait_warp(smem_u32(&bars.pv_done[x ^ 1]), ((t - 1) >> 1) & 1, abortp)) return false;
+            moved = j > 0 && __any_sync(0xffffffffu, m != m_old && m_old != -INFINITY);
+            return true;
+        };
+        auto publish = [&](uint32_t t, float m, float m_old, bool moved) -> bool {
+            if (moved) {  // the accumulator follows, once all products before are in it
+                if (!mbar_wait_warp(smem_u32(&bars.pv_done[(t & 1) ^ 1]), ((t - 1) >> 1) & 1, abortp)) return false;
                 tc_fence_after();
-                const float alpha = moved ? ex2_approx(m_old - m) : 1.f;
+                const float alpha = (m != m_old && m_old != -INFINITY) ? ex2_approx(m_old - m) : 1.f;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
@@ -243,12 +257,13 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 }
                 tc_wait_st();
             }
-            mref[x][tw] = m;
+            mref[t & 1][tw] = m;
             tc_fence_before();
-            mbar_arrive(smem_u32(&bars.ref_ready[x]));
+            mbar_arrive(smem_u32(&bars.ref_ready[t & 1]));
             return true;
         };
-        bool more = load_item(p, 0, it), ok = true, begun = false;  // begun: this item's first reference is out
+        bool more = load_item(p, 0, it), ok = true;
+        int done = 0;  // of this item's tiles: references that are out
         float m = -INFINITY;
         for (int k = 0; more; ++k) {
             const Item w = it;
@@ -259,25 +274,37 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             uint16_t* orow = p.O + (long long)w.b * p.o_batch + (long long)w.h * p.o_head + (long long)row * p.o_row;
             float* lse_out = p.LSE + ((long long)w.b * p.g.heads + w.h) * p.g.N + row;
             const int n = w.tiles.count();
-            for (int j = begun ? 1 : 0; ok && j < n; ++j) ok = reference(w, j, g + j, m);
+            float m_old;
+            bool moved;
+            for (int j = done; ok && j < n; ++j) ok = find(w, j, g + j, m, m_old, moved) && publish(g + j, m, m_old, moved);
             if (!ok) break;
             g += (uint32_t)n;
             more = load_item(p, k + 1, it);
-            begun = false;
-            float m_next = -INFINITY;
+            done = 0;
             if (n == 0) {  // no row of the tile sees anything
                 if (row_ok) {
 #pragma unroll
                     for (int c = 0; c < D / 8; ++c) reinterpret_cast<uint4*>(orow)[c] = make_uint4(0, 0, 0, 0);
                     *lse_out = -INFINITY;
                 }
+                m = -INFINITY;
                 continue;
             }
-            // the next item's first tile comes before this item's end: one warpgroup has work until the accumulator is drained
-            if (more && it.tiles.count() > 0) {
-                ok = reference(it, 0, g, m_next);
+            // The next item's first two tiles come before this item's end, so that both warpgroups have work until the accumulator is
+            // drained; the second one's reference waits until then where it moves the accumulator.
+            const int n_next = more ? it.tiles.count() : 0;
+            float m_next = -INFINITY;
+            bool held = false;
+            if (n_next > 0) {
+                ok = find(it, 0, g, m_next, m_old, moved) && publish(g, m_next, m_old, moved);
+                done = 1;
+                if (ok && n_next > 1) {
+                    ok = find(it, 1, g + 1, m_next, m_old, moved);
+                    held = moved;
+                    if (ok && !held) ok = publish(g + 1, m_next, m_old, false);
+                    done = 2;
+                }
                 if (!ok) break;
-                begun = true;
             }
             if (!mbar_wait_warp(smem_u32(&bars.e_ready), n_it & 1, abortp)) break;
             const float l = lfin[0][tw] + lfin[1][tw];
@@ -300,15 +327,17 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 }
                 if (row_ok) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t v[4];
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t v[8];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            v[e] = seen ? pack_16x2<F16>(__uint_as_float(o[q * 8 + 2 * e]) * inv, __uint_as_float(o[q * 8 + 2 * e + 1]) * inv) : 0u;
-                        *reinterpret_cast<uint4*>(orow + c * 32 + q * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+                        for (int e = 0; e < 8; ++e)
+                            v[e] = seen ? pack_16x2<F16>(__uint_as_float(o[q * 16 + 2 * e]) * inv, __uint_as_float(o[q * 16 + 2 * e + 1]) * inv) : 0u;
+                        st_global_v8_or_2v4(orow + c * 32 + q * 16, v, p.o_wide);
                     }
                 }
+                __syncwarp();
             }
+            if (held && !publish(g + 1, m, m_old, true)) break;
         }
     } else if (warp >= 8) {
         reg_dec<48>();
@@ -422,7 +451,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         }
     } else {
         // =========================== softmax warpgroup x ===========================
-        reg_inc<192>();
+        reg_inc<184>();
         const int x = warp >> 2, tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t t_s = t_lane + (x ? C::kS1 : C::kS0), t_p = t_lane + (x ? C::kP1 : C::kP0);
@@ -434,12 +463,9 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         for (int k = 0; ok && load_item(p, k, it); ++k) {
             const int n = it.tiles.count();
             if (n == 0) continue;
-            const int pos = it.seq.start + it.row0 + tw;
             float m_ref = -INFINITY, l = 0.f;  // the reference of this warpgroup's last tile, and its sum in it
             for (int j = ((g & 1) == (uint32_t)x) ? 0 : 1; j < n; j += 2) {
                 const uint32_t t = g + j;
-                const int key0 = it.tiles.tile(j) * kWinT;
-                const bool full = tile_is_full(p.g, it.range, key0);
                 ok = mbar_wait_warp(b_ref, (t >> 1) & 1, abortp);  // (which is behind s_full)
                 if (!ok) break;
                 tc_fence_after();
@@ -450,17 +476,6 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 tc_wait_ld();
                 tc_fence_before();
                 mbar_arrive(smem_u32(&bars.s_free[x]));
-                if (!full) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) hide(r + c * 32, row_bits(p.g, it.seq, pos, key0 + c * 32));
-                    const int from = it.range.hi - key0, below = it.range.lo - key0;
-                    if (from < kWinT || (below > 0 && p.g.sinks - key0 < below)) {
-                        ok = mbar_wait_warp(smem_u32(&bars.v_full[t % C::kV]), (t / C::kV) & 1, abortp);
-                        if (!ok) break;
-                        zero_unseen_keys<D>(sV + (t % C::kV) * C::kTile, p.g, it.range, key0, tw);
-                        fence_proxy_async_smem();
-                    }
-                }
                 if (m_ref != m) {
                     l *= ex2_approx(m_ref - m);  // (m_ref = -inf: l is zero)
                     m_ref = m;
@@ -468,14 +483,17 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 const float neg_m = (m == -INFINITY) ? 0.f : kShift<F16> - m;
                 const uint64_t nm2 = pack_f32x2(neg_m, neg_m);
                 uint64_t sum01 = pack_f32x2(0.f, 0.f), sum23 = sum01;
-                exp_keys<F16>(r, c22, nm2, sum01, sum23);
                 if (t >= 2) {  // this warpgroup's last P has been read
                     ok = mbar_wait_warp(b_pv, ((t >> 1) - 1) & 1, abortp);
                     if (!ok) break;
                     tc_fence_after();
                 }
-                tmem_st32(t_p, r);
-                tmem_st32(t_p + 32, r + 32);
+                // stored 32 keys at a time, beside the next keys' exponentials (all at the end: 190 -> 174 us at 4 heads, the shape above)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    exp_keys<F16>(r + c * 32, c22, nm2, sum01, sum23);
+                    tmem_st16(t_p + c * 16, r + c * 32);
+                }
                 float s0, s1, s2, s3;
                 unpack_f32x2(sum01, s0, s1);
                 unpack_f32x2(sum23, s2, s3);
@@ -522,7 +540,7 @@ cudaError_t launch_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view
         if (e != cudaSuccess) return e;
         allowed[a.device].store(true, std::memory_order_relaxed);
     }
-    const int grid = a.num_sms < p.n_items ? a.num_sms : p.n_items;
+    const int grid = a.num_sms < p.order.n_items ? a.num_sms : p.order.n_items;
     kernel<<<grid, kThreads, Cfg<D>::kSmem, stream>>>(tq, tk, tv, p);
     count_launch();
     return cudaGetLastError();
@@ -537,6 +555,11 @@ cudaError_t window_status_word(int device, int** out) {
     const cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(out), g_window_status);
     if (e == cudaSuccess) word[device].store(*out, std::memory_order_release);
     return e;
+}
+
+bool view_is_wide(const bsa_view_t& v, int64_t batch, int64_t heads, int64_t rows) {
+    const auto on32 = [](int64_t n, int64_t stride) { return n == 1 || stride % 16 == 0; };
+    return (reinterpret_cast<uintptr_t>(v.data) & 31) == 0 && on32(batch, v.batch) && on32(heads, v.head) && on32(rows, v.row);
 }
 
 bsa_status_t window_args(const bsa_window_desc_t* t, WindowArgs* a) {
@@ -584,16 +607,13 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     p.O = static_cast<uint16_t*>(O->data);
     p.o_batch = O->batch; p.o_head = O->head; p.o_row = O->row;
     p.LSE = LSE;
+    p.o_wide = view_is_wide(*O, a.g.batch, a.g.heads, a.g.N);
     p.scale_log2 = a.scale * 1.4426950408889634f;
     const int n_qt = (a.g.N + kWinT - 1) / kWinT;
-    p.qt = Divisor(n_qt);
+    if ((int64_t)n_qt * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
+    p.order = ItemOrder(n_qt, cut_tiles(a.g, n_qt), a.g.batch * a.g.heads);
     p.heads = Divisor(a.g.heads);
-    p.bh = Divisor(a.g.batch * a.g.heads);
     p.group = Divisor(a.g.group);
-    const int64_t items = (int64_t)n_qt * a.g.batch * a.g.heads;
-    if (items > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
-    p.n_items = (int)items;
-    p.longest_first = a.g.left >= a.g.N_kv;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
     // Up to 32 rows per key head share their keys in one pass of the kernel for few rows.
     if ((int64_t)a.g.N * a.g.group <= 32) {

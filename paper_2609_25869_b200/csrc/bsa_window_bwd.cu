@@ -47,11 +47,10 @@ struct BwdParams {
     uint16_t* dK;
     uint16_t* dV;
     long long q_batch, q_head, q_row, k_batch, k_head, k_row, v_batch, v_head, v_row;  // strides of the gradients
-    int n_dq, n_dkv;       // items of the two kernels
-    int longest_first;
-    Divisor qt, heads, bh, heads_kv, group;  // query tiles of a sequence, heads, batch x heads, key heads, heads that share a key head
-    Divisor kt, bhk, shares, shared;        // key tiles of a sequence that are not cut into shares, batch x key heads, shares of a tile and of a
-                                            // sequence's tiles
+    ItemOrder dq, dkv;                 // query tiles from a sequence's last to its first; key tiles that are not cut into shares
+    int n_shared;                      // items in front of those: shares of the sinks' tiles
+    Divisor heads, heads_kv, group;    // heads; key heads; heads that share a key head
+    Divisor shares, shared;            // shares of a tile, of all of a sequence's tiles
     int sink_tiles, sink_shares;            // key tiles in front that are cut into shares (0: none)
     int wide_q, wide_k, wide_v;             // gradients whose rows lie on 32-byte boundaries
     float* partial;        // [batch * heads_kv][sink_tiles][sink_shares][dV, dK][128][D]
@@ -173,12 +172,9 @@ struct DqItem {
 };
 __device__ __forceinline__ bool load_item(const BwdParams& p, int k, DqItem& it) {
     const int idx = item_index(k);
-    if (idx >= p.n_dq) return false;
-    int bh, qt;
-    if (p.longest_first)
-        qt = (int)p.qt.d - 1 - p.bh.div(idx, bh);
-    else
-        bh = p.qt.div(idx, qt);
+    if (idx >= p.dq.n_items) return false;
+    int tile;
+    const int bh = p.dq.row_of(idx, tile), qt = p.dq.n_tiles - 1 - tile;
     it.b = p.heads.div(bh, it.h);
     int rest;
     it.hk = p.group.div(it.h, rest);
@@ -475,20 +471,15 @@ struct DkvItem {
 // Items: the shares of the sinks' tiles first (the longest), then the other tiles, a sequence's neighbours side by side.
 __device__ __forceinline__ bool load_item(const BwdParams& p, int k, DkvItem& it) {
     int idx = item_index(k);
-    if (idx >= p.n_dkv) return false;
-    const int n_shared = (int)p.bhk.d * p.sink_tiles * p.sink_shares;
-    if (idx < n_shared) {
+    if (idx >= p.n_shared + p.dkv.n_items) return false;
+    if (idx < p.n_shared) {
         it.bh = p.shared.div(idx, idx);
         it.kt = p.shares.div(idx, it.share);
         it.shares = p.sink_shares;
     } else {
-        idx -= n_shared;
         it.share = 0;
         it.shares = 1;
-        if (p.longest_first)  // the first keys are seen by the most rows
-            it.kt = p.bhk.div(idx, it.bh);
-        else
-            it.bh = p.kt.div(idx, it.kt);
+        it.bh = p.dkv.row_of(idx - p.n_shared, it.kt);  // (the last keys are seen by the fewest rows)
         it.kt += p.sink_tiles;
     }
     it.b = p.heads_kv.div(it.bh, it.hk);
@@ -897,8 +888,9 @@ cudaError_t launch(const WindowArgs& a, const Layout& l, const bsa_view_t& Q, co
     }
     window_delta_kernel<D, F16><<<dim3((unsigned)(l.n_pad / 32), (unsigned)(g.batch * g.heads)), 256, 0, stream>>>(
         g, static_cast<const uint16_t*>(O.data), static_cast<const uint16_t*>(G.data), O.batch, O.head, O.row, G.batch, G.head, G.row, LSE, lse2, delta, l.n_pad);
-    dq<<<p.n_dq < a.num_sms ? p.n_dq : a.num_sms, kThreads, DqCfg<D>::kSmem, stream>>>(tq, tk, tv, tg, p);
-    dkv<<<p.n_dkv < a.num_sms ? p.n_dkv : a.num_sms, kThreads, DkvCfg<D>::kSmem, stream>>>(tq, tk, tv, tg, p);
+    const int n_dkv = p.n_shared + p.dkv.n_items;
+    dq<<<p.dq.n_items < a.num_sms ? p.dq.n_items : a.num_sms, kThreads, DqCfg<D>::kSmem, stream>>>(tq, tk, tv, tg, p);
+    dkv<<<n_dkv < a.num_sms ? n_dkv : a.num_sms, kThreads, DkvCfg<D>::kSmem, stream>>>(tq, tk, tv, tg, p);
     count_launch(3);
     if (l.sink_tiles) {
         window_sink_sum_kernel<D, F16><<<dim3((unsigned)(l.sink_tiles * kWinT * D / 8 / 256), (unsigned)(g.batch * g.heads_kv), 2), 256, 0, stream>>>(p);
@@ -949,25 +941,18 @@ extern "C" bsa_status_t bsa_window_backward(const bsa_window_desc_t* t, const bs
     p.q_batch = dQ->batch; p.q_head = dQ->head; p.q_row = dQ->row;
     p.k_batch = dK->batch; p.k_head = dK->head; p.k_row = dK->row;
     p.v_batch = dV->batch; p.v_head = dV->head; p.v_row = dV->row;
-    p.n_dq = l.n_qt * a.g.batch * a.g.heads;
-    p.n_dkv = a.g.batch * a.g.heads_kv * (l.sink_tiles * l.sink_shares + (l.n_kt - l.sink_tiles));
-    p.qt = Divisor(l.n_qt);
+    const int cut = cut_tiles(a.g, l.n_qt), own = l.n_kt - l.sink_tiles;
+    p.dq = ItemOrder(l.n_qt, cut, a.g.batch * a.g.heads);
+    p.dkv = ItemOrder(own, cut < own ? cut : own, a.g.batch * a.g.heads_kv);
+    p.n_shared = a.g.batch * a.g.heads_kv * l.sink_tiles * l.sink_shares;
     p.heads = Divisor(a.g.heads);
-    p.bh = Divisor(a.g.batch * a.g.heads);
     p.heads_kv = Divisor(a.g.heads_kv);
     p.group = Divisor(a.g.group);
-    p.kt = Divisor(l.n_kt > l.sink_tiles ? l.n_kt - l.sink_tiles : 1);
-    p.bhk = Divisor(a.g.batch * a.g.heads_kv);
     p.shares = Divisor(l.sink_shares);
     p.shared = Divisor(l.sink_tiles > 0 ? l.sink_tiles * l.sink_shares : 1);
-    const auto wide = [&](const bsa_view_t* v, int64_t heads, int64_t rows) {
-        const auto on32 = [](int64_t n, int64_t stride) { return n == 1 || stride % 16 == 0; };
-        return (reinterpret_cast<uintptr_t>(v->data) & 31) == 0 && on32(a.g.batch, v->batch) && on32(heads, v->head) && on32(rows, v->row);
-    };
-    p.wide_q = wide(dQ, a.g.heads, a.g.N);
-    p.wide_k = wide(dK, a.g.heads_kv, a.g.N_kv);
-    p.wide_v = wide(dV, a.g.heads_kv, a.g.N_kv);
-    p.longest_first = a.g.left >= a.g.N_kv;
+    p.wide_q = view_is_wide(*dQ, a.g.batch, a.g.heads, a.g.N);
+    p.wide_k = view_is_wide(*dK, a.g.batch, a.g.heads_kv, a.g.N_kv);
+    p.wide_v = view_is_wide(*dV, a.g.batch, a.g.heads_kv, a.g.N_kv);
     p.sink_tiles = l.sink_tiles;
     p.sink_shares = l.sink_shares;
     cudaError_t e = window_status_word(a.device, &p.status);

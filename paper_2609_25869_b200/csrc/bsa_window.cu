@@ -60,8 +60,9 @@ struct Params {
 
 struct __align__(8) Barriers {
     uint64_t q_full[2], q_empty[2];
-    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
-    uint64_t s_full[2], s_free[2], ref_ready[2], p_ready[2], pv_done[2];
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], v_land[4];
+    uint64_t s_full[2], s_free[2], ref_ready[2], p_ready[2];
+    uint64_t pv_done[8];  // tile t: t mod 8 (see the reference warpgroup)
     uint64_t o_full, o_free, e_ready, e_taken;
 };
 
@@ -143,7 +144,8 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     uint8_t* sV = sK + C::kK * C::kTile;
     __shared__ Barriers bars;
     __shared__ float mref[2][kWinT];               // [tile mod 2][row]: the tile's reference maximum (log2 domain)
-    __shared__ float lfin[2][kWinT];  // [warpgroup][row]: an item's row sums, in its last reference
+    __shared__ float lfin[2][kWinT];  // [warpgroup][row]: an item's row sums, each in the reference of the warpgroup's last tile,
+    __shared__ float mfin[kWinT];     // which is here for the warpgroup that did not have the item's last one
     __shared__ uint32_t tmem_base_s, abort_flag;
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -160,14 +162,15 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             mbar_init(smem_u32(&bars.s_free[i]), 128);
             mbar_init(smem_u32(&bars.ref_ready[i]), 128);
             mbar_init(smem_u32(&bars.p_ready[i]), 128);
-            mbar_init(smem_u32(&bars.pv_done[i]), 1);
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(smem_u32(&bars.k_full[i]), 1);
             mbar_init(smem_u32(&bars.k_empty[i]), 1);
             mbar_init(smem_u32(&bars.v_full[i]), 1);
             mbar_init(smem_u32(&bars.v_empty[i]), 1);
+            mbar_init(smem_u32(&bars.v_land[i]), 1);
         }
+        for (int i = 0; i < 8; ++i) mbar_init(smem_u32(&bars.pv_done[i]), 1);
         mbar_init(smem_u32(&bars.o_full), 1);
         mbar_init(smem_u32(&bars.o_free), 128);
         mbar_init(smem_u32(&bars.e_ready), 256);
@@ -207,18 +210,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             if (!mbar_wait_warp(smem_u32(&bars.s_full[t & 1]), (t >> 1) & 1, abortp)) return false;
             tc_fence_after();
             float m0 = -INFINITY, m1 = m0, m2 = m0, m3 = m0;
-#pragma unroll 1
-            for (int c = 0; c < kWinT / 32; ++c) {
-                uint32_t r[32];
-                tmem_ld32(t_s + c * 32, r);
-                tc_wait_ld();
-                if (!full) {
-                    const uint32_t bits = row_bits(p.g, w.seq, w.seq.start + w.row0 + tw, key0 + c * 32);
-                    if (!__all_sync(0xffffffffu, bits == 0xffffffffu)) {
-                        hide(r, bits);
-                        tmem_st32(t_s + c * 32, r);
-                    }
-                }
+            auto take = [&](const uint32_t* r) {  // the maximum of 32 scores
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
                     m0 = max3(m0, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
@@ -226,12 +218,36 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     m2 = max3(m2, __uint_as_float(r[i + 4]), __uint_as_float(r[i + 5]));
                     m3 = max3(m3, __uint_as_float(r[i + 6]), __uint_as_float(r[i + 7]));
                 }
-            }
-            if (!full) {
-                if (w.range.hi - key0 < kWinT || w.range.lo - key0 > max(p.g.sinks - key0, 0)) {  // some keys are seen by no row
-                    if (!mbar_wait_warp(smem_u32(&bars.v_full[t % C::kV]), (t / C::kV) & 1, abortp)) return false;
-                    zero_unseen_keys<D>(sV + (t % C::kV) * C::kTile, p.g, w.range, key0, tw);
-                    fence_proxy_async_smem();
+            };
+            if (full) {
+#pragma unroll 1
+                for (int c = 0; c < kWinT; c += 64) {  // (this way lies on every tile's path: two waits, no votes)
+                    uint32_t r[64];
+                    tmem_ld32(t_s + c, r);
+                    tmem_ld32(t_s + c + 32, r + 32);
+                    tc_wait_ld();
+                    take(r);
+                    take(r + 32);
+                }
+            } else {
+                const RowView view(p.g, w.seq, w.seq.start + w.row0 + tw, key0);
+#pragma unroll 1
+                for (int c = 0; c < kWinT; c += 32) {
+                    const uint32_t bits = view.bits(c);
+                    uint32_t r[32];
+                    if (!__any_sync(0xffffffffu, bits)) {  // (of an edge tile's four pieces a warp mostly has one that is hidden in part)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[i] = 0xff800000u;
+                        tmem_st32(t_s + c, r);
+                        continue;
+                    }
+                    tmem_ld32(t_s + c, r);
+                    tc_wait_ld();
+                    if (!__all_sync(0xffffffffu, bits == 0xffffffffu)) {
+                        hide(r, bits);
+                        tmem_st32(t_s + c, r);
+                    }
+                    take(r);
                 }
                 tc_wait_st();
             }
@@ -242,8 +258,12 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             return true;
         };
         auto publish = [&](uint32_t t, float m, float m_old, bool moved) -> bool {
-            if (moved) {  // the accumulator follows, once all products before are in it
-                if (!mbar_wait_warp(smem_u32(&bars.pv_done[(t & 1) ^ 1]), ((t - 1) >> 1) & 1, abortp)) return false;
+            // The accumulator follows, once all products before are in it.  This wait comes now and then, and a barrier's parity tells whether
+            // its last phase but one or its last is over, no more: the barrier's phase before the one waited for has to be over for sure.
+            // That is P V of tile t - 9: the scores of t are there, so those of t - 2 and t - 3 have been read, so the warpgroups are
+            // done with t - 4 and t - 5, for which they waited until P V of t - 6 and t - 7 was over.
+            if (moved) {
+                if (!mbar_wait_warp(smem_u32(&bars.pv_done[(t - 1) & 7]), ((t - 1) >> 3) & 1, abortp)) return false;
                 tc_fence_after();
                 const float alpha = (m != m_old && m_old != -INFINITY) ? ex2_approx(m_old - m) : 1.f;
 #pragma unroll 1
@@ -307,7 +327,9 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 if (!ok) break;
             }
             if (!mbar_wait_warp(smem_u32(&bars.e_ready), n_it & 1, abortp)) break;
-            const float l = lfin[0][tw] + lfin[1][tw];
+            // (g is the next item's first tile, of the warpgroup that did not have this one's last; -inf where it had none: its sum is zero)
+            const float m_other = mfin[tw], l_other = lfin[g & 1][tw];
+            const float l = lfin[(g & 1) ^ 1][tw] + (m_other == m ? l_other : l_other * ex2_approx(m_other - m));
             mbar_arrive(smem_u32(&bars.e_taken));
             const bool any = seen && l > 0.f;
             const float inv = any ? 1.f / l : 0.f;
@@ -364,21 +386,49 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 }
             }
             if (!ok) let_copies_land();
-        } else if (warp == 11 && lane == 0) {
+        } else if (warp == 11) {
             // =========================== V producer ===========================
+            // A tile with keys that no row sees lands at a barrier of its own; it is handed on once they are zero, behind the next tile's copy.
             Ring ring;
+            uint32_t land_phases = 0;
+            int held = -1, held_key0 = 0;  // stage of the tile that is not handed on yet
+            KeyRange held_range = {0, 0, 0, 0, 0};
+            auto hand_on = [&]() -> bool {
+                if (held < 0) return true;
+                if (!mbar_wait_warp(smem_u32(&bars.v_land[held]), (land_phases >> held) & 1, abortp)) return false;
+                land_phases ^= 1u << held;
+                zero_unseen_keys<D, 32>(sV + held * C::kTile, p.g, held_range, held_key0, lane);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars.v_full[held]));
+                held = -1;
+                return true;
+            };
             bool ok = true;
             for (int k = 0; ok && load_item(p, k, it); ++k) {
                 const int n = it.tiles.count(), hk = it.hk;
                 for (int j = 0; j < n; ++j, ring.advance<C::kV>()) {
-                    ok = mbar_wait(smem_u32(&bars.v_empty[ring.stage]), ring.phase ^ 1, abortp);
+                    const int key0 = it.tiles.tile(j) * kWinT;
+                    // (a slot becomes free without the tile that is held: that is a later one's)
+                    ok = mbar_wait_warp(smem_u32(&bars.v_empty[ring.stage]), ring.phase ^ 1, abortp);
                     if (!ok) break;
-                    const uint32_t bar = smem_u32(&bars.v_full[ring.stage]);
-                    mbar_arrive_expect_tx(bar, C::kTile);
-                    tma_load_rows(smem_u32(sV) + ring.stage * C::kTile, &tmV, bar, it.tiles.tile(j) * kWinT, hk, it.b);
+                    const bool unseen = has_unseen_keys(p.g, it.range, key0);
+                    if (lane == 0) {
+                        const uint32_t bar = smem_u32(unseen ? &bars.v_land[ring.stage] : &bars.v_full[ring.stage]);
+                        mbar_arrive_expect_tx(bar, C::kTile);
+                        tma_load_rows(smem_u32(sV) + ring.stage * C::kTile, &tmV, bar, key0, hk, it.b);
+                    }
+                    ok = hand_on();
+                    if (!ok) break;
+                    if (unseen) {
+                        held = ring.stage;
+                        held_key0 = key0;
+                        held_range = it.range;
+                    }
                 }
             }
-            if (!ok) let_copies_land();
+            ok = ok && hand_on();
+            if (!ok && lane == 0) let_copies_land();
         } else if (warp == 9) {
             // =========================== Q K^T issuer ===========================
             // (Here and below the whole warp walks through the loop and one elected lane issues: with uniform control flow the
@@ -442,7 +492,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                         for (int kk = 0; kk < kWinT / 16; ++kk)
                             mma_ts(d_o, a_p + kk * 8, v0 + (uint64_t)(kk * 128), idesc, kk > 0 ? 1u : keep);
                         mma_commit(smem_u32(&bars.v_empty[ring.stage]));
-                        mma_commit(smem_u32(&bars.pv_done[g & 1]));
+                        mma_commit(smem_u32(&bars.pv_done[g & 7]));
                         if (j == n - 1) mma_commit(smem_u32(&bars.o_full));
                     }
                     ring.advance<C::kV>();
@@ -455,7 +505,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         const int x = warp >> 2, tw = tid & 127;
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t t_s = t_lane + (x ? C::kS1 : C::kS0), t_p = t_lane + (x ? C::kP1 : C::kP0);
-        const uint32_t b_ref = smem_u32(&bars.ref_ready[x]), b_pv = smem_u32(&bars.pv_done[x]);
+        const uint32_t b_ref = smem_u32(&bars.ref_ready[x]);
         const float c2 = p.scale_log2;
         const uint64_t c22 = pack_f32x2(c2, c2);
         uint32_t g = 0, n_it = 0;
@@ -484,7 +534,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 const uint64_t nm2 = pack_f32x2(neg_m, neg_m);
                 uint64_t sum01 = pack_f32x2(0.f, 0.f), sum23 = sum01;
                 if (t >= 2) {  // this warpgroup's last P has been read
-                    ok = mbar_wait_warp(b_pv, ((t >> 1) - 1) & 1, abortp);
+                    ok = mbar_wait_warp(smem_u32(&bars.pv_done[(t - 2) & 7]), ((t - 2) >> 3) & 1, abortp);
                     if (!ok) break;
                     tc_fence_after();
                 }
@@ -503,20 +553,13 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 mbar_arrive(smem_u32(&bars.p_ready[x]));
             }
             if (!ok) break;
-            const uint32_t last = g + n - 1;
-            if ((last & 1) != (uint32_t)x) {  // the other warpgroup had the last tile
-                // (its reference stays in place until both warpgroups have arrived below)
-                ok = mbar_wait_warp(smem_u32(&bars.ref_ready[x ^ 1]), (last >> 1) & 1, abortp);
-                if (!ok) break;
-                const float m = mref[x ^ 1][tw];
-                if (m_ref != m) l *= ex2_approx(m_ref - m);
-            }
             ok = mbar_wait_warp(smem_u32(&bars.e_taken), (n_it & 1) ^ 1, abortp);
             if (!ok) break;
+            g += n;
             lfin[x][tw] = l;
+            if (((g - 1) & 1) != (uint32_t)x) mfin[tw] = m_ref;
             mbar_arrive(smem_u32(&bars.e_ready));
             ++n_it;
-            g += n;
         }
     }
 

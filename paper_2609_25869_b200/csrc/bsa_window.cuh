@@ -82,12 +82,21 @@ __device__ __forceinline__ TileSpan join(const TileSpan& a, const TileSpan& b) {
     return t;
 }
 
-// What the row at `pos` sees of the 32 keys from key0 on, one bit each.
-__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
-__device__ __forceinline__ uint32_t row_bits(const WindowGeom& g, const Sequence& s, int pos, int key0) {
-    const int hi = (pos >= 0 && pos < s.len) ? min(s.len, pos + g.right + 1) : 0;
-    return bits_below(hi - key0) & (~bits_below(pos - g.left - key0) | bits_below(g.sinks - key0));
+// The lowest n bits (none for n <= 0, all from 32 on).
+__device__ __forceinline__ uint32_t bits_below(int n) {
+    uint32_t m;
+    asm("bmsk.clamp.b32 %0, 0, %1;" : "=r"(m) : "r"(max(n, 0)));
+    return m;
 }
+// What a row sees of a tile: bounds on the tile's columns, and 32 of them as bits.
+struct RowView {
+    int hi, lo, sink;
+    __device__ __forceinline__ RowView(const WindowGeom& g, const Sequence& s, int pos, int key0)
+        : hi(((pos >= 0 && pos < s.len) ? min(s.len, pos + g.right + 1) : 0) - key0), lo(pos - g.left - key0), sink(g.sinks - key0) {}
+    __device__ __forceinline__ uint32_t bits(int col) const {
+        return bits_below(hi - col) & (~bits_below(lo - col) | bits_below(sink - col));
+    }
+};
 // Hidden scores become -inf: two instructions each (a test of the two bounds branched, 7000 clk a tile).
 __device__ __forceinline__ void hide(uint32_t* r, uint32_t bits) {
 #pragma unroll
@@ -95,19 +104,22 @@ __device__ __forceinline__ void hide(uint32_t* r, uint32_t bits) {
 }
 
 // Rows of a tile in shared memory that no row of the CTA sees may hold anything, and a weight of zero times NaN would not be zero:
-// they become zero themselves (all their 64-column sub-tiles, whatever the swizzle).  128 threads, eight to a row, so that a warp's stores
-// fall into different banks (with a row to a thread a window's edge tile took 2000 clk more); the caller fences.
-template <int D>
+// they become zero themselves (all their 64-column sub-tiles, whatever the swizzle).  Eight of the THREADS to a row, so that a warp's
+// stores fall into different banks (with a row to a thread a window's edge tile took 2000 clk more); the caller fences.
+template <int D, int THREADS>
 __device__ __forceinline__ void zero_rows(uint8_t* tile, int from, int to, int thread) {
-    for (int row = max(from, 0) + (thread >> 3); row < min(to, kWinT); row += 16)
+    for (int row = max(from, 0) + (thread >> 3); row < min(to, kWinT); row += THREADS / 8)
 #pragma unroll
         for (int s = 0; s < D / 64; ++s)
             *reinterpret_cast<uint4*>(tile + s * (kWinT * 128) + row * 128 + (thread & 7) * 16) = make_uint4(0, 0, 0, 0);
 }
-template <int D>
+__device__ __forceinline__ bool has_unseen_keys(const WindowGeom& g, const KeyRange& k, int key0) {
+    return k.hi - key0 < kWinT || k.lo - key0 > max(g.sinks - key0, 0);
+}
+template <int D, int THREADS>
 __device__ __forceinline__ void zero_unseen_keys(uint8_t* tile, const WindowGeom& g, const KeyRange& k, int key0, int thread) {
-    zero_rows<D>(tile, g.sinks - key0, k.lo - key0, thread);
-    zero_rows<D>(tile, k.hi - key0, kWinT, thread);
+    zero_rows<D, THREADS>(tile, g.sinks - key0, k.lo - key0, thread);
+    zero_rows<D, THREADS>(tile, k.hi - key0, kWinT, thread);
 }
 
 // Division of non-negative ints by a constant of the call: the items of a persistent CTA are decoded on its critical path.

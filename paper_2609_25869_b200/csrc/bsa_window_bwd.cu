@@ -371,12 +371,13 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                     r[c + 1] = __float_as_uint(ex2_approx(e));
                 }
                 if (!full) {
-                    zero_unseen_keys<D>(sK + (t % C::kK) * C::kTile, p.g, it.range, key0, tw);
+                    zero_unseen_keys<D, 128>(sK + (t % C::kK) * C::kTile, p.g, it.range, key0, tw);
                     fence_proxy_async_smem();
                 }
                 ok = mbar_wait_warp(smem_u32(&bars.dp_full[x]), (t >> 1) & 1, abortp);
                 if (!ok) break;
                 tc_fence_after();
+                const RowView view(p.g, it.seq, pos, key0);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     uint32_t d[32];
@@ -391,7 +392,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                         d[e + 1] = __float_as_uint(v);
                     }
                     if (!full) {
-                        const uint32_t bits = row_bits(p.g, it.seq, pos, key0 + c * 32);
+                        const uint32_t bits = view.bits(c * 32);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) d[e] = (bits & (1u << e)) ? d[e] : 0u;
                     }
@@ -706,8 +707,8 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                         ok = mbar_wait_warp(smem_u32(&bars.o_full[ring.stage]), ring.phase, abortp);
                         if (!ok) break;
                         uint8_t* rows = (x ? sQ : sG) + ring.stage * C::kTile;
-                        zero_rows<D>(rows, 0, -pos0, tw);
-                        zero_rows<D>(rows, seq.len - pos0, kWinT, tw);
+                        zero_rows<D, 128>(rows, 0, -pos0, tw);
+                        zero_rows<D, 128>(rows, seq.len - pos0, kWinT, tw);
                         fence_proxy_async_smem();
                     }
                 }

@@ -154,7 +154,7 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         ok = mbar_wait_warp(bV + slot * 8, phase, abortp);
         if (!ok) break;
         if (!full) {
-            const uint32_t lo_bits = row_bits(p.g, seq, pos[0], key0), hi_bits = row_bits(p.g, seq, pos[1], key0);
+            const uint32_t lo_bits = RowView(p.g, seq, pos[0], key0).bits(0), hi_bits = RowView(p.g, seq, pos[1], key0).bits(0);
 #pragma unroll
             for (int n = 0; n < NT_S; ++n) {
                 const int c = n * 8 + 2 * t;

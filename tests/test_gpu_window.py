@@ -150,6 +150,25 @@ def test_scores_that_grow_along_the_keys(n, dtype):
     check_forward(q, k, v, **kw)
 
 
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "bf16"), (128, "fp16")])
+def test_references_that_move_now_and_then(d, dtype):
+    """Long lists in which single tiles lie far above all before them, in places that differ from head to head; many items per CTA, windows
+    and sinks, so that such tiles come first, second and last in their lists."""
+    h, n = 40, 2600
+    q, k, v, _ = tensors(21, "hnd", 1, h, h, n, n, d, dtype)
+    g = torch.Generator().manual_seed(5)
+    q[..., 0], k[..., 0] = 6.0, 0.0
+    level = torch.zeros(h, n)
+    for i in range(h):
+        for j in sorted(torch.randint(0, n, (6,), generator=g).tolist()):
+            level[i, j:] += float(torch.randint(2, 9, (1,), generator=g)) * d ** 0.5 / 6.0
+        # falls again now and then, so that windows further on see their own rises
+        level[i, torch.randint(0, n, (1,), generator=g).item():] *= 0.25
+    k[0, :, :, 0] = level.to(k)
+    for kw in (dict(left=900, right=0, sinks=3), dict(left=400, right=200, sinks=140), dict(left=-1, right=0)):
+        check_forward(q, k, v, **kw)
+
+
 def test_scale_and_large_scores():
     q, k, v, g = tensors(14, "hnd", 1, 2, 2, 256, 256, 64, "fp16")
     for scale in (1.0, 1e-3):
@@ -224,6 +243,21 @@ def test_bits_do_not_change_from_run_to_run_or_with_the_batch(d):
     assert torch.equal(O1, O[1:2, :6]) and torch.equal(L1, L[1:2, :6])
     dQ1 = bsa.window_backward(*one, O1, L1, g[1:2, :6].contiguous(), **kw)[0]
     assert torch.equal(dQ1, G[0][1:2, :6])
+
+
+def test_many_items_with_edges_on_every_tile():
+    """Short windows over many items: the protocol between the warps runs through all of its orders, and ends."""
+    q, k, v, g = tensors(22, "nhd", 2, 24, 24, 6000, 6000, 64, "bf16")
+    kw = dict(left=200, right=100, sinks=300, layout="nhd")
+    O, L = bsa.window_forward(q, k, v, **kw)
+    for _ in range(20):
+        O2, L2 = bsa.window_forward(q, k, v, **kw)
+    assert bsa.window_status() == 0 and torch.equal(O, O2) and torch.equal(L, L2)
+    part = dict(left=200, right=100, sinks=300, layout="nhd")
+    for h in (0, 23):
+        wO, wL, tO, tL = R.forward(q[1:, :, h:h + 1], k[1:, :, h:h + 1], v[1:, :, h:h + 1], u=2.0 ** -8, **part)
+        R.assert_within(O[1:, :, h:h + 1], wO, tO, "O")
+        R.assert_within(L[1:, h:h + 1], wL, tL, "LSE")
 
 
 @pytest.mark.parametrize("n", [2, 300])

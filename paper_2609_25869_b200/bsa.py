@@ -372,6 +372,7 @@ def request_host(mask: np.ndarray, B_Q: int, B_KV: int, N: int, heads: int, d: i
 
 # ---------------------------------------------------------------- positions and windows
 # The C structs as packed bytes: filling a ctypes structure field by field takes longer than the smallest kernels.
+_PTR = struct.Struct("@P")
 _VIEW = struct.Struct("@Pqqq")                       # bsa_view_t
 _ROPE = struct.Struct("@4iq2i4i4idPPqq4i4i")         # bsa_rope_desc_t
 _WINDOW = struct.Struct("@4iqqqqqifPP")              # bsa_window_desc_t
@@ -422,13 +423,22 @@ def _int32_ptr(t, shapes, dev: int, what: str) -> int:
     return t.data_ptr()
 
 
-def _on_device(dev: int, call, stream):
-    """``call(stream pointer)`` with device ``dev`` current, on ``stream`` or the device's current stream."""
+def _fresh_view(t, like, nhd: bool, dtype, dev: int, packed: bytes) -> bytes:
+    """The view of ``t``, just allocated like ``like``, whose own view is ``packed``: the same strides where ``like`` is dense."""
+    if like.is_contiguous():
+        return _PTR.pack(t.data_ptr()) + packed[8:]
+    return _view(t, nhd, dtype, dev, "out")[4]
+
+
+def _call(dev: int, stream, where: str, call, *args):
+    """``call(*args, stream pointer)`` with device ``dev`` current, on ``stream`` or the device's current stream; raises its errors."""
     if dev != _torch._C._cuda_getDevice():
         with _torch.cuda.device(dev):
-            return call(_stream_ptr(stream))
-    # (the handle alone, as in _stream_ptr)
-    return call((_torch._C._cuda_getCurrentRawStream(dev) or None) if stream is None else _stream_ptr(stream))
+            status = call(*args, _stream_ptr(stream))
+    else:  # (the handle alone, as in _stream_ptr)
+        status = call(*args, (_torch._C._cuda_getCurrentRawStream(dev) or None) if stream is None else _stream_ptr(stream))
+    if status:
+        _check(status, where)
 
 
 def rope(Q, K=None, *, axes, positions=None, grid=None, first: int = 0, origin=None, theta: float = 10000.0, freq=None,
@@ -446,19 +456,24 @@ def rope(Q, K=None, *, axes, positions=None, grid=None, first: int = 0, origin=N
     dt, dev = _tensor_of(Q, "Q")
     dtype = Q.dtype
     b, h, n, d, vq = _view(Q, nhd, dtype, dev, "Q")
-    if out is None:
-        oq, ok = _torch.empty_like(Q), None if K is None else _torch.empty_like(K)
-    else:
-        oq, ok = (out, None) if K is None else out
-        if oq.shape != Q.shape or (K is not None and ok.shape != K.shape):
-            raise ValueError("out has to have the shapes of Q and K")
-    voq = _view(oq, nhd, dtype, dev, "out")[4]
-    hk, vk, vok = 0, None, None
+    hk, vk, ok, vok = 0, None, None, None
     if K is not None:
         bk, hk, nk, dk, vk = _view(K, nhd, dtype, dev, "K")
         if bk != b or nk != n or dk != d:
             raise ValueError("Q and K have to agree in batch, tokens and channels")
-        vok = _view(ok, nhd, dtype, dev, "out")[4]
+    if out is None:
+        oq = _torch.empty_like(Q)
+        voq = _fresh_view(oq, Q, nhd, dtype, dev, vq)
+        if K is not None:
+            ok = _torch.empty_like(K)
+            vok = _fresh_view(ok, K, nhd, dtype, dev, vk)
+    else:
+        oq, ok = (out, None) if K is None else out
+        if oq.shape != Q.shape or (K is not None and ok.shape != K.shape):
+            raise ValueError("out has to have the shapes of Q and K")
+        voq = _view(oq, nhd, dtype, dev, "out")[4]
+        if K is not None:
+            vok = _view(ok, nhd, dtype, dev, "out")[4]
     na = len(axes)
     if not 1 <= na <= 4 or (positions is None) == (grid is None):
         raise ValueError("one to four axes, and either positions or a grid")
@@ -479,9 +494,7 @@ def rope(Q, K=None, *, axes, positions=None, grid=None, first: int = 0, origin=N
         freqs = (ctypes.c_double * len(freq))(*freq)
     desc = _ROPE.pack(b, h, hk, d, n, dt, na, *axes, *pad, PAIRS[pairs], shared_freq, inverse, 0, theta,
                       0 if freqs is None else ctypes.addressof(freqs), pos, per_batch, first, *where)
-    status = _on_device(dev, lambda st: lib().bsa_rope(desc, vq, vk, voq, vok, st), stream)
-    if status:
-        _check(status, "bsa_rope")
+    _call(dev, stream, "bsa_rope", lib().bsa_rope, desc, vq, vk, voq, vok)
     return oq if K is None else (oq, ok)
 
 
@@ -513,16 +526,16 @@ def window_forward(Q, K, V, *, left: int, right: int = 0, sinks: int = 0, q_star
     desc, vq, vk, vv, shape, dev = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, nhd)
     if O is None:
         O = _torch.empty_like(Q)
-    elif O.shape != Q.shape:
-        raise ValueError("O has to have the shape of Q")
+        vo = _fresh_view(O, Q, nhd, Q.dtype, dev, vq)
+    else:
+        if O.shape != Q.shape:
+            raise ValueError("O has to have the shape of Q")
+        vo = _view(O, nhd, Q.dtype, dev, "O")[4]
     if LSE is None:
         LSE = Q.new_empty(shape, dtype=_torch.float32)
     else:
         _check_lse(LSE, shape, dev)
-    vo = _view(O, nhd, Q.dtype, dev, "O")[4]
-    status = _on_device(dev, lambda st: lib().bsa_window_forward(desc, vq, vk, vv, vo, LSE.data_ptr(), st), stream)
-    if status:
-        _check(status, "bsa_window_forward")
+    _call(dev, stream, "bsa_window_forward", lib().bsa_window_forward, desc, vq, vk, vv, vo, LSE.data_ptr())
     return O, LSE
 
 
@@ -535,7 +548,7 @@ def window_backward(Q, K, V, O, LSE, dO, *, left: int, right: int = 0, sinks: in
                     scale: float = 0.0, layout: str = "hnd", dQ=None, dK=None, dV=None, stream=None):
     """``bsa_window_backward``: ``(dQ, dK, dV)`` of ``window_forward`` from its inputs, its outputs and the gradient ``dO`` of
     ``O``; arguments as there.  dK and dV are summed over the query heads that share a key head.  The workspace comes from
-    torch's allocator on the current stream; with ``stream`` given, that one has to be the tensors' as torch knows it."""
+    torch's allocator, on the current stream or on ``stream`` (a torch stream)."""
     nhd = LAYOUTS[layout] == 1
     desc, vq, vk, vv, shape, dev = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, nhd)
     if O.shape != Q.shape or dO.shape != Q.shape:
@@ -547,11 +560,19 @@ def window_backward(Q, K, V, O, LSE, dO, *, left: int, right: int = 0, sinks: in
         raise ValueError("gradients have to have the shapes of their tensors")
     views = [_view(t, nhd, Q.dtype, dev, n)[4] for t, n in ((O, "O"), (dO, "dO"), (dQ, "dQ"), (dK, "dK"), (dV, "dV"))]
 
-    def call(st):
-        n = lib().bsa_window_workspace_bytes(desc)
+    L = lib()
+    if dev != _torch._C._cuda_getDevice():
+        with _torch.cuda.device(dev):
+            n = L.bsa_window_workspace_bytes(desc)
+    else:
+        n = L.bsa_window_workspace_bytes(desc)
+    # (where the description is refused n is 0, and the call says why)
+    if stream is None:
         ws = _torch.empty(n, dtype=_torch.uint8, device=Q.device)
-        return lib().bsa_window_backward(desc, vq, vk, vv, views[0], LSE.data_ptr(), *views[1:], ws.data_ptr(), n, st)
-    _check(_on_device(dev, call, stream), "bsa_window_backward")
+    else:  # the workspace's memory is free again when that stream has come past this call
+        with _torch.cuda.stream(stream):
+            ws = _torch.empty(n, dtype=_torch.uint8, device=Q.device)
+    _call(dev, stream, "bsa_window_backward", L.bsa_window_backward, desc, vq, vk, vv, views[0], LSE.data_ptr(), *views[1:], ws.data_ptr(), n)
     return dQ, dK, dV
 
 

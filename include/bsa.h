@@ -390,7 +390,7 @@ BSA_API bsa_status_t bsa_rope(const bsa_rope_desc_t* desc, const bsa_view_t* Q, 
  * so right = 0 is causal, and sinks lift the left limit only.  A row at no position of its sequence (p < 0 or
  * p >= kv_len: padding) sees nothing: O = 0, LSE = -inf, and it adds nothing to any gradient.
  *     S = scale * q . k,   LSE = log sum exp S,   O = sum exp(S - LSE) v      over the keys that the row sees.
- * Query head h reads key head h / (heads / heads_kv).  Keys that no row of a 256-row tile sees (beyond kv_len, left of the
+ * Query head h reads key head h / (heads / heads_kv).  Keys that no row of a tile of 128 rows sees (beyond kv_len, left of the
  * window) may hold anything, NaN included; a key that some row of a tile sees and another does not has to be finite for the
  * other's sake (its weight there is zero).
  *   Scores, softmax and accumulators are fp32; P (and dS in the backward) is rounded to the element type for its product,
@@ -401,7 +401,8 @@ BSA_API bsa_status_t bsa_rope(const bsa_rope_desc_t* desc, const bsa_view_t* Q, 
  *   dK and dV summed over the query heads that share a key head and written for all N_kv rows (zero where nothing sees the
  *   key).  workspace_dev: bsa_window_workspace_bytes(desc) bytes of device memory on a 256-byte boundary, the call's own until its
  *   work on the stream is done (calls that may overlap each bring their own).
- * A bounded device wait that expires ends the kernel with BSA_ERR_DEVICE_TIMEOUT in bsa_window_status; it never hangs.
+ * A bounded device wait that expires ends the kernel with BSA_ERR_DEVICE_TIMEOUT in bsa_window_status; it never hangs.  (The limit is
+ * about a second; bsa_debug_set_wait_limit sets that of the plans' kernels only.)
  * Errors: INVALID_ARG (null, misaligned or overlapping strides, sizes below one, left or right below -1, sinks below 0, heads not
  * a multiple of heads_kv, workspace too small), UNSUPPORTED (d not 64 or 128, N or N_kv above 2^29, more than 65535
  * sequences x heads), CUDA.

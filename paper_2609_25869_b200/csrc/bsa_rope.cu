@@ -3,7 +3,8 @@
 // The kernel is bound by memory: every element is read and written once, 4 bytes of traffic against three operations.  A
 // thread owns 8 channels (16 bytes; with paired halves 8 + 8) of one token and walks over heads with them: the pair's
 // angle depends on the token alone, so its sine and cosine are computed once and serve every head of Q and K in registers.
-// The loads of several heads are issued before the first is used.
+// The loads of four heads are issued before the first is used (two: 4 % slower, eight: 1 % faster on the largest call, 5 % slower on
+// paired halves).  75600 tokens, 24 + 24 heads, d = 128, token-major: 288 us, 98 % of the rate of a plain copy; one token of 40 heads 2.6 us.
 //
 // Angles.  A position of 10^6 times a frequency near 1 leaves no correct bit of the angle's fraction in fp32.  The host
 // turns each frequency into F = freq / 2 pi in units of 2^-64 turns; pos * F in wrap-around 64-bit integers IS the angle

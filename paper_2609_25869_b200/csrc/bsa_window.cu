@@ -13,9 +13,13 @@
 // than that over a tile (latencies), so two must run at once and neither may wait: S and P have their own columns, Q K^T runs
 // two tiles ahead, and the maxima are found by a third warpgroup while the tile in front is still in the softmax.  That also
 // makes one reference maximum per row for both warpgroups, and one accumulator.
-// On one GPU, 25088 keys for 4736 rows, d = 128, 12 heads: 256 rows per CTA, a slot of 128 per warpgroup with P in the place of S (so that a
-// slot's softmax, P V and Q K^T follow each other) 900 TFLOP/s; 128 rows, warpgroups finding the maxima themselves 1100.
-// Tensor-memory columns: S0 0, S1 128, O 256, P0 384, P1 448.
+// On one GPU, 25088 keys for 4736 rows, bf16, d = 128, 12 heads: 256 rows per CTA, a slot of 128 per warpgroup with P in the place of S (so
+// that a slot's softmax, P V and Q K^T follow each other) 900 TFLOP/s; 128 rows, warpgroups finding the maxima themselves 1100; this form
+// 1280 (4 heads, where the power cap takes less: 1380), d = 64 760.  The tensor pipe and the special-function unit are 69 % busy each
+// (16384 rows, 8 heads, causal window 4096).  Short windows pay per item: edge tiles take the reference warpgroup 1400 clk instead of 550, an
+// item's end 2000.
+// Tensor-memory columns: S0 0, S1 128, O 256, P0 384, P1 448.  Registers (setmaxnreg): 256 * 184 + 128 * 96 + 128 * 48 = 65536, the
+// launch's 512 * 128.
 #include <cuda_bf16.h>
 #include <math.h>
 

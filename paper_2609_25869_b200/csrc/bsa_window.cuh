@@ -62,7 +62,6 @@ struct TileSpan {
     int st, w0, w1;
     __device__ __forceinline__ int count() const { return st + (w1 - w0); }
     __device__ __forceinline__ int tile(int j) const { return j < st ? j : w0 + (j - st); }
-    __device__ __forceinline__ bool has(int t) const { return t < st || (t >= w0 && t < w1); }
 };
 __device__ __forceinline__ TileSpan tile_span(const KeyRange& k) {
     TileSpan t;
@@ -71,17 +70,6 @@ __device__ __forceinline__ TileSpan tile_span(const KeyRange& k) {
     t.st = min((k.sink_hi + kWinT - 1) / kWinT, t.w0);
     return t;
 }
-// The tiles of either span (an empty span: w0 = w1 = 0).
-__device__ __forceinline__ TileSpan join(const TileSpan& a, const TileSpan& b) {
-    if (a.w1 == 0) return b;
-    if (b.w1 == 0) return a;
-    TileSpan t;
-    t.w0 = min(a.w0, b.w0);
-    t.w1 = max(a.w1, b.w1);
-    t.st = min(max(a.st, b.st), t.w0);
-    return t;
-}
-
 // The lowest n bits (none for n <= 0, all from 32 on).
 __device__ __forceinline__ uint32_t bits_below(int n) {
     uint32_t m;

@@ -9,6 +9,8 @@
 //   * the warps' (m, l, O) are joined in shared memory, the CTAs' through distributed shared memory, each CTA writing its
 //     share of the columns: one launch, no workspace, no counters, the same bits every time.
 // Two CTAs of six warps per SM: 192 KB of copies in flight, and one CTA's start and end beside the other's middle.
+// Six sequences of 1111 to 115200 keys, 32 + 8 heads, d = 128, one token: 236 us for 1.37 GB, 5.8 TB/s; four sequences with a window of 1024:
+// 7.7 us in a graph (clusters of two instead of eight 10.3; the joins' loads one after the other 8.4).
 #include <cuda_bf16.h>
 #include <math.h>
 

@@ -385,3 +385,31 @@ def test_refusals():
     assert call(ws.data_ptr(), need - 1) == 1 and call(None, need) == 1 and call(ws.data_ptr() + 4, need) == 1
     assert call(ws.data_ptr(), need) == 0
     torch.cuda.synchronize()
+
+
+def test_first_calls_of_a_process_may_be_captured():
+    """Nothing that a first call sets up (attributes, addresses, module loading) is refused while a stream is being captured."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2609_25869_b200 import bsa
+x = [torch.randn(1, 2, 200, 64, device='cuda').bfloat16() for _ in range(4)]
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    q, k = bsa.rope(x[0], x[1], axes=(64,), grid=(200,))
+    O, L = bsa.window_forward(q, k, x[2], left=20, sinks=2)
+    o, _ = bsa.window_forward(q[:, :, -1:], k, x[2], left=20, sinks=2)
+    G = bsa.window_backward(q, k, x[2], O, L, x[3], left=20, sinks=2)
+g.replay()
+torch.cuda.synchronize()
+q2, k2 = bsa.rope(x[0], x[1], axes=(64,), grid=(200,))
+O2, L2 = bsa.window_forward(q2, k2, x[2], left=20, sinks=2)
+assert torch.equal(O, O2) and torch.equal(L, L2)
+assert all(torch.equal(a, b) for a, b in zip(G, bsa.window_backward(q2, k2, x[2], O2, L2, x[3], left=20, sinks=2)))
+assert bsa.window_status() == 0
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]

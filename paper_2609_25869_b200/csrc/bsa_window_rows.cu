@@ -1,4 +1,4 @@
-// Attention over a sliding window and a few first tokens: forward for few rows (the next token, a handful of drafted ones).
+// Attention over a sliding window and a few first tokens: forward for few rows (the next token, a handful of drafted ones, a short chunk).
 //
 // The same mathematics as the kernel for tiles of rows (bsa_window.cu), but the work is to read the visible keys and values once:
 // with R rows per key head (query tokens x heads that share it) there are R multiplications per element read, far below what

@@ -84,7 +84,11 @@ FEW = [
     (1, 16, 16, 1, 20000, -1, 0, 0, None, None),
     (2, 3, 3, 1, 64, 8, 0, 2, [0, 0], [0, 1]),                         # no keys; one key
     (1, 4, 1, 8, 600, 590, 0, 1, None, None),                          # 32 rows of different windows
-    (1, 4, 1, 9, 600, 590, 0, 1, None, None),                          # 36: the kernel for tiles
+    (1, 4, 1, 9, 600, 590, 0, 1, None, None),                          # 36: three blocks, the last of four rows
+    (1, 2, 1, 32, 900, 130, 40, 20, [780], [800]),                     # 64, the last rows at no position
+    (1, 3, 1, 85, 5000, -1, 40, 20, [4700], [4750]),                   # 255 over many keys, the last rows at no position
+    (1, 1, 1, 256, 5000, 4500, 0, 0, None, None),                      # 256: the most that this kernel takes
+    (2, 75, 75, 17, 300, 100, 0, 3, [283, 100], [300, 116]),           # 150 heads, two blocks each: the kernel for tiles, with few rows
 ]
 
 

@@ -10,8 +10,9 @@
 //            (K Q^T, V dO^T, P^T dO, dS^T Q: four products a tile)
 // Seven products instead of the five that one kernel for all three gradients needs; that one would add either dQ or dK and dV up
 // in global memory, in an order that changes from run to run, or keep partial sums of one of them per tile of the other.  Here
-// every gradient is summed in tensor memory by one CTA.  Only the keys of the first tokens, seen by every query, are cut into
-// several shares of their queries, whose sums are added up in a fixed order by a fourth kernel.
+// every gradient is summed in tensor memory by one CTA.  Only the keys of the first tokens, seen by every query, and the keys of calls
+// that would leave the GPU idle, are cut into several shares of their queries, whose sums are added up in a fixed order by a fourth
+// kernel.
 // In both kernels eight softmax warps (thread = row of a tile), one warp that copies and one that issues the products.
 // 16384 rows, 16 + 4 heads, d = 128, causal window 2048, 16 sinks: delta 24 us (bytes), dQ 359, dK and dV 470, the sinks' sum 5.  Per tile dQ
 // takes 2230 clk where its three products are 1536: two of them read both operands from shared memory, 224 KB a tile with the copies, at
@@ -856,20 +857,28 @@ Layout layout_of(const WindowArgs& a) {
     // tiles are cut into shares about as long as the other tiles' work, as long as no more than four items per SM come out
     // of it (their partial sums are 128 KB each at d = 128).
     const int64_t window = ((int64_t)g.left + g.right + 2 * kWinT - 1) / kWinT + 1;
-    const int64_t tiles = (g.sinks + kWinT - 1) / kWinT;
+    const int64_t tiles = (g.sinks + kWinT - 1) / kWinT, rows = (int64_t)g.batch * g.heads_kv;
     if (tiles > 0 && window * 2 <= l.n_qt) {
         l.sink_tiles = (int)(tiles < l.n_kt ? tiles : l.n_kt);
-        const int64_t most = 4 * (int64_t)a.num_sms / ((int64_t)g.batch * g.heads_kv * l.sink_tiles);
+        const int64_t most = 4 * (int64_t)a.num_sms / (rows * l.sink_tiles);
         int64_t shares = (l.n_qt + window - 1) / window;
         if (shares > most) shares = most;
         l.sink_shares = (int)(shares > 1 ? shares : 1);
         if (l.sink_shares == 1) l.sink_tiles = 0;
     }
+    // Where all key tiles together leave most of the GPU idle, every one is cut: into as many shares as fill it, of four query tiles at least
+    // (the sum of the shares costs about 5 us, a query tile 1.6).
+    const int64_t work = (window < l.n_qt ? window : l.n_qt) * g.group;
+    const int64_t fill = a.num_sms / (rows * l.n_kt), each = work / 4;
+    if (fill >= 2 && each >= 2) {
+        l.sink_tiles = l.n_kt;
+        l.sink_shares = (int)(fill < each ? fill : each);
+    }
     if (l.sink_tiles == 0) l.sink_shares = 1;
-    const int64_t rows = (int64_t)g.batch * g.heads * l.n_pad * 4;
+    const int64_t bytes = (int64_t)g.batch * g.heads * l.n_pad * 4;
     l.lse2 = 0;
-    l.delta = rows;
-    l.partial = (2 * rows + 255) / 256 * 256;
+    l.delta = bytes;
+    l.partial = (2 * bytes + 255) / 256 * 256;
     l.bytes = l.partial + (l.sink_tiles ? (int64_t)g.batch * g.heads_kv * l.sink_tiles * l.sink_shares * 2 * kWinT * a.d * 4 : 0);
     return l;
 }

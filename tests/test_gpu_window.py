@@ -191,6 +191,17 @@ def test_sinks_of_long_sequences(sinks, left, group):
     check_backward(q, k, v, g, O, L, **kw)
 
 
+@pytest.mark.parametrize("h,hk,n,left", [(1, 1, 1500, -1), (2, 1, 1200, 900), (8, 1, 600, 100), (3, 3, 1100, -1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_of_few_heads(h, hk, n, left, d):
+    """So few key tiles that every one is cut into shares."""
+    q, k, v, g = tensors(23, "hnd", 1, h, hk, n, n, d, "bf16")
+    kw = dict(left=left, right=0, sinks=5, kv_len=ints([n - 70]), q_start=ints([0]))
+    O, L = check_forward(q, k, v, **kw)
+    G = check_backward(q, k, v, g, O, L, **kw)
+    assert all(torch.equal(a, b) for a, b in zip(G, bsa.window_backward(q, k, v, O, L, g, **kw)))
+
+
 def test_views_of_a_fused_projection_and_of_a_cache():
     b, n, h, d = 2, 200, 4, 128
     qkv = torch.randn(b, n, 3, h, d, device="cuda").bfloat16()

@@ -29,7 +29,6 @@ constexpr int kRows = 16;
 constexpr int kRing = 8192;  // bytes of a warp's K or V ring
 constexpr int kSlot = 4096;
 constexpr int kSlots = kRing / kSlot;
-constexpr int kMaxCluster = 8;
 constexpr unsigned kAll = 0xffffffffu;
 // Half: P, at most one, is computed 2^15 times as large (half ends at 2^16), so that less of it falls below 2^-14.
 template <bool F16>
@@ -60,7 +59,8 @@ __device__ __forceinline__ float2 ld_cluster(uint32_t addr) {
     return v;
 }
 
-template <int D, bool F16>
+// MAX_C: most CTAs of the cluster, eight or sixteen (the join's loads are written out).
+template <int D, bool F16, int MAX_C>
 __global__ void __launch_bounds__(kWarps * 32, 2)
 window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ RowsParams p) {
     constexpr int KS = kSlot / (D * 2);  // keys per step
@@ -287,18 +287,18 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     const uint32_t a_sum = smem_u32(sum), a_ml = smem_u32(cml);
     for (int i = rank * per + 2 * threadIdx.x; i < (rank + 1) * per; i += 2 * kWarps * 32) {
         const int r = i / D, c = (i - r * D) ^ ((r & 7) << 3);  // element i of the stored order is column c
-        float2 ml[kMaxCluster], v[kMaxCluster];
+        float2 ml[MAX_C], v[MAX_C];
 #pragma unroll
-        for (int q = 0; q < kMaxCluster; ++q) {  // all loads on their way before the first is used (ranks beyond C: this one again)
+        for (int q = 0; q < MAX_C; ++q) {  // all loads on their way before the first is used (ranks beyond C: this one again)
             const uint32_t from = q < C ? q : rank;
             ml[q] = ld_cluster(map_to_rank(a_ml + r * 8, from));
             v[q] = ld_cluster(map_to_rank(a_sum + i * 4, from));
         }
         float M = -INFINITY, L = 0.f, v0 = 0.f, v1 = 0.f;
 #pragma unroll
-        for (int q = 0; q < kMaxCluster; ++q) M = fmaxf(M, ml[q].x);
+        for (int q = 0; q < MAX_C; ++q) M = fmaxf(M, ml[q].x);
 #pragma unroll
-        for (int q = 0; q < kMaxCluster; ++q) {
+        for (int q = 0; q < MAX_C; ++q) {
             const float f = (q >= C || ml[q].x == -INFINITY) ? 0.f : ex2_approx(ml[q].x - M);
             L = fmaf(f, ml[q].y, L);
             v0 = fmaf(f, v[q].x, v0);
@@ -325,20 +325,27 @@ cudaError_t launch(const WindowArgs& a, const bsa_view_t& K, const bsa_view_t& V
     CUtensorMap tk, tv;
     if (!encode_view_map(&tk, K, a.g.N_kv, a.g.heads_kv, a.g.batch, D, KS, F16) || !encode_view_map(&tv, V, a.g.N_kv, a.g.heads_kv, a.g.batch, D, KS, F16))
         return cudaErrorInvalidValue;
-    const auto kernel = window_rows_kernel<D, F16>;
+    const auto kernel = window_rows_kernel<D, F16, 8>, wide_kernel = window_rows_kernel<D, F16, 16>;
     static std::atomic<bool> allowed[kMaxDevices];
     if (!allowed[a.device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(wide_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         allowed[a.device].store(true, std::memory_order_relaxed);
     }
     const unsigned blocks = (unsigned)((p.n_rows + kRows - 1) / kRows), heads = (unsigned)(a.g.batch * a.g.heads_kv);
     // CTAs of a cluster: until the GPU is full (two per SM), and eight at once where a sequence may be long: how the lengths differ
-    // is not known here, and smaller shares even the SMs out.  Not more than there are steps for their warps.
+    // is not known here, and smaller shares even the SMs out.  Not more than there are steps for their warps.  Sixteen start 11 us later
+    // (four sequences, window 1024: 8.3 -> 19.1 us): only where eight leave the GPU idle and a warp has 64 steps and more (65536 keys, 8 key
+    // heads 59.5 -> 46.6 us, 115200 keys, one 97 -> 52).
     const int64_t longest = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N;
     const int64_t steps = ((longest < a.g.N_kv ? longest : a.g.N_kv) + KS - 1) / KS;
+    const auto idle = [&](int c) { return (int64_t)c * blocks * heads < 2 * a.num_sms; };
+    const auto long_shares = [&](int c) { return steps > (int64_t)c * kWarps * 64; };
     int C = 1;
-    while (C < kMaxCluster && (int64_t)C * kWarps < steps && ((int64_t)C * blocks * heads < 2 * a.num_sms || steps > (int64_t)C * kWarps * 64)) C *= 2;
+    while (C < 8 && (int64_t)C * kWarps < steps && (idle(C) || long_shares(C))) C *= 2;
+    if (C == 8 && idle(8) && long_shares(8)) C = 16;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)C, blocks, heads);
     cfg.blockDim = dim3(kWarps * 32);
@@ -350,7 +357,12 @@ cudaError_t launch(const WindowArgs& a, const bsa_view_t& K, const bsa_view_t& V
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, tk, tv, p);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, C > 8 ? wide_kernel : kernel, tk, tv, p);
+    if (e != cudaSuccess && C > 8) {  // no place for sixteen on this GPU
+        cudaGetLastError();
+        cfg.gridDim.x = attr[0].val.clusterDim.x = 8;
+        e = cudaLaunchKernelEx(&cfg, kernel, tk, tv, p);
+    }
     if (e == cudaSuccess) count_launch();
     return e;
 }

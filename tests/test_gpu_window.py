@@ -83,6 +83,7 @@ FEW = [
     (2, 2, 2, 3, 777, 20, 5, 33, [300, -1], [777, 400]),               # sinks end inside a step, windows inside others
     (1, 16, 16, 1, 20000, -1, 0, 0, None, None),
     (2, 3, 3, 1, 64, 8, 0, 2, [0, 0], [0, 1]),                         # no keys; one key
+    (2, 2, 1, 1, 110000, -1, 0, 0, [109998, 70000], [109999, 70001]),  # clusters of sixteen
     (1, 4, 1, 8, 600, 590, 0, 1, None, None),                          # 32 rows of different windows
     (1, 4, 1, 9, 600, 590, 0, 1, None, None),                          # 36: three blocks, the last of four rows
     (1, 2, 1, 32, 900, 130, 40, 20, [780], [800]),                     # 64, the last rows at no position

@@ -270,7 +270,8 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const int r = threadIdx.x;
         float M = -INFINITY, L = 0.f;
         for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w][r]);
-        for (int w = 0; w < kWarps; ++w) L += wm[w][r] == -INFINITY ? 0.f : wl[w][r] * ex2_approx(wm[w][r] - M);
+        // (a maximum of -inf: nothing seen, the sum is zero, or nothing but NaN, which the maximum passes over and the sum keeps)
+        for (int w = 0; w < kWarps; ++w) L += wm[w][r] == -INFINITY ? wl[w][r] : wl[w][r] * ex2_approx(wm[w][r] - M);
         cml[r] = make_float2(M, L);
     }
     __syncthreads();
@@ -308,7 +309,9 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         if (row < p.n_rows) {
             const int n = row / p.g.group, h = hk * p.g.group + (row - n * p.g.group);
             const int at = seq.start + n;
-            const bool any = at >= 0 && at < seq.len && L > 0.f;  // (steps that the rows of the sequence see whole are not masked)
+            // Decided by the position alone: a row at a position sees its own key at least, and a sum that is NaN belongs to its outputs.
+            // (A row at none may have a sum: steps that the rows of the sequence see whole are not masked.)
+            const bool any = at >= 0 && at < seq.len;
             const float inv = any ? 1.f / L : 0.f;
             *reinterpret_cast<uint32_t*>(p.O + (long long)b * p.o_batch + (long long)h * p.o_head + (long long)n * p.o_row + c) =
                 any ? pack_16x2<F16>(v0 * inv, v1 * inv) : 0u;

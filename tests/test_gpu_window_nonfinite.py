@@ -1,0 +1,59 @@
+"""NaN and infinities where a row of windowed attention sees them: they belong to that row's outputs, and to no other row's."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_25869_b200 import bsa
+from tests import window_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def tensors(seed, b, h, hk, n, nk, d, dtype=torch.bfloat16):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return [torch.empty(s, device="cuda", dtype=dtype).normal_(0, 1, generator=g) for s in ((b, h, n, d), (b, hk, nk, d), (b, hk, nk, d))]
+
+
+def check(q, k, v, clean, hit, **kw):
+    """Rows of ``hit`` [batch, heads, N] are NaN in O and LSE; the others have the bits of the clean call."""
+    O, L = bsa.window_forward(q, k, v, **kw)
+    assert torch.isnan(O[hit]).all() and torch.isnan(L[hit]).all()
+    assert torch.equal(O[~hit], clean[0][~hit]) and torch.equal(L[~hit], clean[1][~hit])
+
+
+# (batch, heads, key heads, rows, keys): one CTA, clusters of several sizes, of sixteen; rows of several heads and windows in one block
+FEW = [(1, 1, 1, 1, 40), (2, 8, 2, 1, 700), (1, 4, 1, 8, 900), (1, 8, 2, 4, 20000), (1, 1, 1, 1, 110000)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", FEW, ids=lambda s: "x".join(map(str, s)))
+def test_a_row_of_few_that_sees_a_nan(size, d):
+    b, h, hk, n, nk = size
+    q, k, v = tensors(31, b, h, hk, n, nk, d)
+    kw = dict(left=nk - 20, right=0, sinks=3)
+    clean = bsa.window_forward(q, k, v, **kw)
+    sees = R.sees(n, nk, b, nk - 20, 0, 3, None, None, "cuda")
+    bad = q.clone()  # a query with one NaN
+    bad[-1, -1, -1, 5] = math.nan
+    hit = torch.zeros(b, h, n, dtype=torch.bool, device="cuda")
+    hit[-1, -1, -1] = True
+    check(bad, k, v, clean, hit, **kw)
+    for j in (0, nk // 2, nk - n, nk - 1):  # one key of one key head
+        bad = k.clone()
+        bad[0, 0, j, -1] = math.nan
+        hit = torch.zeros(b, h, n, dtype=torch.bool, device="cuda")
+        hit[0, :h // hk] = sees[0, :, j]
+        check(q, bad, v, clean, hit, **kw)
+    bad = torch.full_like(k, math.nan)  # nothing but NaN: no maximum at all
+    check(q, bad, v, clean, torch.ones(b, h, n, dtype=torch.bool, device="cuda"), **kw)
+    bad = torch.where(torch.arange(nk, device="cuda")[:, None] == nk - n, math.inf, k.abs())  # an infinite score of every row
+    check(q.abs(), bad, v, clean, torch.ones(b, h, n, dtype=torch.bool, device="cuda"), **kw)
+    part = dict(kw, kv_len=ints([nk] * (b - 1) + [0]))  # no keys: still nothing seen, whatever the query holds
+    O, L = bsa.window_forward(torch.full_like(q, math.nan), k, v, **part)
+    assert not O[-1].any() and (L[-1] == -math.inf).all()

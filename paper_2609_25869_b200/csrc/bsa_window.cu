@@ -335,9 +335,9 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             const float m_other = mfin[tw], l_other = lfin[g & 1][tw];
             const float l = lfin[(g & 1) ^ 1][tw] + (m_other == m ? l_other : l_other * ex2_approx(m_other - m));
             mbar_arrive(smem_u32(&bars.e_taken));
-            const bool any = seen && l > 0.f;
-            const float inv = any ? 1.f / l : 0.f;
-            if (row_ok) *lse_out = any ? fmaf(m - kShift<F16>, 0.6931471805599453f, logf(l)) : -INFINITY;
+            // (a row at a position sees its own key at least: its sum is above zero, or NaN, which belongs to its outputs)
+            const float inv = seen ? 1.f / l : 0.f;
+            if (row_ok) *lse_out = seen ? fmaf(m - kShift<F16>, 0.6931471805599453f, logf(l)) : -INFINITY;
             m = m_next;
             if (!mbar_wait_warp(smem_u32(&bars.o_full), n_it & 1, abortp)) break;
             ++n_it;

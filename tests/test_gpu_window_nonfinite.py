@@ -57,3 +57,34 @@ def test_a_row_of_few_that_sees_a_nan(size, d):
     part = dict(kw, kv_len=ints([nk] * (b - 1) + [0]))  # no keys: still nothing seen, whatever the query holds
     O, L = bsa.window_forward(torch.full_like(q, math.nan), k, v, **part)
     assert not O[-1].any() and (L[-1] == -math.inf).all()
+
+
+# (batch, heads, key heads, rows, keys, left, right, sinks): whole tiles, edges on every tile, several items per CTA
+TILES = [(1, 2, 1, 300, 300, -1, 0, 0), (2, 4, 2, 400, 1000, 200, 60, 5), (1, 40, 40, 900, 900, 130, 0, 140)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", TILES, ids=lambda s: "x".join(map(str, s)))
+def test_a_row_of_a_tile_that_sees_a_nan(size, d, dtype):
+    b, h, hk, n, nk, left, right, sinks = size
+    q, k, v = tensors(32, b, h, hk, n, nk, d, dtype)
+    kw = dict(left=left, right=right, sinks=sinks)
+    clean = bsa.window_forward(q, k, v, **kw)
+    sees = R.sees(n, nk, b, left, right, sinks, None, None, "cuda")
+    bad = q.clone()
+    hit = torch.zeros(b, h, n, dtype=torch.bool, device="cuda")
+    for row in (0, 130, n - 1):
+        bad[-1, -1, row, 5] = math.nan
+        hit[-1, -1, row] = True
+    check(bad, k, v, clean, hit, **kw)
+    for j in (0, nk // 2, nk - 1):
+        bad = k.clone()
+        bad[0, 0, j, -1] = math.nan
+        hit = torch.zeros(b, h, n, dtype=torch.bool, device="cuda")
+        hit[0, :h // hk] = sees[0, :, j]
+        check(q, bad, v, clean, hit, **kw)
+    check(q, torch.full_like(k, math.nan), v, clean, torch.ones(b, h, n, dtype=torch.bool, device="cuda"), **kw)
+    part = dict(kw, q_start=ints([0] * b), kv_len=ints([nk] * (b - 1) + [150]))  # rows behind the length: nothing seen, whatever they hold
+    O, L = bsa.window_forward(torch.full_like(q, math.nan), k, v, **part)
+    assert not O[-1, :, 150:].any() and (L[-1, :, 150:] == -math.inf).all() and torch.isnan(L[-1, :, :150]).all()

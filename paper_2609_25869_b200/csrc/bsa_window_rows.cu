@@ -300,10 +300,11 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         for (int q = 0; q < MAX_C; ++q) M = fmaxf(M, ml[q].x);
 #pragma unroll
         for (int q = 0; q < MAX_C; ++q) {
-            const float f = (q >= C || ml[q].x == -INFINITY) ? 0.f : ex2_approx(ml[q].x - M);
-            L = fmaf(f, ml[q].y, L);
-            v0 = fmaf(f, v[q].x, v0);
-            v1 = fmaf(f, v[q].y, v1);
+            const float f = ml[q].x == -INFINITY ? 0.f : ex2_approx(ml[q].x - M);
+            const bool own = q < C;  // (left out, not taken times zero: an infinite sum would become NaN)
+            L = own ? fmaf(f, ml[q].y, L) : L;
+            v0 = own ? fmaf(f, v[q].x, v0) : v0;
+            v1 = own ? fmaf(f, v[q].y, v1) : v1;
         }
         const int row = row0 + r;
         if (row < p.n_rows) {

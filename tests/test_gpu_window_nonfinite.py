@@ -88,3 +88,20 @@ def test_a_row_of_a_tile_that_sees_a_nan(size, d, dtype):
     part = dict(kw, q_start=ints([0] * b), kv_len=ints([nk] * (b - 1) + [150]))  # rows behind the length: nothing seen, whatever they hold
     O, L = bsa.window_forward(torch.full_like(q, math.nan), k, v, **part)
     assert not O[-1, :, 150:].any() and (L[-1, :, 150:] == -math.inf).all() and torch.isnan(L[-1, :, :150]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", FEW, ids=lambda s: "x".join(map(str, s)))
+def test_an_infinite_value_that_a_row_of_few_sees(size, d):
+    """In its own column only, with its sign: the weights of all keys are above zero, so the sum is infinite, not NaN."""
+    b, h, hk, n, nk = size
+    q, k, v = tensors(33, b, h, hk, n, nk, d)
+    kw = dict(left=-1, right=-1, scale=1e-3)
+    O, L = bsa.window_forward(q, k, v, **kw)
+    for j in (0, nk - 1):
+        bad = v.clone()
+        bad[0, 0, j, 3], bad[0, 0, j, d - 2] = math.inf, -math.inf
+        want = O.clone()
+        want[0, :h // hk, :, 3], want[0, :h // hk, :, d - 2] = math.inf, -math.inf
+        O2, L2 = bsa.window_forward(q, k, bad, **kw)
+        assert torch.equal(O2, want) and torch.equal(L2, L)

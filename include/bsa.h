@@ -401,8 +401,7 @@ BSA_API bsa_status_t bsa_rope(const bsa_rope_desc_t* desc, const bsa_view_t* Q, 
  *   dK and dV summed over the query heads that share a key head and written for all N_kv rows (zero where nothing sees the
  *   key).  workspace_dev: bsa_window_workspace_bytes(desc) bytes of device memory on a 256-byte boundary, the call's own until its
  *   work on the stream is done (calls that may overlap each bring their own).
- * A bounded device wait that expires ends the kernel with BSA_ERR_DEVICE_TIMEOUT in bsa_window_status; it never hangs.  (The limit is
- * about a second; bsa_debug_set_wait_limit sets that of the plans' kernels only.)
+ * A bounded device wait that expires ends the kernel with BSA_ERR_DEVICE_TIMEOUT in bsa_window_status; it never hangs.
  * Errors: INVALID_ARG (null, misaligned or overlapping strides, sizes below one, left or right below -1, sinks below 0, heads not
  * a multiple of heads_kv, workspace too small), UNSUPPORTED (d not 64 or 128, N or N_kv above 2^29, more than 65535
  * sequences x heads), CUDA.
@@ -496,14 +495,16 @@ BSA_API void bsa_force_plan(int plan_id);
 /* ---------------------------------------------------------------------------------------------
  * Test hooks for the give-up path of the kernels' bounded waits (no counterpart in the paper).
  * Every wait inside the attention kernels (on a copy, an MMA, another warp) has a limit in SM clock
- * cycles; when it runs out the CTA records BSA_ERR_DEVICE_TIMEOUT in the plan's device_status, lets
+ * cycles; when it runs out the CTA records BSA_ERR_DEVICE_TIMEOUT in the plan's device_status (windowed
+ * attention: in the word that bsa_window_status reads), lets
  * its copies in flight land, frees its tensor memory and returns.  Both settings are per device
  * (the current one), apply to forwards launched afterwards, and synchronise the device.
  *   bsa_debug_set_wait_limit(cycles)   : the limit; <= 0 restores the default (2e9 cycles, about 1 s).
  *   bsa_debug_withhold_arrival(on)     : while on, the ping-pong kernel's V producer leaves out the
  *                                        copy of each CTA's first tile and the arrival announcing it,
  *                                        so the waits behind it run out.  Nothing faults; O and LSE
- *                                        of such a forward are undefined.
+ *                                        of such a forward are undefined.  The windowed kernels do the
+ *                                        same with V, and with dO where dK and dV are computed.
  */
 BSA_API bsa_status_t bsa_debug_set_wait_limit(long long cycles);
 /* Measurement hook: launches the Split-K reduction kernel of a plan alone on `stream`, over the partial results the

@@ -2816,10 +2816,13 @@ extern "C" __attribute__((visibility("default"))) int bsa_debug_trace_copy(long 
 // Test hooks: the limit of the bounded device waits, and the withheld arrival described at g_withhold_arrival.
 extern "C" __attribute__((visibility("default"))) bsa_status_t bsa_debug_set_wait_limit(long long cycles) {
     const long long v = cycles > 0 ? cycles : 2000000000ll;
-    return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &v, sizeof v) == cudaSuccess ? BSA_OK : BSA_ERR_CUDA;
+    return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &v, sizeof v) == cudaSuccess && set_window_wait_limit(v) == cudaSuccess &&
+                   set_window_rows_wait_limit(v) == cudaSuccess && set_window_bwd_wait_limit(v) == cudaSuccess
+               ? BSA_OK : BSA_ERR_CUDA;
 }
 extern "C" __attribute__((visibility("default"))) bsa_status_t bsa_debug_withhold_arrival(int on) {
     const int v = on ? 1 : 0;
+    set_window_withhold(on != 0);
     return cudaMemcpyToSymbol(g_withhold_arrival, &v, sizeof v) == cudaSuccess ? BSA_OK : BSA_ERR_CUDA;
 }
 

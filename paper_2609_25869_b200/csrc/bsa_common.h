@@ -141,6 +141,14 @@ int rb_max_chunk(int d);  // largest T_KV (keys per staged chunk) for head dimen
 int attention_max_stages(int d, int T_KV, int kernel);
 int attention_smem_bytes(int d, int T_KV, int stages, int kernel);
 
+// The windowed kernels' part of the test hooks for bounded waits: the limit (each source file's kernels have their own copy), and whether
+// calls leave out the copy of every CTA's (few rows: warp's) first tile of V, or of dO in the kernel for dK and dV.
+cudaError_t set_window_wait_limit(long long cycles);
+cudaError_t set_window_rows_wait_limit(long long cycles);
+cudaError_t set_window_bwd_wait_limit(long long cycles);
+void set_window_withhold(bool on);
+bool window_withhold();
+
 void count_launch(int n = 1);
 void set_cuda_err(cudaError_t e, const char* where);  // what bsa_last_cuda_error reports to this thread
 

@@ -58,6 +58,7 @@ struct Params {
     float* LSE;
     int o_wide;        // rows of O lie on 32-byte boundaries
     float scale_log2;  // scale * log2(e)
+    int withhold;      // test hook: no copy of the first tile of V
     ItemOrder order;       // 128-row tiles, from a sequence's last to its first
     Divisor heads, group;  // heads; heads that share a key head
 };
@@ -101,24 +102,6 @@ template <int R>
 __device__ __forceinline__ void reg_dec() {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R));
 }
-
-// after a wait gave up: copies in flight land before the CTA's shared memory goes away
-__device__ __forceinline__ void let_copies_land() {
-    const uint64_t t0 = globaltimer_ns();
-    while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-}
-
-struct Ring {
-    int stage = 0;
-    uint32_t phase = 0;
-    template <int DEPTH>
-    __device__ __forceinline__ void advance() {
-        if (++stage == DEPTH) {
-            stage = 0;
-            phase ^= 1u;
-        }
-    }
-};
 
 // P of 32 keys in the place of their scores: exp2(s * c2 + neg_m), rounded and packed by pairs; its unrounded sum.
 template <bool F16>
@@ -389,7 +372,6 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     tma_load_rows(smem_u32(sK) + ring.stage * C::kTile, &tmK, bar, it.tiles.tile(j) * kWinT, hk, it.b);
                 }
             }
-            if (!ok) let_copies_land();
         } else if (warp == 11) {
             // =========================== V producer ===========================
             // A tile with keys that no row sees lands at a barrier of its own; it is handed on once they are zero, behind the next tile's copy.
@@ -408,7 +390,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 held = -1;
                 return true;
             };
-            bool ok = true;
+            bool ok = true, first = true;
             for (int k = 0; ok && load_item(p, k, it); ++k) {
                 const int n = it.tiles.count(), hk = it.hk;
                 for (int j = 0; j < n; ++j, ring.advance<C::kV>()) {
@@ -417,11 +399,12 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     ok = mbar_wait_warp(smem_u32(&bars.v_empty[ring.stage]), ring.phase ^ 1, abortp);
                     if (!ok) break;
                     const bool unseen = has_unseen_keys(p.g, it.range, key0);
-                    if (lane == 0) {
+                    if (lane == 0 && !(p.withhold && first)) {
                         const uint32_t bar = smem_u32(unseen ? &bars.v_land[ring.stage] : &bars.v_full[ring.stage]);
                         mbar_arrive_expect_tx(bar, C::kTile);
                         tma_load_rows(smem_u32(sV) + ring.stage * C::kTile, &tmV, bar, key0, hk, it.b);
                     }
+                    first = false;
                     ok = hand_on();
                     if (!ok) break;
                     if (unseen) {
@@ -431,8 +414,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     }
                 }
             }
-            ok = ok && hand_on();
-            if (!ok && lane == 0) let_copies_land();
+            if (ok) hand_on();
         } else if (warp == 9) {
             // =========================== Q K^T issuer ===========================
             // (Here and below the whole warp walks through the loop and one elected lane issues: with uniform control flow the
@@ -567,9 +549,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         }
     }
 
-    tc_fence_before();
-    __syncthreads();
-    if (tid == 0 && abort_flag) atomicExch(&g_window_status, (int)BSA_ERR_DEVICE_TIMEOUT);
+    end_of_cta(abortp, &g_window_status);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 
@@ -594,6 +574,11 @@ cudaError_t launch_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view
 }
 
 }  // namespace
+
+cudaError_t set_window_wait_limit(long long cycles) { return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &cycles, sizeof cycles); }
+static std::atomic<bool> g_withhold{false};
+void set_window_withhold(bool on) { g_withhold.store(on, std::memory_order_relaxed); }
+bool window_withhold() { return g_withhold.load(std::memory_order_relaxed); }
 
 cudaError_t window_status_word(int device, int** out) {
     static std::atomic<int*> word[kMaxDevices];
@@ -656,6 +641,7 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     p.LSE = LSE;
     p.o_wide = view_is_wide(*O, a.g.batch, a.g.heads, a.g.N);
     p.scale_log2 = a.scale * 1.4426950408889634f;
+    p.withhold = window_withhold();
     const int n_qt = (a.g.N + kWinT - 1) / kWinT;
     if ((int64_t)n_qt * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
     p.order = ItemOrder(n_qt, cut_tiles(a.g, n_qt), a.g.batch * a.g.heads);

@@ -60,6 +60,7 @@ struct BwdParams {
     int wide_q, wide_k, wide_v;             // gradients whose rows lie on 32-byte boundaries
     float* partial;        // [batch * heads_kv][sink_tiles][sink_shares][dV, dK][128][D]
     int* status;
+    int withhold;          // test hook: no copy of the first tile of V (dQ) or of dO (dK, dV)
 };
 
 struct __align__(8) DqBarriers {
@@ -71,27 +72,12 @@ struct __align__(8) DkvBarriers {
     uint64_t s_full, dp_full, p_ready[2], ds_ready, acc_full, acc_free;
 };
 
-__device__ __forceinline__ void let_copies_land() {
-    const uint64_t t0 = globaltimer_ns();
-    while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-}
 // 1-D copy of whole 16-byte pieces, counted in bytes on an mbarrier
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                  : "memory");
 }
-struct Ring {
-    int stage = 0;
-    uint32_t phase = 0;
-    template <int DEPTH>
-    __device__ __forceinline__ void advance() {
-        if (++stage == DEPTH) {
-            stage = 0;
-            phase ^= 1u;
-        }
-    }
-};
 // The k-th item of a persistent CTA, dealt in alternating directions (the longest items come first).
 __device__ __forceinline__ int item_index(int k) {
     const int G = gridDim.x;
@@ -264,12 +250,13 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                     if (j + 1 < n) ok = copy_k(j + 1);
                     ok = ok && mbar_wait(smem_u32(&bars.v_empty), (n_v & 1) ^ 1, abortp);
                     if (!ok) break;
-                    mbar_arrive_expect_tx(smem_u32(&bars.v_full), C::kTile);
-                    tma_load_rows(smem_u32(sV), &tmV, smem_u32(&bars.v_full), it.tiles.tile(j) * kWinT, it.hk, it.b);
+                    if (!(p.withhold && n_v == 0)) {
+                        mbar_arrive_expect_tx(smem_u32(&bars.v_full), C::kTile);
+                        tma_load_rows(smem_u32(sV), &tmV, smem_u32(&bars.v_full), it.tiles.tile(j) * kWinT, it.hk, it.b);
+                    }
                     ++n_v;
                 }
             }
-            if (!ok) let_copies_land();
         }
     } else if (warp == 9) {
         // Tile t (counted over the CTA's items) belongs to softmax warpgroup t mod 2 and has dP buffer t mod 2, where its dS goes as
@@ -430,9 +417,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             }
         }
     }
-    tc_fence_before();
-    __syncthreads();
-    if (tid == 0 && abort_flag) atomicExch(p.status, (int)BSA_ERR_DEVICE_TIMEOUT);
+    end_of_cta(abortp, p.status);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 
@@ -590,11 +575,11 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                     bulk_load(rows + kWinT * 4, p.neg_delta + from, kWinT * 4, bar);
                     ok = mbar_wait(smem_u32(&bars.o_empty[ring.stage]), ring.phase ^ 1, abortp);
                     if (!ok) break;
+                    if (p.withhold && n_it == 1 && i == 0) continue;
                     mbar_arrive_expect_tx(smem_u32(&bars.o_full[ring.stage]), C::kTile);
                     tma_load_rows(smem_u32(sG) + ring.stage * C::kTile, &tmG, smem_u32(&bars.o_full[ring.stage]), row, h, it.b);
                 }
             }
-            if (!ok) let_copies_land();
         }
     } else if (warp == 9) {
         // Order: S(0), dP(0); then for every tile i: dV(i) behind its P, S(i + 1) in the place of that P, dK(i) behind its dS,
@@ -812,9 +797,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             }
         }
     }
-    tc_fence_before();
-    __syncthreads();
-    if (tid == 0 && abort_flag) atomicExch(p.status, (int)BSA_ERR_DEVICE_TIMEOUT);
+    end_of_cta(abortp, p.status);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 
@@ -916,6 +899,8 @@ cudaError_t launch(const WindowArgs& a, const Layout& l, const bsa_view_t& Q, co
 }  // namespace
 }  // namespace bsa
 
+cudaError_t bsa::set_window_bwd_wait_limit(long long cycles) { return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &cycles, sizeof cycles); }
+
 using namespace bsa;
 
 extern "C" int64_t bsa_window_workspace_bytes(const bsa_window_desc_t* t) {
@@ -969,6 +954,7 @@ extern "C" bsa_status_t bsa_window_backward(const bsa_window_desc_t* t, const bs
     p.wide_v = view_is_wide(*dV, a.g.batch, a.g.heads_kv, a.g.N_kv);
     p.sink_tiles = l.sink_tiles;
     p.sink_shares = l.sink_shares;
+    p.withhold = window_withhold();
     cudaError_t e = window_status_word(a.device, &p.status);
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
     if (e == cudaSuccess)

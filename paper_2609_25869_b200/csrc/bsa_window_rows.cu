@@ -42,6 +42,7 @@ struct RowsParams {
     long long q_batch, q_head, q_row, o_batch, o_head, o_row;
     float scale_log2;
     int n_rows;  // N * group
+    int withhold;  // test hook: no copy of a warp's first tile of V
     int* status;
 };
 
@@ -102,7 +103,7 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     if (lane == 0) {
         for (int i = 0; i < kSlots && first + i < last; ++i) {
             copy_in(sK + i * kSlot, &tmK, bK + i * 8, key_of(first + i));
-            copy_in(sV + i * kSlot, &tmV, bV + i * 8, key_of(first + i));
+            if (!(p.withhold && i == 0)) copy_in(sV + i * kSlot, &tmV, bV + i * 8, key_of(first + i));
         }
     }
     // Q fragments (A operand, row-major 16 x 16 per step) of rows gid and gid + 8
@@ -235,10 +236,7 @@ window_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             phase ^= 1u;
         }
     }
-    if (!ok) {  // copies in flight land before the shared memory is used for anything else
-        const uint64_t t0 = globaltimer_ns();
-        while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-    }
+    if (!ok) let_copies_land();  // before the rings are used for anything else (a warp that came to its end has waited for all of its own)
     // ---- join the warps: weights first, then the rows, scaled, into shared memory ----
     l_lo += __shfl_xor_sync(kAll, l_lo, 1);
     l_hi += __shfl_xor_sync(kAll, l_hi, 1);
@@ -373,6 +371,8 @@ cudaError_t launch(const WindowArgs& a, const bsa_view_t& K, const bsa_view_t& V
 
 }  // namespace
 
+cudaError_t set_window_rows_wait_limit(long long cycles) { return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &cycles, sizeof cycles); }
+
 cudaError_t launch_window_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
                                float* LSE, cudaStream_t stream) {
     RowsParams p = {};
@@ -384,6 +384,7 @@ cudaError_t launch_window_rows(const WindowArgs& a, const bsa_view_t& Q, const b
     p.o_batch = O.batch; p.o_head = O.head; p.o_row = O.row;
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.n_rows = a.g.N * a.g.group;
+    p.withhold = window_withhold();
     const cudaError_t e = window_status_word(a.device, &p.status);
     if (e != cudaSuccess) return e;
     return a.d == 64 ? (a.f16 ? launch<64, true>(a, K, V, p, stream) : launch<64, false>(a, K, V, p, stream))

@@ -24,6 +24,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <mutex>
 
 #include "bsa_window.cuh"
 
@@ -34,6 +35,9 @@ using namespace ptx;
 namespace {
 
 __device__ int g_window_status = 0;
+__device__ int g_window_taken = 0;
+// Read and cleared in one step: what a call of another thread sets meanwhile is left for the next look.
+__global__ void take_window_status() { g_window_taken = atomicExch(&g_window_status, 0); }
 
 constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;
@@ -675,14 +679,18 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
 
 extern "C" bsa_status_t bsa_window_status(int* status_out) {
     if (!status_out) return BSA_ERR_INVALID_ARG;
-    int* word = nullptr;
     int v = 0;
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e == cudaSuccess && device >= kMaxDevices) return BSA_ERR_CUDA;
-    if (e == cudaSuccess) e = window_status_word(device, &word);
-    if (e == cudaSuccess) e = cudaMemcpy(&v, word, sizeof v, cudaMemcpyDeviceToHost);
-    if (e == cudaSuccess && v != 0) e = cudaMemset(word, 0, sizeof v);
+    static std::mutex one_look;  // of a process at a time: g_window_taken is the look's
+    const std::lock_guard<std::mutex> lock(one_look);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();  // (a copy alone is not ordered behind non-blocking streams)
+    if (e == cudaSuccess) {
+        take_window_status<<<1, 1>>>();
+        e = cudaGetLastError();
+    }
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&v, g_window_taken, sizeof v);
     if (e != cudaSuccess) {
         set_cuda_err(e, "bsa_window_status");
         return BSA_ERR_CUDA;

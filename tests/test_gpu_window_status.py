@@ -46,3 +46,23 @@ def test_a_wait_that_runs_out_ends_in_a_status_not_a_hang(n, nk, left, d):
     G2 = bsa.window_backward(q, k, v, O, L, g, **kw)
     assert bsa.window_status() == 0
     assert torch.equal(O, O2) and torch.equal(L, L2) and all(torch.equal(a, b) for a, b in zip(G, G2))
+
+
+@pytest.mark.parametrize("n", [2, 300])
+def test_the_status_waits_for_streams_that_do_not_block(n):
+    """A look behind calls on a side stream, while that stream still has work in front of them, is a look at them."""
+    q, k, v, g = tensors(n, 600, 64)
+    bsa.window_forward(q, k, v, left=50)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with withheld_tiles():
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(400_000_000)  # about 0.2 s
+            O, L = bsa.window_forward(q, k, v, left=50)
+        assert bsa.window_status() == TIMEOUT and side.query()
+        assert bsa.window_status() == 0
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)
+        O, L = bsa.window_forward(q, k, v, left=50)
+        bsa.window_backward(q, k, v, O, L, g, left=50)
+    assert bsa.window_status() == 0 and side.query()

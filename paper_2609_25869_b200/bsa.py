@@ -165,6 +165,16 @@ def _stream_ptr(stream) -> Optional[int]:
     return getattr(stream, "cuda_stream", stream) or None
 
 
+def _pool(stream, dev: int):
+    """Context in which a call on ``stream`` (a torch stream or a handle) allocates: its memory comes from that stream's pool.  From the
+    current stream's it could be memory that work queued there is still using, and be handed out again while ``stream`` writes it."""
+    import torch
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream_ptr(stream)
+        stream = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
+    return torch.cuda.stream(stream)
+
+
 def _lse_shape(Q, layout: str):
     """[heads, N] for Q stored [heads, N, d], [N, heads, d] or, batched and token-major, [batch, N, heads/batch, d]."""
     if layout == "hnd":
@@ -451,7 +461,8 @@ def rope(Q, K=None, *, axes, positions=None, grid=None, first: int = 0, origin=N
     ``positions``, int32 ``[N, len(axes)]`` or ``[batch, N, len(axes)]``, or ``grid`` = the axes' lengths: the tokens from
     ``first`` on stand on it row-major, ``origin`` added, and the others stay as they are.  ``freq``: the pairs' own
     frequencies instead of ``theta``'s.  ``inverse=True`` is the way back: gradients, or positions taken off.
-    ``out``: the tensors to write (``(Q, K)`` themselves for in place), e.g. views of a cache."""
+    ``out``: the tensors to write (``(Q, K)`` themselves for in place), e.g. views of a cache.
+    ``stream``: a torch stream or a handle; fresh outputs come from its pool, as if allocated with it current."""
     nhd = LAYOUTS[layout] == 1
     dt, dev = _tensor_of(Q, "Q")
     dtype = Q.dtype
@@ -462,10 +473,13 @@ def rope(Q, K=None, *, axes, positions=None, grid=None, first: int = 0, origin=N
         if bk != b or nk != n or dk != d:
             raise ValueError("Q and K have to agree in batch, tokens and channels")
     if out is None:
-        oq = _torch.empty_like(Q)
+        if stream is None:
+            oq, ok = _torch.empty_like(Q), None if K is None else _torch.empty_like(K)
+        else:
+            with _pool(stream, dev):
+                oq, ok = _torch.empty_like(Q), None if K is None else _torch.empty_like(K)
         voq = _fresh_view(oq, Q, nhd, dtype, dev, vq)
         if K is not None:
-            ok = _torch.empty_like(K)
             vok = _fresh_view(ok, K, nhd, dtype, dev, vk)
     else:
         oq, ok = (out, None) if K is None else out
@@ -521,20 +535,26 @@ def window_forward(Q, K, V, *, left: int, right: int = 0, sinks: int = 0, q_star
     Q ``[heads, N, d]`` or ``[batch, heads, N, d]``, K and V likewise with ``heads_kv`` heads and ``N_kv`` tokens
     (``layout="nhd"``: heads behind tokens); any strides that are multiples of 8 elements.  ``q_start``, ``kv_len``: int32
     CUDA tensors ``[batch]``, each sequence's first query position and its number of keys (default: the queries are the last N
-    of N_kv positions).  LSE is fp32 ``[batch, heads, N]`` (``[heads, N]``) in either layout."""
+    of N_kv positions).  LSE is fp32 ``[batch, heads, N]`` (``[heads, N]``) in either layout.  ``stream``: as for ``rope``."""
     nhd = LAYOUTS[layout] == 1
     desc, vq, vk, vv, shape, dev = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, nhd)
-    if O is None:
-        O = _torch.empty_like(Q)
-        vo = _fresh_view(O, Q, nhd, Q.dtype, dev, vq)
-    else:
+    if O is not None:
         if O.shape != Q.shape:
             raise ValueError("O has to have the shape of Q")
         vo = _view(O, nhd, Q.dtype, dev, "O")[4]
-    if LSE is None:
-        LSE = Q.new_empty(shape, dtype=_torch.float32)
-    else:
+    if LSE is not None:
         _check_lse(LSE, shape, dev)
+    if O is None or LSE is None:
+        fresh = O is None
+        if stream is None:
+            O = _torch.empty_like(Q) if fresh else O
+            LSE = Q.new_empty(shape, dtype=_torch.float32) if LSE is None else LSE
+        else:
+            with _pool(stream, dev):
+                O = _torch.empty_like(Q) if fresh else O
+                LSE = Q.new_empty(shape, dtype=_torch.float32) if LSE is None else LSE
+        if fresh:
+            vo = _fresh_view(O, Q, nhd, Q.dtype, dev, vq)
     _call(dev, stream, "bsa_window_forward", lib().bsa_window_forward, desc, vq, vk, vv, vo, LSE.data_ptr())
     return O, LSE
 
@@ -548,18 +568,12 @@ def window_backward(Q, K, V, O, LSE, dO, *, left: int, right: int = 0, sinks: in
                     scale: float = 0.0, layout: str = "hnd", dQ=None, dK=None, dV=None, stream=None):
     """``bsa_window_backward``: ``(dQ, dK, dV)`` of ``window_forward`` from its inputs, its outputs and the gradient ``dO`` of
     ``O``; arguments as there.  dK and dV are summed over the query heads that share a key head.  The workspace comes from
-    torch's allocator, on the current stream or on ``stream`` (a torch stream)."""
+    torch's allocator, as the outputs do."""
     nhd = LAYOUTS[layout] == 1
     desc, vq, vk, vv, shape, dev = _window_desc(Q, K, V, left, right, sinks, q_start, kv_len, scale, nhd)
     if O.shape != Q.shape or dO.shape != Q.shape:
         raise ValueError("O and dO have to have the shape of Q")
     _check_lse(LSE, shape, dev)
-    empty = _torch.empty_like
-    dQ, dK, dV = empty(Q) if dQ is None else dQ, empty(K) if dK is None else dK, empty(V) if dV is None else dV
-    if dQ.shape != Q.shape or dK.shape != K.shape or dV.shape != K.shape:
-        raise ValueError("gradients have to have the shapes of their tensors")
-    views = [_view(t, nhd, Q.dtype, dev, n)[4] for t, n in ((O, "O"), (dO, "dO"), (dQ, "dQ"), (dK, "dK"), (dV, "dV"))]
-
     L = lib()
     if dev != _torch._C._cuda_getDevice():
         with _torch.cuda.device(dev):
@@ -567,11 +581,19 @@ def window_backward(Q, K, V, O, LSE, dO, *, left: int, right: int = 0, sinks: in
     else:
         n = L.bsa_window_workspace_bytes(desc)
     # (where the description is refused n is 0, and the call says why)
+
+    def allocate():
+        empty = _torch.empty_like
+        return (empty(Q) if dQ is None else dQ, empty(K) if dK is None else dK, empty(V) if dV is None else dV,
+                _torch.empty(n, dtype=_torch.uint8, device=Q.device))
     if stream is None:
-        ws = _torch.empty(n, dtype=_torch.uint8, device=Q.device)
-    else:  # the workspace's memory is free again when that stream has come past this call
-        with _torch.cuda.stream(stream):
-            ws = _torch.empty(n, dtype=_torch.uint8, device=Q.device)
+        dQ, dK, dV, ws = allocate()
+    else:  # (the workspace's memory is free again when that stream has come past this call)
+        with _pool(stream, dev):
+            dQ, dK, dV, ws = allocate()
+    if dQ.shape != Q.shape or dK.shape != K.shape or dV.shape != K.shape:
+        raise ValueError("gradients have to have the shapes of their tensors")
+    views = [_view(t, nhd, Q.dtype, dev, n)[4] for t, n in ((O, "O"), (dO, "dO"), (dQ, "dQ"), (dK, "dK"), (dV, "dV"))]
     _call(dev, stream, "bsa_window_backward", L.bsa_window_backward, desc, vq, vk, vv, views[0], LSE.data_ptr(), *views[1:], ws.data_ptr(), n)
     return dQ, dK, dV
 

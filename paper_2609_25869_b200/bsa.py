@@ -7,6 +7,7 @@ been built -- there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -184,6 +185,19 @@ def _lse_shape(Q, layout: str):
     return (Q.shape[1], Q.shape[0])
 
 
+def _fresh_outputs(Q, layout: str, O, LSE, stream):
+    """O and LSE of a plan's forward, those that are None allocated where ``stream`` (None: the current one) writes them."""
+    import torch
+    if stream is not None:
+        with _pool(stream, Q.get_device()):
+            return _fresh_outputs(Q, layout, O, LSE, None)
+    if O is None:
+        O = torch.empty_like(Q)
+    if LSE is None:  # [heads, N] whatever the layout of Q
+        LSE = Q.new_empty(_lse_shape(Q, layout), dtype=torch.float32)
+    return O, LSE
+
+
 class Plan:
     """Handle of a prepared plan (``bsa_plan_create`` ... ``bsa_plan_destroy``)."""
 
@@ -192,14 +206,13 @@ class Plan:
         self.layout = layout
 
     def forward(self, Q, K, V, O=None, LSE=None, stream=None):
-        """``bsa_forward``: Q, K, V are bf16 CUDA tensors ``[heads, N, d]``; returns ``(O, LSE)``."""
+        """``bsa_forward``: Q, K, V are bf16 CUDA tensors ``[heads, N, d]``; returns ``(O, LSE)``.  ``stream``: a torch stream or a
+        handle; fresh outputs come from its pool, as if allocated with it current."""
         import torch
         assert Q.is_cuda and Q.dtype in (torch.bfloat16, torch.float16) and Q.is_contiguous()  # as the plan's dtype
         assert K.is_contiguous() and V.is_contiguous() and K.dtype == V.dtype == Q.dtype
-        if O is None:
-            O = torch.empty_like(Q)
-        if LSE is None:  # [heads, N] whatever the layout of Q
-            LSE = Q.new_empty(_lse_shape(Q, self.layout), dtype=torch.float32)
+        if O is None or LSE is None:
+            O, LSE = _fresh_outputs(Q, self.layout, O, LSE, stream)
         _check(lib().bsa_forward(self._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), LSE.data_ptr(),
                                  _stream_ptr(stream)), "bsa_forward")
         return O, LSE
@@ -272,12 +285,9 @@ def request(mask, B_Q: int, B_KV: int, N: int, heads: int, d: int, Q, K, V, O=No
             max_workspace_bytes: int = 0, stream=None, N_kv: int = 0, dtype: str = "bf16", layout: str = "hnd",
             row_stride: int = 0):
     """``bsa_request_device``: plan create + forward in one call (CUDA tensors).  Returns ``(plan, O, LSE)``; the plan
-    can run further forwards and is given back with ``plan.destroy()``."""
-    import torch
-    if O is None:
-        O = torch.empty_like(Q)
-    if LSE is None:
-        LSE = Q.new_empty(_lse_shape(Q, layout), dtype=torch.float32)
+    can run further forwards and is given back with ``plan.destroy()``.  ``stream``: as for ``Plan.forward``."""
+    if O is None or LSE is None:
+        O, LSE = _fresh_outputs(Q, layout, O, LSE, stream)
     h = ctypes.c_void_p()
     opt = Options(plan_id, DTYPES[dtype], max_workspace_bytes, N_kv, LAYOUTS[layout], 0)
     _check(lib().bsa_request_device(mask.data_ptr(), row_stride, B_Q, B_KV, N, heads, d, Q.data_ptr(), K.data_ptr(),
@@ -611,11 +621,12 @@ NOALLOC_MAX_ROWS = 1 << 20
 def mask_stats_noalloc(mask, out=None, stream=None):
     """``bsa_mask_stats_noalloc``: statistics of a uint8/bool CUDA mask ``[heads, nQb, nKb]`` into an int64
     CUDA tensor of 4 entries, using the library's built-in scratch (no allocation inside the call when
-    ``out`` is given).  Returns ``out``; raises ``BsaError`` (UNSUPPORTED) beyond ``NOALLOC_MAX_ROWS`` rows."""
+    ``out`` is given; ``stream`` as for ``Plan.forward``).  Returns ``out``; raises ``BsaError`` (UNSUPPORTED) beyond ``NOALLOC_MAX_ROWS`` rows."""
     import torch
     assert mask.is_cuda and mask.is_contiguous() and mask.dtype in (torch.uint8, torch.bool) and mask.dim() == 3
     if out is None:
-        out = torch.empty(4, dtype=torch.int64, device=mask.device)
+        with contextlib.nullcontext() if stream is None else _pool(stream, mask.get_device()):
+            out = torch.empty(4, dtype=torch.int64, device=mask.device)
     assert out.is_cuda and out.dtype == torch.int64 and out.numel() >= 4 and out.is_contiguous()
     h, nq, nk = mask.shape
     _check(lib().bsa_mask_stats_noalloc(mask.data_ptr(), h, nq, nk, out.data_ptr(), _stream_ptr(stream)),

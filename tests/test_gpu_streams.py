@@ -41,3 +41,29 @@ def test_fresh_outputs_come_from_the_pool_of_the_stream_that_writes_them(op, han
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     got = calls[op](0 if handle else torch.cuda.default_stream())
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("op", ["forward", "request", "statistics"])
+def test_so_do_the_outputs_of_plans(op, handle):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(52)
+    h, n, d = 8, 4096, 128
+    q, k, v = [torch.empty((h, n, d), device="cuda", dtype=torch.bfloat16).normal_(0, 1, generator=g) for _ in range(3)]
+    mask = torch.ones((h, n // 64, n // 64), dtype=torch.uint8, device="cuda")
+    with bsa.plan_create(mask, 64, 64, n, h, d) as plan:
+        other = []
+
+        def request(s):
+            p, O, L = bsa.request(mask, 64, 64, n, h, d, q, k, v, stream=s)
+            other.append(p)
+            return O, L
+        calls = {"forward": lambda s: plan.forward(q, k, v, stream=s), "request": request,
+                 "statistics": lambda s: (bsa.mask_stats_noalloc(mask, stream=s),)}
+        want = calls[op](None)
+        sizes = [t.numel() * t.element_size() for t in want]
+        side = torch.cuda.Stream()
+        got = behind_queued_work(calls[op], sizes, side.cuda_stream if handle else side)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        for p in other:
+            p.destroy()

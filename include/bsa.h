@@ -332,7 +332,8 @@ BSA_API bsa_status_t bsa_mask_stats_noalloc(const uint8_t* mask_dev, int heads, 
  *
  * A view: element strides of a tensor [batch][heads][rows][d]; d is contiguous.  data must lie on a 16-byte boundary and
  * every stride of a dimension with more than one entry must be a positive multiple of 8 elements (16 bytes), else
- * INVALID_ARG (GPU untouched); strides of dimensions with one entry are ignored.  Entries of an output may not overlap.
+ * INVALID_ARG (GPU untouched); strides of dimensions with one entry are ignored.  Entries of an output may not overlap
+ * (INVALID_ARG as well; those of an input may).
  */
 typedef struct bsa_view {
     void* data;
@@ -358,7 +359,7 @@ enum { BSA_PAIRS_INTERLEAVED = 0, BSA_PAIRS_HALVES = 1 };
  * Angles are taken modulo one turn in 64-bit fixed point before anything is rounded, so that they hold at any int32
  * position; products and sums are fp32, rounded once to the element type.
  * Outputs may be the inputs themselves (same data and strides); any other overlap is not allowed.
- * Errors: INVALID_ARG (null or misaligned pointers, sizes below one, odd axis_dim, R > d, a grid that does not fit into N
+ * Errors: INVALID_ARG (null, misaligned or overlapping views, sizes below one, odd axis_dim, R > d, a grid that does not fit into N
  * tokens), UNSUPPORTED (d not a multiple of 8 or above 256, N above 2^29), CUDA.
  */
 typedef struct bsa_rope_desc {
@@ -402,7 +403,7 @@ BSA_API bsa_status_t bsa_rope(const bsa_rope_desc_t* desc, const bsa_view_t* Q, 
  *   key).  workspace_dev: bsa_window_workspace_bytes(desc) bytes of device memory on a 256-byte boundary, the call's own until its
  *   work on the stream is done (calls that may overlap each bring their own).
  * A bounded device wait that expires ends the kernel with BSA_ERR_DEVICE_TIMEOUT in bsa_window_status; it never hangs.
- * Errors: INVALID_ARG (null, misaligned or overlapping strides, sizes below one, left or right below -1, sinks below 0, heads not
+ * Errors: INVALID_ARG (null, misaligned or overlapping views, sizes below one, left or right below -1, sinks below 0, heads not
  * a multiple of heads_kv, workspace too small), UNSUPPORTED (d not 64 or 128, N or N_kv above 2^29, more than 65535
  * sequences x heads), CUDA.
  */

@@ -131,10 +131,11 @@ cudaError_t launch_forward_rb(const ForwardArgs& a, cudaStream_t stream, const c
 // Tensor map of K or V as {64 columns, N rows, d/64 column groups, heads}: a copy brings box_rows whole rows, 128-byte
 // swizzle, 64-column halves one after the other (defined with the other tensor maps).
 bool encode_kv_map(CUtensorMap* m, const void* base, int64_t N, int heads, int d, int box_rows, bool f16, bool nhd);
+// What bsa_view_t promises, for a tensor of these sizes, and what it promises besides for an output (defined with the rotary kernel).
+bool view_ok(const bsa_view_t* v, int64_t batch, int64_t heads, int64_t rows);
+bool view_overlaps(const bsa_view_t& v, int64_t batch, int64_t heads, int64_t rows, int d);
 // Tensor map of a strided [batch][heads][rows][d] view (strides in elements) as {64 columns, rows, d/64 column groups, heads, batch},
 // box {64, box_rows, d/64, 1, 1}: what the windowed kernels copy tiles with.
-// What bsa_view_t promises, for a tensor of these sizes (defined with the rotary kernel).
-bool view_ok(const bsa_view_t* v, int64_t batch, int64_t heads, int64_t rows);
 bool encode_view_map(CUtensorMap* m, const bsa_view_t& v, int64_t rows, int heads, int batch, int d, int box_rows, bool f16);
 int rb_max_chunk(int d);  // largest T_KV (keys per staged chunk) for head dimension d
 // `stages` counts K buffers plus V buffers for the paired kernel (kernel 1), K = V ring depth for kernel 0

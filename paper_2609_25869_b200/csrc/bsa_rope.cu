@@ -13,6 +13,8 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <algorithm>
+
 #include "bsa_common.h"
 #include "sm100_ptx.cuh"
 
@@ -183,6 +185,41 @@ bool view_ok(const bsa_view_t* v, int64_t batch, int64_t heads, int64_t rows) {
     return true;
 }
 
+// Whether two entries of a view (view_ok) share an element: for an output, whose entries different threads write.
+bool view_overlaps(const bsa_view_t& v, int64_t batch, int64_t heads, int64_t rows, int d) {
+    struct { int64_t n, s; } e[3];
+    int dims = 0;
+    const int64_t n[3] = {batch, heads, rows}, s[3] = {v.batch, v.head, v.row};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1) e[dims++] = {n[i], s[i]};
+    std::sort(e, e + dims, [](const auto& a, const auto& b) { return a.s < b.s; });
+    __int128 extent = d;  // of the dimensions so far
+    bool nested = true;   // each dimension steps over all of those with smaller strides: every ordinary layout
+    for (int i = 0; i < dims; ++i) {
+        nested = nested && e[i].s >= extent;
+        extent += (__int128)e[i].s * (e[i].n - 1);
+    }
+    if (nested) return false;
+    // Interleaved dimensions may still keep apart.  Two entries meet if their distance i * s0 + j * s1 + k * s2 is below d; of the most
+    // numerous dimension only the k nearest to it and its neighbour count, once its own stride is at least d.
+    std::sort(e, e + dims, [](const auto& a, const auto& b) { return a.n < b.n; });
+    while (dims < 3) {
+        for (int i = dims++; i > 0; --i) e[i] = e[i - 1];
+        e[0] = {1, 0};
+    }
+    if (e[2].s < d) return true;
+    if ((__int128)e[0].n * e[1].n > (1 << 23)) return true;  // (kept apart, 2^23 to the 3/2 rows of 16 bytes would not fit a GPU)
+    for (int64_t i = 0; i < e[0].n; ++i)
+        for (int64_t j = i ? 1 - e[1].n : 0; j < e[1].n; ++j) {
+            if (i == 0 && j == 0) continue;
+            __int128 x = (__int128)i * e[0].s + (__int128)j * e[1].s;
+            if (x < 0) x = -x;  // (k takes either sign)
+            const __int128 k = x / e[2].s;
+            if ((k < e[2].n && x - k * e[2].s < d) || (k + 1 < e[2].n && (k + 1) * e[2].s - x < d)) return true;
+        }
+    return false;
+}
+
 }  // namespace bsa
 
 using namespace bsa;
@@ -206,6 +243,8 @@ extern "C" bsa_status_t bsa_rope(const bsa_rope_desc_t* t, const bsa_view_t* Q, 
     if (!t->freq_host && !(t->theta > 0.0 && isfinite(t->theta))) return BSA_ERR_INVALID_ARG;
     if (!view_ok(Q, t->batch, t->heads, t->N) || !view_ok(Q_out, t->batch, t->heads, t->N)) return BSA_ERR_INVALID_ARG;
     if (t->heads_kv > 0 && (!view_ok(K, t->batch, t->heads_kv, t->N) || !view_ok(K_out, t->batch, t->heads_kv, t->N)))
+        return BSA_ERR_INVALID_ARG;
+    if (view_overlaps(*Q_out, t->batch, t->heads, t->N, t->d) || (t->heads_kv > 0 && view_overlaps(*K_out, t->batch, t->heads_kv, t->N, t->d)))
         return BSA_ERR_INVALID_ARG;
 
     RopeParams p = {};

@@ -611,6 +611,10 @@ bsa_status_t window_args(const bsa_window_desc_t* t, WindowArgs* a) {
     a->d = t->d;
     a->f16 = t->dtype == BSA_DTYPE_FP16;
     a->scale = t->scale > 0.f ? t->scale : 1.f / sqrtf((float)t->d);
+    return BSA_OK;
+}
+
+bsa_status_t window_device(WindowArgs* a) {
     static std::atomic<int> sms[kMaxDevices];
     cudaError_t e = cudaGetDevice(&a->device);
     if (e == cudaSuccess && a->device >= kMaxDevices) return BSA_ERR_CUDA;
@@ -636,7 +640,9 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
         !view_ok(K, t->batch, t->heads_kv, t->N_kv) || !view_ok(V, t->batch, t->heads_kv, t->N_kv))
         return BSA_ERR_INVALID_ARG;
     WindowArgs a;
-    const bsa_status_t st = window_args(t, &a);
+    bsa_status_t st = window_args(t, &a);
+    if (st == BSA_OK && view_overlaps(*O, t->batch, t->heads, t->N, t->d)) st = BSA_ERR_INVALID_ARG;
+    if (st == BSA_OK) st = window_device(&a);
     if (st != BSA_OK) return st;
     Params p = {};
     p.g = a.g;

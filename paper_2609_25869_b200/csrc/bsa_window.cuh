@@ -195,8 +195,9 @@ struct WindowArgs {
     float scale;
     int device, num_sms;
 };
-// Checks a description and fills `a` in; the current device becomes the call's.
+// Checks a description and fills `a` in, all but the device; the current device becomes the call's.
 bsa_status_t window_args(const bsa_window_desc_t* t, WindowArgs* a);
+bsa_status_t window_device(WindowArgs* a);
 // Whether every row of a view with these sizes lies on a 32-byte boundary.
 bool view_is_wide(const bsa_view_t& v, int64_t batch, int64_t heads, int64_t rows);
 // Forward for few rows (bsa_window_rows.cu).

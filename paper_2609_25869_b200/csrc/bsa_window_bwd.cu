@@ -905,7 +905,7 @@ using namespace bsa;
 
 extern "C" int64_t bsa_window_workspace_bytes(const bsa_window_desc_t* t) {
     WindowArgs a;
-    return window_args(t, &a) == BSA_OK ? layout_of(a).bytes : 0;
+    return window_args(t, &a) == BSA_OK && window_device(&a) == BSA_OK ? layout_of(a).bytes : 0;
 }
 
 extern "C" bsa_status_t bsa_window_backward(const bsa_window_desc_t* t, const bsa_view_t* Q, const bsa_view_t* K, const bsa_view_t* V,
@@ -917,7 +917,11 @@ extern "C" bsa_status_t bsa_window_backward(const bsa_window_desc_t* t, const bs
     for (const bsa_view_t* v : {K, V, dK, dV})
         if (!view_ok(v, t->batch, t->heads_kv, t->N_kv)) return BSA_ERR_INVALID_ARG;
     WindowArgs a;
-    const bsa_status_t st = window_args(t, &a);
+    bsa_status_t st = window_args(t, &a);
+    if (st == BSA_OK && (view_overlaps(*dQ, t->batch, t->heads, t->N, t->d) || view_overlaps(*dK, t->batch, t->heads_kv, t->N_kv, t->d) ||
+                         view_overlaps(*dV, t->batch, t->heads_kv, t->N_kv, t->d)))
+        st = BSA_ERR_INVALID_ARG;
+    if (st == BSA_OK) st = window_device(&a);
     if (st != BSA_OK) return st;
     const Layout l = layout_of(a);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < l.bytes) return BSA_ERR_INVALID_ARG;

@@ -106,3 +106,13 @@ def test_the_binding_refuses_what_does_not_fit_together():
     with pytest.raises(ValueError):
         bsa.window_backward(x, x, x, x, x, x, left=1)
     assert (bsa._VIEW.size, bsa._ROPE.size, bsa._WINDOW.size) == (32, 136, 80)
+
+
+# d = 128 of 2 x 4 x 100 entries: rows that share elements, heads inside each other's rows, batches inside heads, one stride for two dimensions
+@pytest.mark.parametrize("bad", [dict(row=64), dict(row=120), dict(head=64), dict(head=128 * 99), dict(batch=1 << 16), dict(batch=128 * 50, head=1 << 20),
+                                 dict(row=1 << 16), dict(head=1 << 20), dict(batch=3 * (1 << 16) + 128 * 99), dict(row=(1 << 16) + 120)])
+def test_outputs_whose_entries_overlap(bad):
+    assert forward(window(N_kv=100), o=view(**bad)) == INVALID
+    for i in (5, 6, 7):
+        assert backward(window(N_kv=100, heads_kv=4), [view(**bad) if j == i else view() for j in range(8)]) == INVALID
+    assert rope(qo=view(**bad), heads_kv=0) == INVALID and rope(ko=view(**bad), heads_kv=4) == INVALID

@@ -402,9 +402,12 @@ BSA_API bsa_status_t bsa_rope(const bsa_rope_desc_t* desc, const bsa_view_t* Q, 
  *   dK and dV summed over the query heads that share a key head and written for all N_kv rows (zero where nothing sees the
  *   key).  workspace_dev: bsa_window_workspace_bytes(desc) bytes of device memory on a 256-byte boundary, the call's own until its
  *   work on the stream is done (calls that may overlap each bring their own).
+ * Outputs may take the places of inputs that are read for the last time in front of them (same data and strides): O that of Q; dQ that
+ *   of O; dK and dV those of K, V and O.  Any other overlap of an output with another tensor of the call is not allowed; where both
+ *   begin at the same address it is refused.
  * A bounded device wait that expires ends the kernel with BSA_ERR_DEVICE_TIMEOUT in bsa_window_status; it never hangs.
  * Errors: INVALID_ARG (null, misaligned or overlapping views, sizes below one, left or right below -1, sinks below 0, heads not
- * a multiple of heads_kv, workspace too small), UNSUPPORTED (d not 64 or 128, N or N_kv above 2^29, more than 65535
+ * a multiple of heads_kv, an output in a place that is still read, workspace too small), UNSUPPORTED (d not 64 or 128, N or N_kv above 2^29, more than 65535
  * sequences x heads), CUDA.
  */
 typedef struct bsa_window_desc {

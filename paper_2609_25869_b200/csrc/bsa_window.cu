@@ -641,7 +641,7 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
         return BSA_ERR_INVALID_ARG;
     WindowArgs a;
     bsa_status_t st = window_args(t, &a);
-    if (st == BSA_OK && view_overlaps(*O, t->batch, t->heads, t->N, t->d)) st = BSA_ERR_INVALID_ARG;
+    if (st == BSA_OK && (view_overlaps(*O, t->batch, t->heads, t->N, t->d) || O->data == K->data || O->data == V->data)) st = BSA_ERR_INVALID_ARG;
     if (st == BSA_OK) st = window_device(&a);
     if (st != BSA_OK) return st;
     Params p = {};

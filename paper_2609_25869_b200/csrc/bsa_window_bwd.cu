@@ -921,6 +921,14 @@ extern "C" bsa_status_t bsa_window_backward(const bsa_window_desc_t* t, const bs
     if (st == BSA_OK && (view_overlaps(*dQ, t->batch, t->heads, t->N, t->d) || view_overlaps(*dK, t->batch, t->heads_kv, t->N_kv, t->d) ||
                          view_overlaps(*dV, t->batch, t->heads_kv, t->N_kv, t->d)))
         st = BSA_ERR_INVALID_ARG;
+    // The kernels read Q, K, V and dO until the last: dQ is finished before K and V are read for dK and dV, and any key tile's dK and dV
+    // before another's rows of Q and dO.  (O is read in front of them; a key tile's K and V before its own dK and dV.)
+    const auto over = [](const bsa_view_t* x, std::initializer_list<const bsa_view_t*> others) {
+        for (const bsa_view_t* y : others)
+            if (x->data == y->data) return true;
+        return false;
+    };
+    if (st == BSA_OK && (over(dQ, {Q, K, V, dO, dK, dV}) || over(dK, {Q, dO, dV}) || over(dV, {Q, dO}))) st = BSA_ERR_INVALID_ARG;
     if (st == BSA_OK) st = window_device(&a);
     if (st != BSA_OK) return st;
     const Layout l = layout_of(a);

@@ -55,3 +55,35 @@ def test_inputs_may_overlap():
     with pytest.raises(bsa.BsaError) as e:
         bsa.window_forward(x, x, x, left=20, O=x)
     assert e.value.status == 1
+
+
+@pytest.mark.parametrize("h,hk,n,nk", [(4, 4, 700, 700), (8, 2, 700, 1500), (2, 1, 3, 900), (40, 20, 900, 900)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_outputs_in_the_place_of_what_was_read_before(h, hk, n, nk, d):
+    """O over Q, dQ over O, dK and dV over K and V, either way round: the bits of outputs of their own."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(61)
+    q, k, v, dO = [torch.empty(s, device="cuda", dtype=torch.bfloat16).normal_(0, 1, generator=g)
+                   for s in ((1, h, n, d), (1, hk, nk, d), (1, hk, nk, d), (1, h, n, d))]
+    kw = dict(left=300, right=20, sinks=5)
+    O, L = bsa.window_forward(q, k, v, **kw)
+    G = bsa.window_backward(q, k, v, O, L, dO, **kw)
+    q2 = q.clone()
+    O2, L2 = bsa.window_forward(q2, k, v, O=q2, **kw)
+    assert O2 is q2 and torch.equal(O2, O) and torch.equal(L2, L)
+    for swap in (False, True):
+        k2, v2, o2 = k.clone(), v.clone(), O.clone()
+        G2 = bsa.window_backward(q, k2, v2, o2, L, dO, dQ=o2, dK=v2 if swap else k2, dV=k2 if swap else v2, **kw)
+        assert all(torch.equal(a, b) for a, b in zip(G, G2))
+    if hk == h:
+        o2 = O.clone()
+        G2 = bsa.window_backward(q, k, v, o2, L, dO, dK=o2, **kw)
+        assert all(torch.equal(a, b) for a, b in zip(G, G2))
+    for name, x in (("dQ", q), ("dQ", dO)):
+        with pytest.raises(bsa.BsaError) as e:
+            bsa.window_backward(q, k, v, O, L, dO, **{name: x}, **kw)
+        assert e.value.status == 1
+    for x in (k, v):
+        if x.shape == q.shape:
+            with pytest.raises(bsa.BsaError):
+                bsa.window_forward(q, k, v, O=x, **kw)

@@ -116,3 +116,14 @@ def test_outputs_whose_entries_overlap(bad):
     for i in (5, 6, 7):
         assert backward(window(N_kv=100, heads_kv=4), [view(**bad) if j == i else view() for j in range(8)]) == INVALID
     assert rope(qo=view(**bad), heads_kv=0) == INVALID and rope(ko=view(**bad), heads_kv=4) == INVALID
+
+
+def test_outputs_in_the_place_of_what_is_still_read():
+    """Q, K, V, O, dO, dQ, dK, dV by their numbers: dQ over Q, K, V, dO, dK, dV; dK over Q, dO, dV; dV over Q, dO; O over K, V."""
+    own = [FAKE * (i + 1) for i in range(8)]
+    square = window(N=100, N_kv=100, heads=4, heads_kv=4)  # so that any tensor can stand in for any other
+    for out, others in ((5, (0, 1, 2, 4, 6, 7)), (6, (0, 4, 7)), (7, (0, 4))):
+        for other in others:
+            assert backward(square, [view(data=own[other if i == out else i]) for i in range(8)], n=1 << 50) == INVALID
+    for other in (1, 2):
+        assert forward(square, *[view(data=own[other if i == 3 else i]) for i in range(4)]) == INVALID

@@ -360,7 +360,7 @@ enum { BSA_PAIRS_INTERLEAVED = 0, BSA_PAIRS_HALVES = 1 };
  * position; products and sums are fp32, rounded once to the element type.
  * Outputs may be the inputs themselves (same data and strides); any other overlap is not allowed.
  * Errors: INVALID_ARG (null, misaligned or overlapping views, sizes below one, odd axis_dim, R > d, a grid that does not fit into N
- * tokens), UNSUPPORTED (d not a multiple of 8 or above 256, N above 2^29), CUDA.
+ * tokens or, with its origin, into int32 positions), UNSUPPORTED (d not a multiple of 8 or above 256, N above 2^29), CUDA.
  */
 typedef struct bsa_rope_desc {
     int32_t batch, heads, heads_kv, d;  /* heads_kv: heads of K, 0: there is no K                      */

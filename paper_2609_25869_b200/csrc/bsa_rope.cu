@@ -273,7 +273,7 @@ extern "C" bsa_status_t bsa_rope(const bsa_rope_desc_t* t, const bsa_view_t* Q, 
         p.first = t->first;
         p.grid_tokens = 1;
         for (int a = 0; a < t->n_axes; ++a) {
-            if (t->grid[a] < 1) return BSA_ERR_INVALID_ARG;
+            if (t->grid[a] < 1 || t->origin[a] > INT32_MAX - (t->grid[a] - 1)) return BSA_ERR_INVALID_ARG;
             p.grid[a] = t->grid[a];
             p.origin[a] = t->origin[a];
             p.grid_tokens *= t->grid[a];

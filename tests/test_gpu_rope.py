@@ -162,3 +162,12 @@ def test_streams_graphs_and_refusals():
         bsa.rope(x[:, :, 1:121], axes=(100,), grid=(100,))  # no 16-byte boundary
     with pytest.raises(bsa.BsaError):
         bsa.rope(x[:1].expand(4, 100, 128), axes=(128,), grid=(100,), out=torch.empty_like(x))
+
+
+def test_a_grid_that_ends_at_the_last_int32_position():
+    """Its last token stands on 2^31 - 1 of either axis, as if given; the first axis from the lowest position on."""
+    x = torch.randn(2, 30, 64, device="cuda").bfloat16()
+    origin, grid = (-(1 << 31), (1 << 31) - 1 - 4), (6, 5)
+    where = [(origin[0] + i, origin[1] + j) for i in range(6) for j in range(5)]
+    want = bsa.rope(x, axes=(24, 40), positions=torch.tensor(where, dtype=torch.int32, device="cuda"))
+    assert torch.equal(bsa.rope(x, axes=(24, 40), grid=grid, origin=origin), want)

@@ -89,6 +89,11 @@ def test_rotations_that_make_no_sense(bad):
     assert rope(**bad) == INVALID
 
 
+@pytest.mark.parametrize("origin", [(0, 0, (1 << 31) - 5), ((1 << 31) - 1, 0, 0), (0, (1 << 31) - 4, -(1 << 31))])
+def test_a_grid_that_reaches_beyond_int32_positions(origin):
+    assert rope(pos=0, grid=(4, 5, 6), N=120, origin=origin) == INVALID
+
+
 def test_rotations_beyond_the_kernel():
     assert rope(d=100, axes=(16,), grid=(0,), origin=(0,)) == UNSUPPORTED
     assert rope(d=264, axes=(16,), grid=(0,), origin=(0,)) == UNSUPPORTED

@@ -328,43 +328,53 @@ cudaError_t launch(const WindowArgs& a, const bsa_view_t& K, const bsa_view_t& V
     if (!encode_view_map(&tk, K, a.g.N_kv, a.g.heads_kv, a.g.batch, D, KS, F16) || !encode_view_map(&tv, V, a.g.N_kv, a.g.heads_kv, a.g.batch, D, KS, F16))
         return cudaErrorInvalidValue;
     const auto kernel = window_rows_kernel<D, F16, 8>, wide_kernel = window_rows_kernel<D, F16, 16>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     static std::atomic<bool> allowed[kMaxDevices];
-    if (!allowed[a.device].load(std::memory_order_relaxed)) {
+    static std::atomic<int> resident8[kMaxDevices], resident16[kMaxDevices];  // clusters that the GPU holds at once
+    if (!allowed[a.device].load(std::memory_order_acquire)) {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(wide_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        int n = 0;
+        cfg.gridDim = dim3(attr[0].val.clusterDim.x = 8);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
         if (e != cudaSuccess) return e;
-        allowed[a.device].store(true, std::memory_order_relaxed);
+        resident8[a.device].store(n, std::memory_order_relaxed);
+        cfg.gridDim = dim3(attr[0].val.clusterDim.x = 16);
+        if (cudaOccupancyMaxActiveClusters(&n, wide_kernel, &cfg) != cudaSuccess) {  // a GPU without a place for them
+            cudaGetLastError();
+            n = 0;
+        }
+        resident16[a.device].store(n, std::memory_order_relaxed);
+        allowed[a.device].store(true, std::memory_order_release);
     }
     const unsigned blocks = (unsigned)((p.n_rows + kRows - 1) / kRows), heads = (unsigned)(a.g.batch * a.g.heads_kv);
     // CTAs of a cluster: until the GPU is full (two per SM), and eight at once where a sequence may be long: how the lengths differ
-    // is not known here, and smaller shares even the SMs out.  Not more than there are steps for their warps.  Sixteen start 11 us later
-    // (four sequences, window 1024: 8.3 -> 19.1 us): only where eight leave the GPU idle and a warp has 64 steps and more (65536 keys, 8 key
-    // heads 59.5 -> 46.6 us, 115200 keys, one 97 -> 52).
+    // is not known here, and smaller shares even the SMs out.  Not more than there are steps for their warps.  Sixteen where eight leave
+    // the GPU idle and a warp has 64 steps and more, if all clusters run at once, or if not all of eight would either (this B200 holds 14
+    // of sixteen, 33 of eight).  us, eight / sixteen, d = 128, 65536 keys: 1 key head 56 / 31, 8: 59 / 46, 11: 63 / 60, 14: 73 / 75,
+    // 16: 85 / 101, 24: 120 / 123, 33: 168 / 171, 36: 199 / 182; four sequences, window 1024, 8.3 / 19.1.  Where the tensors are long and the
+    // lengths short sixteen start later (500 of 131072 keys, 9 key heads: 6.5 / 8.2); 30000 of them: 32 / 28.
     const int64_t longest = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N;
     const int64_t steps = ((longest < a.g.N_kv ? longest : a.g.N_kv) + KS - 1) / KS;
     const auto idle = [&](int c) { return (int64_t)c * blocks * heads < 2 * a.num_sms; };
     const auto long_shares = [&](int c) { return steps > (int64_t)c * kWarps * 64; };
     int C = 1;
     while (C < 8 && (int64_t)C * kWarps < steps && (idle(C) || long_shares(C))) C *= 2;
-    if (C == 8 && idle(8) && long_shares(8)) C = 16;
-    cudaLaunchConfig_t cfg = {};
+    const int64_t clusters = (int64_t)blocks * heads;
+    const int at_once8 = resident8[a.device].load(std::memory_order_relaxed), at_once16 = resident16[a.device].load(std::memory_order_relaxed);
+    if (C == 8 && idle(8) && long_shares(8) && at_once16 > 0 && (clusters <= at_once16 || clusters > at_once8)) C = 16;
     cfg.gridDim = dim3((unsigned)C, blocks, heads);
-    cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = kSmem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)C;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, C > 8 ? wide_kernel : kernel, tk, tv, p);
-    if (e != cudaSuccess && C > 8) {  // no place for sixteen on this GPU
-        cudaGetLastError();
-        cfg.gridDim.x = attr[0].val.clusterDim.x = 8;
-        e = cudaLaunchKernelEx(&cfg, kernel, tk, tv, p);
-    }
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, C > 8 ? wide_kernel : kernel, tk, tv, p);
     if (e == cudaSuccess) count_launch();
     return e;
 }

@@ -429,3 +429,18 @@ assert bsa.window_status() == 0
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads", [9, 16, 36])
+def test_one_row_of_several_heads_against_a_long_cache(heads, d):
+    """Clusters of sixteen that run at once, of eight, and of sixteen again where not all of eight would run at once; short lengths too."""
+    n, nk = 1, 100000
+    q, k, v, _ = tensors(24, "hnd", 1, heads, heads, n, nk, d, "bf16")
+    for length in (nk, 70001, 300):
+        kw = dict(left=-1, sinks=0, kv_len=ints([length]))
+        O, L = bsa.window_forward(q, k, v, **kw)
+        for h in (0, heads - 1):
+            wO, wL, tO, tL = R.forward(q[:, h:h + 1], k[:, h:h + 1, :length], v[:, h:h + 1, :length], left=-1, u=2.0 ** -8)
+            R.assert_within(L[:, h:h + 1], wL, tL, "LSE")
+            R.assert_within(O[:, h:h + 1], wO, tO, "O")

@@ -356,8 +356,8 @@ enum { BSA_PAIRS_INTERLEAVED = 0, BSA_PAIRS_HALVES = 1 };
  *   0: one set for all); else tokens first .. first + prod(grid) - 1 stand on the grid, row-major with the last axis
  *   fastest, shifted by origin[a], and all other tokens (text in front or behind, padding) stay as they are.
  * inverse = 1 rotates by -t: the gradient of the rotation's input from its output's (the rotation is orthogonal).
- * Angles are taken modulo one turn in 64-bit fixed point before anything is rounded, so that they hold at any int32
- * position; products and sums are fp32, rounded once to the element type.
+ * Angles are taken modulo one turn in 64-bit fixed point before anything is rounded to fp32, so that they hold at any int32
+ * position (to 2^-27 turns at the last, for frequencies up to 1; a larger one's error grows with it); products and sums are fp32, rounded once to the element type.
  * Outputs may be the inputs themselves (same data and strides); any other overlap is not allowed.
  * Errors: INVALID_ARG (null, misaligned or overlapping views, sizes below one, odd axis_dim, R > d, a grid that does not fit into N
  * tokens or, with its origin, into int32 positions), UNSUPPORTED (d not a multiple of 8 or above 256, N above 2^29), CUDA.
@@ -393,7 +393,9 @@ BSA_API bsa_status_t bsa_rope(const bsa_rope_desc_t* desc, const bsa_view_t* Q, 
  *     S = scale * q . k,   LSE = log sum exp S,   O = sum exp(S - LSE) v      over the keys that the row sees.
  * Query head h reads key head h / (heads / heads_kv).  Keys that no row of a tile of 128 rows sees (beyond kv_len, left of the
  * window) may hold anything, NaN included; a key that some row of a tile sees and another does not has to be finite for the
- * other's sake (its weight there is zero).
+ * other's sake (its weight there is zero), and in the backward so has a row of Q and dO for the keys of a tile that it does not see.
+ * What a row sees reaches its outputs: with a score of NaN or +inf among its keys O and LSE are NaN; -inf is the LSE of
+ * rows that see nothing, or no score above -inf.
  *   Scores, softmax and accumulators are fp32; P (and dS in the backward) is rounded to the element type for its product,
  *   outputs are rounded once.  No atomics touch a result: the same call gives the same bits.
  * Forward: writes O [batch, heads, N, d] and LSE (fp32, contiguous [batch][heads][N], natural log).
@@ -428,7 +430,8 @@ BSA_API bsa_status_t bsa_window_backward(const bsa_window_desc_t* desc, const bs
                                          const bsa_view_t* dQ, const bsa_view_t* dK, const bsa_view_t* dV, void* workspace_dev,
                                          int64_t workspace_bytes, void* stream);
 /* The current device's status word of the windowed kernels, and clears it: 0, or BSA_ERR_DEVICE_TIMEOUT if a bounded wait of any of
- * their calls has expired since the last look (that call's outputs are undefined then).  Synchronises the device. */
+ * their calls has expired since the last look (that call's outputs are undefined then).  Synchronises the device, all its
+ * streams; the word is read and cleared in one step. */
 BSA_API bsa_status_t bsa_window_status(int* status_out);
 
 /* ---------------------------------------------------------------------------------------------

@@ -7,8 +7,10 @@
 // paired halves).  75600 tokens, 24 + 24 heads, d = 128, token-major: 288 us, 98 % of the rate of a plain copy; one token of 40 heads 2.6 us.
 //
 // Angles.  A position of 10^6 times a frequency near 1 leaves no correct bit of the angle's fraction in fp32.  The host
-// turns each frequency into F = freq / 2 pi in units of 2^-64 turns; pos * F in wrap-around 64-bit integers IS the angle
-// modulo one turn, exact to pos * 2^-65 turns.  Its upper 32 bits become a float in [-1, 1) half turns for sincospif.
+// turns each frequency into F = freq / 2 pi in units of 2^-64 turns; pos * F in wrap-around 64-bit integers is the angle
+// modulo one turn, off by pos times what F is off: 2^-65 turns of its own rounding, and the frequency's error (below; a given one
+// of f radians per position: f 2^-66 turns, from the product with 1 / 2 pi).  For theta = 10^4 and 128 pairs that is pos * 2^-62.3, 2^-31.3
+// turns at the last int32 position.  The upper 32 bits become a float in [-1, 1) half turns for sincospif.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -281,7 +283,9 @@ extern "C" bsa_status_t bsa_rope(const bsa_rope_desc_t* t, const bsa_view_t* Q, 
         }
         if (p.first > t->N - p.grid_tokens) return BSA_ERR_INVALID_ARG;
     }
-    // theta^(-2 i / n) by repeated products in 64-bit mantissas: the last of 128 is off by 2^-57 of itself at most.
+    // theta^(-2 i / n) by repeated products in 64-bit mantissas.  The step is off by 2^-63 of itself (a power within one unit), which its
+    // i-th power takes i times, and every product by 2^-64: 3 i 2^-64, below 2^-55 for the last of 128.  In turns that is largest where
+    // i theta^(-2 i / n) is: 2^-62.7 at theta = 10^4 and 128 pairs, 2^-58 where all frequencies are near 1.
     // (A power for each of 64 pairs cost the host 6 us of a call.)
     int pair = 0;
     long double f = 1.0L;

@@ -267,11 +267,6 @@ bsa_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
                 }
                 ++itq;
             }
-            if (!ok) {
-                // let copies in flight land before the CTA's shared memory goes away
-                const uint64_t t0 = globaltimer_ns();
-                while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-            }
         }
     } else if (warp == 5 && !DUAL) {
         // =========================== MMA issuer ===========================
@@ -555,9 +550,7 @@ bsa_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         }
     }
 
-    tc_fence_before();
-    __syncthreads();
-    if (tid == 0 && abort_flag) atomicExch(&p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
+    end_of_cta(abortp, &p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
     if (warp == 5) tmem_dealloc(tmem, kTmemCols);
 }
 
@@ -687,10 +680,6 @@ bsa_attention_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
                                     kv0, it.head);
                 }
                 ++itq;
-            }
-            if (!ok) {
-                const uint64_t t0 = globaltimer_ns();
-                while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
             }
         } else if (warp == 9 && lane == 0) {
             // =========================== Q K^T issuer (both slots) ===========================
@@ -918,9 +907,7 @@ bsa_attention_pair_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_
         }
     }
 
-    tc_fence_before();
-    __syncthreads();
-    if (tid == 0 && abort_flag) atomicExch(&p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
+    end_of_cta(abortp, &p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 
@@ -1038,10 +1025,6 @@ bsa_attention_cs_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                                     s * 64, kv0, it.head);
                 }
                 ++itq;
-            }
-            if (!ok) {
-                const uint64_t t0 = globaltimer_ns();
-                while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
             }
         }
     } else if (warp == 9) {
@@ -1307,9 +1290,7 @@ bsa_attention_cs_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         }
     }
 
-    tc_fence_before();
-    __syncthreads();
-    if (tid == 0 && abort_flag) atomicExch(&p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
+    end_of_cta(abortp, &p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 
@@ -1797,10 +1778,6 @@ bsa_attention_pp_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
                 if (__all_sync(0xffffffffu, second_pass())) run(IntC<1>());
             }
         }
-        if (!ok && tw == 0) {  // a Q tile in flight lands before the CTA's shared memory goes away
-            const uint64_t t0 = globaltimer_ns();
-            while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-        }
     } else if (warp >= 8) {
         reg_dec<48>();
         if (warp == 8 && lane == 0) {
@@ -1852,10 +1829,6 @@ bsa_attention_pp_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             };
             run(IntC<0>());
             if constexpr (kFirstRef) if (ok && second_pass()) run(IntC<1>());
-            if (!ok) {
-                const uint64_t t0 = globaltimer_ns();
-                while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-            }
         } else if (warp == 11 && lane == 0) {
             // =========================== V producer ===========================
             uint32_t g = 0;
@@ -1888,10 +1861,6 @@ bsa_attention_pp_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             };
             run(IntC<0>());
             if constexpr (kFirstRef) if (ok && second_pass()) run(IntC<1>());
-            if (!ok) {
-                const uint64_t t0 = globaltimer_ns();
-                while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-            }
         } else if (warp == 9 && lane == 0) {
             // =========================== Q K^T issuer ===========================
             constexpr uint32_t idesc_qk = make_idesc_f32(kTQ, TK, 0, 0, F16);
@@ -2509,9 +2478,7 @@ bsa_attention_pp_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
 #endif
     }
 
-    tc_fence_before();
-    __syncthreads();
-    if (tid == 0 && abort_flag) atomicExch(&p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
+    end_of_cta(abortp, &p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 #ifdef BSA_TRACE
     if (tid == 0 && blockIdx.x < 4096) g_cta_times[1][blockIdx.x] = (long long)globaltimer_ns();

@@ -319,8 +319,7 @@ bsa_attention_rb_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     }
     if (!ok) {  // a wait ran out: copies in flight land before the CTA's shared memory goes away
         if (lane == 0) atomicExch(&p.counters->status, (int)BSA_ERR_DEVICE_TIMEOUT);
-        const uint64_t t0 = globaltimer_ns();
-        while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+        let_copies_land();
     }
 }
 

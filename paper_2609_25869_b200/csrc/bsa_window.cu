@@ -553,7 +553,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         }
     }
 
-    end_of_cta(abortp, &g_window_status);
+    end_of_cta(abortp, &g_window_status, (int)BSA_ERR_DEVICE_TIMEOUT);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 

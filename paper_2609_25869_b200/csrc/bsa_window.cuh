@@ -123,26 +123,6 @@ struct Ring {
     }
 };
 
-// After a wait gave up: 200 us, in which copies and products in flight end (microseconds in a healthy run).
-__device__ __forceinline__ void let_copies_land() {
-    const uint64_t t0 = ptx::globaltimer_ns();
-    while (ptx::globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
-}
-// The end of a CTA of the tile kernels, for all of its threads.  Where a wait gave up, copies may be in flight that nobody will wait for,
-// also those of a producer that came to its list's end, and products that read shared and tensor memory: no warp issues any more behind
-// the first barrier, and the memory stays the CTA's until they have ended.
-__device__ __forceinline__ void end_of_cta(volatile uint32_t* abort_flag, int* status) {
-    ptx::tc_fence_before();
-    __syncthreads();
-    if (*abort_flag) {
-        if (threadIdx.x == 0) {
-            let_copies_land();
-            atomicExch(status, (int)BSA_ERR_DEVICE_TIMEOUT);
-        }
-        __syncthreads();
-    }
-}
-
 // Division of non-negative ints by a constant of the call: the items of a persistent CTA are decoded on its critical path.
 struct Divisor {
     uint32_t d, mul, shift;

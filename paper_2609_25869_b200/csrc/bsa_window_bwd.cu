@@ -417,7 +417,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             }
         }
     }
-    end_of_cta(abortp, p.status);
+    end_of_cta(abortp, p.status, (int)BSA_ERR_DEVICE_TIMEOUT);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 
@@ -797,7 +797,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             }
         }
     }
-    end_of_cta(abortp, p.status);
+    end_of_cta(abortp, p.status, (int)BSA_ERR_DEVICE_TIMEOUT);
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 

@@ -339,6 +339,27 @@ __device__ __forceinline__ uint32_t pack_16x2(float lo, float hi) {
     return F16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
 }
 
+// ---------------------------------------------------------------- the end of a CTA
+// After a wait gave up: 200 us, in which copies and products in flight end (microseconds in a healthy run).
+__device__ __forceinline__ void let_copies_land() {
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+}
+// The end of a CTA of the tile kernels, for all of its threads.  Where a wait gave up, copies may be in flight that nobody will wait for,
+// also those of a producer that came to its list's end, and products that read shared and tensor memory: no warp issues any more behind
+// the first barrier, and the memory stays the CTA's until they have ended.
+__device__ __forceinline__ void end_of_cta(volatile uint32_t* abort_flag, int* status, int timed_out) {
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) {
+            let_copies_land();
+            atomicExch(status, timed_out);
+        }
+        __syncthreads();
+    }
+}
+
 // ---------------------------------------------------------------- register-level tensor instruction
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"

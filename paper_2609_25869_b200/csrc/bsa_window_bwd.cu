@@ -446,12 +446,14 @@ __device__ __forceinline__ RowSpan row_span(const WindowGeom& g, const Sequence&
     r.t1 = (p1 - s.start) / kWinT + 1;
     return r;
 }
-// Which of the 32 query rows from row q0 on see key j.
-__device__ __forceinline__ uint32_t key_bits(const WindowGeom& g, const Sequence& s, int j, int q0) {
-    if (j >= s.len) return 0u;
-    const int from = max(j - g.right, 0), to = min(j < g.sinks ? s.len - 1 : j + g.left, s.len - 1);  // positions
-    return bits_below(to + 1 - s.start - q0) & ~bits_below(from - s.start - q0);
-}
+// The query rows [lo, hi) that see a key, none behind the last query: positions may follow in its tile, and a key that only they would see
+// may hold anything.  And 32 of them from row q0 on as bits.
+struct KeyView {
+    int lo, hi;
+    __device__ __forceinline__ KeyView(const WindowGeom& g, const Sequence& s, int key)
+        : lo(max(key - g.right, 0) - s.start), hi(key < s.len ? min(min(key < g.sinks ? s.len : key + g.left + 1, s.len) - s.start, g.N) : 0) {}
+    __device__ __forceinline__ uint32_t bits(int q0) const { return bits_below(hi - q0) & ~bits_below(lo - q0); }
+};
 
 struct DkvItem {
     int b, hk, bh, kt, share, shares;
@@ -673,6 +675,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         for (int k = 0; ok && load_item(p, k, it); ++k) {
             const int n = it.n, key0 = it.key0, key = key0 + tw;
             const Sequence seq = it.seq;
+            const KeyView view(p.g, seq, key);
             Cursor at(it);
             for (int i = 0; i < n; ++i, ++t, ring.advance<C::kQ>(), at.next(it)) {
                 const int row0 = (it.t0 + at.tile) * kWinT, pos0 = seq.start + row0;
@@ -691,8 +694,8 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 const uint64_t c22 = pack_f32x2(c2, c2), unshift2 = pack_f32x2(kUnshift<F16>, kUnshift<F16>);
                 uint32_t bits[2] = {0xffffffffu, 0xffffffffu};
                 if (!full) {
-                    bits[0] = key_bits(p.g, seq, key, row0 + x * 64);
-                    bits[1] = key_bits(p.g, seq, key, row0 + x * 64 + 32);
+                    bits[0] = view.bits(row0 + x * 64);
+                    bits[1] = view.bits(row0 + x * 64 + 32);
                     if (!rows_ok) {  // rows at no position
                         ok = mbar_wait_warp(smem_u32(&bars.o_full[ring.stage]), ring.phase, abortp);
                         if (!ok) break;

@@ -105,3 +105,26 @@ def test_an_infinite_value_that_a_row_of_few_sees(size, d):
         want[0, :h // hk, :, 3], want[0, :h // hk, :, d - 2] = math.inf, -math.inf
         O2, L2 = bsa.window_forward(q, k, bad, **kw)
         assert torch.equal(O2, want) and torch.equal(L2, L)
+
+
+# batch, heads, key heads, rows, keys, left, right, sinks, starts, lengths: the sequences go on behind the last query
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", [(1, 1, 1, 8, 54, 1, 0, 0, [0], [21]), (2, 3, 1, 13, 118, 129, 1, 1, [65, 54], [118, 67]),
+                                  (1, 8, 2, 153, 1174, 1, 0, 4, [0], [747]), (3, 16, 16, 249, 2687, 128, 30, 1, [0, 700, 2400], [771, 2687, 2500]),
+                                  (1, 2, 2, 38, 1367, -1, 0, 0, [0], [1367])], ids=lambda c: "x".join(map(str, c[:8])))
+def test_keys_behind_the_last_query_may_hold_anything(case, d):
+    """Keys that only rows of the last tile behind the last query would see change no bit of the gradients, and have none of their own."""
+    b, h, hk, n, nk, left, right, sinks, starts, lengths = case
+    q, k, v = tensors(34, b, h, hk, n, nk, d)
+    g = torch.randn_like(q)
+    kw = dict(left=left, right=right, sinks=sinks, q_start=ints(starts), kv_len=ints(lengths))
+    O, L = bsa.window_forward(q, k, v, **kw)
+    G = bsa.window_backward(q, k, v, O, L, g, **kw)
+    hidden = ~R.sees(n, nk, b, left, right, sinks, kw["q_start"], kw["kv_len"], "cuda").any(1)
+    for value in (math.nan, math.inf):
+        k2, v2 = k.clone(), v.clone()
+        k2.transpose(1, 2)[hidden], v2.transpose(1, 2)[hidden] = value, value
+        O2, L2 = bsa.window_forward(q, k2, v2, **kw)
+        G2 = bsa.window_backward(q, k2, v2, O2, L2, g, **kw)
+        assert torch.equal(O, O2) and torch.equal(L, L2) and all(torch.equal(x, y) for x, y in zip(G, G2))
+    assert not G[1].transpose(1, 2)[hidden].any() and not G[2].transpose(1, 2)[hidden].any()

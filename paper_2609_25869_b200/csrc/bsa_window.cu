@@ -660,8 +660,8 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
     // Which kernel.  Per 128 keys the one for few rows takes an SM 0.77 us for each 16 rows of a key head (d = 128) and spreads the keys over the
     // GPU; the one for tiles takes 0.73 us for 128 rows of a query head and gives a tile to one SM, so that it needs whole rounds of them.
-    // us, few rows / tiles: 65536 keys, 32 + 8 heads: 64 rows per key head, one sequence 76 / 375, eight 685 / 922; 96 rows, eight sequences
-    // 982 / 936; 256 rows, one 294 / 375; 512 rows, one 580 / 375; 16384 keys, 8 x 16 heads, d = 64: 16 rows 84 / 97, 48 rows 131 / 105.
+    // us, few rows / tiles: 65536 keys, 32 + 8 heads: 64 rows per key head, one sequence 75 / 375, eight 590 / 922; 96 rows, eight sequences
+    // 982 / 936; 256 rows, one 305 to 365 / 375; 512 rows, one 580 / 375; 16384 keys, 8 x 16 heads, d = 64: 16 rows 84 / 97, 48 rows 131 / 105.
     // Over a short window the joins weigh more: 1024 keys, one sequence, 64 rows 10 / 19, 96 rows 18 / 14.
     const int64_t window = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N, most = (window < a.g.N_kv ? window : a.g.N_kv) > 4096 ? 256 : 64;
     const int64_t rows = (int64_t)a.g.N * a.g.group, blocks = (rows + 15) / 16 * a.g.batch * a.g.heads_kv;

@@ -435,6 +435,60 @@ BSA_API bsa_status_t bsa_window_backward(const bsa_window_desc_t* desc, const bs
 BSA_API bsa_status_t bsa_window_status(int* status_out);
 
 /* ---------------------------------------------------------------------------------------------
+ * The 8-bit cache -- keys and values of a sequence's past tokens in one byte an element, written as they come, read back, or attended to where they
+ * lie (no counterpart in the paper).  As for the windows above: strided tensors, no state between calls, any streams, recordable into a CUDA graph.
+ *
+ * K, V   : codes [batch][heads][N][d], e4m3 numbers (four exponent bits, three of mantissa, largest 448; 0x7f and 0xff: NaN).  A view whose strides
+ *          are multiples of 16 elements.
+ * K_scale, V_scale : a byte s for each block of `block` tokens of a head, [batch][heads][ceil(N / block)], scale_batch and scale_head elements
+ *          between batch entries and heads (of both; the blocks of a head are contiguous): the element's value is code * 2^(s - 127); 255: NaN.
+ * The memory is the caller's; nothing has to be initialised.  Calls that write one cache are stream-ordered by the caller with those that use it.
+ */
+typedef struct bsa_cache {
+    bsa_view_t K, V;
+    uint8_t *K_scale, *V_scale;
+    int64_t scale_batch, scale_head;
+    int64_t N;                          /* tokens that fit                                              */
+    int32_t batch, heads, d;            /* d: 64 or 128                                                 */
+    int32_t block;                      /* 16, 32, 64 or 128                                            */
+} bsa_cache_t;
+
+/* Which tokens a call writes or reads: rows i < count of sequence b stand at positions start + i. */
+typedef struct bsa_cache_rows {
+    int64_t N;                          /* rows of the call's K and V                                   */
+    int32_t dtype;                      /* their BSA_DTYPE_*                                            */
+    int32_t reserved;                   /* 0                                                            */
+    const int32_t* start_dev;           /* [batch] device memory, or NULL: 0                            */
+    const int32_t* count_dev;           /* [batch] device memory, clamped to [0, N]; NULL: N            */
+} bsa_cache_rows_t;
+
+/* bsa_cache_write -- rows of K and V [batch][heads][N][d] (bf16 or fp16) become codes.
+ * Rows at no position of the cache (below 0, from its N on) are left out, and so are those from count on.
+ * With a the largest |x| of a block's new elements (infinities and NaN aside) the block needs the smallest s with a <= 448 * 2^(s - 127), 0 at least.
+ * That is its scale; but a block in which tokens stand in front of the call's first position keeps its scale s' if that is larger, and if
+ * not, those tokens' codes become the ones nearest to their values in the new scale (the same values, but for the subnormal codes).  A code is the
+ * e4m3 number nearest to x / 2^(s - 127), ties to even; infinities become NaN.  Tokens behind the last row of a call keep their codes, not
+ * their block's scale: a write ends the sequence there.
+ * bsa_cache_read -- and back: code * 2^(s - 127), rounded to the element type (exact but at the ends of its range; beyond it the largest number),
+ * zero for the rows that a write would leave out.
+ * Errors: INVALID_ARG (null, misaligned or overlapping views and scales, sizes below one, another block, an output in the place of another tensor),
+ * UNSUPPORTED (d not 64 or 128, N above 2^29, more than 65535 sequences x heads), CUDA.
+ */
+BSA_API bsa_status_t bsa_cache_write(const bsa_cache_t* cache, const bsa_cache_rows_t* rows, const bsa_view_t* K, const bsa_view_t* V, void* stream);
+BSA_API bsa_status_t bsa_cache_read(const bsa_cache_t* cache, const bsa_cache_rows_t* rows, const bsa_view_t* K, const bsa_view_t* V, void* stream);
+
+/* bsa_cache_forward -- bsa_window_forward over a cache: desc, Q, O and LSE as there (desc's batch, heads_kv, d and N_kv are the cache's), the same
+ * keys seen, the same treatment of what nobody sees, of padding and of NaN.  A block's scale of 255 reaches the rows of a tile that see any of it.
+ *   Few rows per key head: codes widen to half, which is exact, and P is rounded to half.  More: the visible keys and values go through
+ *   workspace_dev in the element type (values beyond its range: its largest number) and P is rounded to that.
+ *   workspace_dev: bsa_cache_workspace_bytes(desc, cache) bytes (0: none is needed; also for what the call refuses) on a 256-byte boundary, the call's
+ *   own until its work on the stream is done.
+ * Errors: as bsa_window_forward and bsa_cache_write; INVALID_ARG too where desc and cache disagree or the workspace is too small. */
+BSA_API int64_t bsa_cache_workspace_bytes(const bsa_window_desc_t* desc, const bsa_cache_t* cache);
+BSA_API bsa_status_t bsa_cache_forward(const bsa_window_desc_t* desc, const bsa_cache_t* cache, const bsa_view_t* Q, const bsa_view_t* O,
+                                       float* LSE_dev, void* workspace_dev, int64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Introspection (tests, benches, the offline profiler).  These synchronise with the plan's stream.
  */
 BSA_API bsa_status_t bsa_plan_get_info(const bsa_plan_t* plan, bsa_plan_info_t* info_out);

@@ -103,6 +103,11 @@ def lib() -> ctypes.CDLL:
     L.bsa_window_backward.argtypes = [ctypes.c_char_p] * 5 + [vp] + [ctypes.c_char_p] * 4 + [vp, i64, vp]
     L.bsa_window_workspace_bytes.argtypes = [ctypes.c_char_p]
     L.bsa_window_workspace_bytes.restype = i64
+    L.bsa_cache_write.argtypes = [ctypes.c_char_p] * 4 + [vp]
+    L.bsa_cache_read.argtypes = [ctypes.c_char_p] * 4 + [vp]
+    L.bsa_cache_workspace_bytes.argtypes = [ctypes.c_char_p] * 2
+    L.bsa_cache_workspace_bytes.restype = i64
+    L.bsa_cache_forward.argtypes = [ctypes.c_char_p] * 4 + [vp, vp, i64, vp]
     L.bsa_window_status.argtypes = [ctypes.POINTER(ctypes.c_int)]
     L.bsa_plan_get_info.argtypes = [vp, ctypes.POINTER(PlanInfo)]
     L.bsa_plan_export_csr.argtypes = [vp, vp, vp]
@@ -396,19 +401,28 @@ _PTR = struct.Struct("@P")
 _VIEW = struct.Struct("@Pqqq")                       # bsa_view_t
 _ROPE = struct.Struct("@4iq2i4i4idPPqq4i4i")         # bsa_rope_desc_t
 _WINDOW = struct.Struct("@4iqqqqqifPP")              # bsa_window_desc_t
+_CACHE = struct.Struct("@PqqqPqqqPPqqq4i")           # bsa_cache_t
+_ROWS = struct.Struct("@qiiPP")                      # bsa_cache_rows_t
 PAIRS = {"interleaved": 0, "halves": 1}  # BSA_PAIRS_*
 _PAD = ((0, 0, 0, 0), (0, 0, 0), (0, 0), (0,), ())  # of an array of BSA_MAX_AXES entries behind so many given ones
 _torch = None      # the module and its two element types, once a call has needed them
 _DTYPE_IDS: Dict = {}
 
 
-def _tensor_of(t, what: str):
-    """(type id, device index) of a call's first tensor."""
+def _tensors():
+    """torch, once a call has needed it."""
     global _torch
     if _torch is None:
         import torch
         _DTYPE_IDS.update({torch.bfloat16: 0, torch.float16: 1})
         _torch = torch
+    return _torch
+
+
+def _tensor_of(t, what: str):
+    """(type id, device index) of a call's first tensor."""
+    if _torch is None:
+        _tensors()
     dt, dev = _DTYPE_IDS.get(t.dtype), t.get_device()
     if dt is None or dev < 0:
         raise ValueError(f"{what} has to be a bf16 or fp16 CUDA tensor")
@@ -613,6 +627,139 @@ def window_status() -> int:
     out = ctypes.c_int(0)
     _check(lib().bsa_window_status(ctypes.byref(out)), "bsa_window_status")
     return out.value
+
+
+# ---------------------------------------------------------------- the 8-bit cache
+class Cache:
+    """Keys and values of past tokens in 8 bits (``bsa_cache_t``): the handle that ``cache_write``, ``cache_read`` and ``cache_forward`` take.
+
+    ``K``, ``V``: float8_e4m3fn CUDA tensors ``[heads_kv, N, d]`` or ``[batch, heads_kv, N, d]`` (``layout="nhd"``: heads behind N),
+    strides in multiples of 16.  ``K_scale``, ``V_scale``: float8_e8m0fnu ``[heads_kv, ceil(N / block)]`` or with a batch in front, the blocks
+    contiguous, both with the same strides; an element's value is its code times its block's scale.  ``block``: 16, 32, 64 or 128 tokens.
+    The tensors stay the caller's: views of longer ones, or of some sequences of more, make handles of their own."""
+
+    __slots__ = ("K", "V", "K_scale", "V_scale", "block", "layout", "batch", "heads", "N", "d", "device", "_packed")
+
+    def __init__(self, K, V, K_scale, V_scale, *, block: int = 64, layout: str = "hnd"):
+        import torch
+        nhd = LAYOUTS[layout] == 1
+        dev = K.get_device()
+        if dev < 0 or K.dtype is not torch.float8_e4m3fn:
+            raise ValueError("K has to be a float8_e4m3fn CUDA tensor")
+        b, h, n, d, vk = _view(K, nhd, K.dtype, dev, "K")
+        if V.shape != K.shape:
+            raise ValueError("K and V have to have one shape")
+        vv = _view(V, nhd, K.dtype, dev, "V")[4]
+        if block not in (16, 32, 64, 128):
+            raise ValueError("a block has 16, 32, 64 or 128 tokens")
+        shape = (h, -(-n // block)) if K.dim() == 3 else (b, h, -(-n // block))
+        for t, what in ((K_scale, "K_scale"), (V_scale, "V_scale")):
+            if t.dtype is not torch.float8_e8m0fnu or t.get_device() != dev or tuple(t.shape) != shape or (t.stride(-1) != 1 and shape[-1] > 1):
+                raise ValueError(f"{what} has to be a float8_e8m0fnu tensor {shape} on the device of K, contiguous in its last dimension")
+        strides = K_scale.stride()[:-1]
+        if any(n > 1 and x != y for n, x, y in zip(shape, strides, V_scale.stride())):
+            raise ValueError("K_scale and V_scale have to have the same strides")
+        sb, sh = strides if len(strides) == 2 else (0, *strides)
+        self.K, self.V, self.K_scale, self.V_scale, self.block, self.layout = K, V, K_scale, V_scale, block, layout
+        self.batch, self.heads, self.N, self.d, self.device = b, h, n, d, dev
+        self._packed = _CACHE.pack(*_VIEW.unpack(vk), *_VIEW.unpack(vv), K_scale.data_ptr(), V_scale.data_ptr(), sb, sh, n, b, h, d, block)
+
+
+def cache_create(batch: int, heads_kv: int, N: int, d: int, *, block: int = 64, layout: str = "hnd", device="cuda") -> Cache:
+    """A ``Cache`` of its own tensors for ``N`` tokens of each sequence (all zero)."""
+    import torch
+    shape = (batch, heads_kv, N, d) if LAYOUTS[layout] == 0 else (batch, N, heads_kv, d)
+    new = lambda s, t: torch.zeros(s, dtype=torch.uint8, device=device).view(t)  # noqa: E731
+    scales = (batch, heads_kv, -(-N // block))
+    return Cache(new(shape, torch.float8_e4m3fn), new(shape, torch.float8_e4m3fn), new(scales, torch.float8_e8m0fnu),
+                 new(scales, torch.float8_e8m0fnu), block=block, layout=layout)
+
+
+def _cache_rows(cache: Cache, K, V, start, count):
+    """(packed bsa_cache_rows_t, packed views of K and V): what writing and reading check alike."""
+    nhd = LAYOUTS[cache.layout] == 1
+    dt, dev = _tensor_of(K, "K")
+    if dev != cache.device:
+        raise ValueError("K has to be on the cache's device")
+    b, h, n, d, vk = _view(K, nhd, K.dtype, dev, "K")
+    if b != cache.batch or h != cache.heads or d != cache.d or V.shape != K.shape or K.dim() != cache.K.dim():
+        raise ValueError("K and V have to have one shape, and batch, heads and channels of the cache")
+    vv = _view(V, nhd, K.dtype, dev, "V")[4]
+    return _ROWS.pack(n, dt, 0, 0 if start is None else _int32_ptr(start, ((b,),), dev, "start"),
+                      0 if count is None else _int32_ptr(count, ((b,),), dev, "count")), vk, vv, dev
+
+
+def cache_write(cache: Cache, K, V, *, start=None, count=None, stream=None) -> None:
+    """``bsa_cache_write``: rows of K and V (bf16 or fp16, the cache's layout, N of them) become the cache's tokens ``start .. start +
+    count - 1``.  ``start``, ``count``: int32 CUDA tensors ``[batch]`` (default: 0, and all rows); tokens outside of the cache are left out.
+    A write ends its sequences: tokens behind it are no longer valid where they share a block with it."""
+    rows, vk, vv, dev = _cache_rows(cache, K, V, start, count)
+    _call(dev, stream, "bsa_cache_write", lib().bsa_cache_write, cache._packed, rows, vk, vv)
+
+
+def cache_read(cache: Cache, N: int, *, start=None, count=None, dtype=None, K=None, V=None, stream=None):
+    """``bsa_cache_read``: the values of the cache's tokens ``start .. start + count - 1``, N rows of every sequence, zero beyond those; as
+    ``(K, V)`` in ``dtype`` (bf16 by default) and the cache's layout, or in the tensors given.  ``stream``: as for ``rope``."""
+    if (K is None) != (V is None):
+        raise ValueError("K and V are given together")
+    if K is None:
+        tokens = -3 if LAYOUTS[cache.layout] == 1 else -2
+        shape = list(cache.K.shape)
+        shape[tokens] = N
+        dtype = dtype or _tensors().bfloat16
+        if stream is None:
+            K, V = (_torch.empty(shape, dtype=dtype, device=cache.K.device) for _ in range(2))
+        else:
+            with _pool(stream, cache.device):
+                K, V = (_torch.empty(shape, dtype=dtype, device=cache.K.device) for _ in range(2))
+    elif K.dim() < 3 or K.shape[-3 if LAYOUTS[cache.layout] == 1 else -2] != N or (dtype is not None and K.dtype is not dtype):
+        raise ValueError("K and V have to have N tokens and the given type")
+    rows, vk, vv, dev = _cache_rows(cache, K, V, start, count)
+    _call(dev, stream, "bsa_cache_read", lib().bsa_cache_read, cache._packed, rows, vk, vv)
+    return K, V
+
+
+def cache_forward(Q, cache: Cache, *, left: int, right: int = 0, sinks: int = 0, q_start=None, kv_len=None, scale: float = 0.0, O=None,
+                  LSE=None, stream=None):
+    """``bsa_cache_forward``: ``window_forward`` of Q (the cache's layout) over the keys and values of a cache; arguments and results as there.
+    A workspace, where one is needed, comes from torch's allocator."""
+    nhd = LAYOUTS[cache.layout] == 1
+    dt, dev = _tensor_of(Q, "Q")
+    if dev != cache.device:
+        raise ValueError("Q has to be on the cache's device")
+    b, h, n, d, vq = _view(Q, nhd, Q.dtype, dev, "Q")
+    if b != cache.batch or d != cache.d or Q.dim() != cache.K.dim():
+        raise ValueError("Q has to have batch and channels of the cache")
+    desc = _WINDOW.pack(b, h, cache.heads, d, n, cache.N, left, right, sinks, dt, scale,
+                        0 if q_start is None else _int32_ptr(q_start, ((b,),), dev, "q_start"),
+                        0 if kv_len is None else _int32_ptr(kv_len, ((b,),), dev, "kv_len"))
+    shape = (b, h, n) if Q.dim() == 4 else (h, n)
+    if O is not None:
+        if O.shape != Q.shape:
+            raise ValueError("O has to have the shape of Q")
+        vo = _view(O, nhd, Q.dtype, dev, "O")[4]
+    if LSE is not None:
+        _check_lse(LSE, shape, dev)
+    L = lib()
+    if dev != _torch._C._cuda_getDevice():
+        with _torch.cuda.device(dev):
+            need = L.bsa_cache_workspace_bytes(desc, cache._packed)
+    else:
+        need = L.bsa_cache_workspace_bytes(desc, cache._packed)
+    fresh = O is None
+
+    def allocate():
+        return (_torch.empty_like(Q) if fresh else O, Q.new_empty(shape, dtype=_torch.float32) if LSE is None else LSE,
+                _torch.empty(need, dtype=_torch.uint8, device=Q.device) if need else None)
+    if stream is None:
+        O, LSE, ws = allocate()
+    else:  # (the workspace's memory is free again when that stream has come past this call)
+        with _pool(stream, dev):
+            O, LSE, ws = allocate()
+    if fresh:
+        vo = _fresh_view(O, Q, nhd, Q.dtype, dev, vq)
+    _call(dev, stream, "bsa_cache_forward", L.bsa_cache_forward, desc, cache._packed, vq, vo, LSE.data_ptr(), ws.data_ptr() if need else None, need)
+    return O, LSE
 
 
 NOALLOC_MAX_ROWS = 1 << 20

@@ -2728,6 +2728,20 @@ bool encode_view_map(CUtensorMap* m, const bsa_view_t& v, int64_t rows, int head
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_codes_map(CUtensorMap* m, const uint8_t* data, long long batch_stride, long long head_stride, long long row_stride, int rows, int heads,
+                      int batch, int d, int box_rows) {
+    EncodeTiledFn enc = get_encode_fn();
+    if (!enc) return false;
+    const cuuint64_t any = (cuuint64_t)d;  // the stride of a dimension with one entry is never used
+    cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)rows, (cuuint64_t)heads, (cuuint64_t)batch};
+    cuuint64_t strides[3] = {rows > 1 ? (cuuint64_t)row_stride : any, heads > 1 ? (cuuint64_t)head_stride : any, batch > 1 ? (cuuint64_t)batch_stride : any};
+    cuuint32_t box[4] = {(cuuint32_t)d, (cuuint32_t)box_rows, 1, 1};
+    cuuint32_t es[4] = {1, 1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(data), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Shared-memory budget: 227 KB per CTA minus each kernel's static shared memory (barriers, exchange
 // buffer), which the compiler rounds up to the 1024-byte alignment of the dynamic part.
 static int static_smem_bytes(int kernel) { return (kernel == 2 || kernel == 4) ? 3072 : 1024; }
@@ -2784,7 +2798,7 @@ extern "C" __attribute__((visibility("default"))) int bsa_debug_trace_copy(long 
 extern "C" __attribute__((visibility("default"))) bsa_status_t bsa_debug_set_wait_limit(long long cycles) {
     const long long v = cycles > 0 ? cycles : 2000000000ll;
     return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &v, sizeof v) == cudaSuccess && set_window_wait_limit(v) == cudaSuccess &&
-                   set_window_rows_wait_limit(v) == cudaSuccess && set_window_bwd_wait_limit(v) == cudaSuccess
+                   set_window_rows_wait_limit(v) == cudaSuccess && set_window_bwd_wait_limit(v) == cudaSuccess && set_cache_rows_wait_limit(v) == cudaSuccess
                ? BSA_OK : BSA_ERR_CUDA;
 }
 extern "C" __attribute__((visibility("default"))) bsa_status_t bsa_debug_withhold_arrival(int on) {

@@ -1,0 +1,41 @@
+// The 8-bit cache: codes, scales, and what its kernels share.
+//
+// An element is an e4m3 number, and the elements of a block of tokens of one head share a scale 2^(s - 127), s an unsigned byte
+// (e8m0; 255: NaN).  e4m3 is a floating type, so a scale between two powers of two would gain no precision; powers of two make
+// quantising one rounding, a growing scale a shift of the exponents of what is there already (exact above e4m3's subnormals), and
+// reading back exact.
+#pragma once
+#include "bsa_window.cuh"
+
+namespace bsa {
+
+// Two e4m3 numbers as halves (exact).
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
+    return r;
+}
+// Nearest e4m3 numbers, ties to even; beyond 448 the largest, NaN stays NaN.
+__device__ __forceinline__ uint32_t f32x2_to_e4m3x2(float lo, float hi) {
+    unsigned short r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// 2^(code - 127): an exponent field, but for 0 (2^-127 is subnormal) and 255.
+__device__ __forceinline__ float scale_of(int code) {
+    return __int_as_float(code == 0 ? 0x00400000 : code == 255 ? 0x7fc00000 : code << 23);
+}
+
+struct CacheGeom {
+    int batch, heads, d, lg_block;
+    int N, blocks;  // tokens that fit, blocks of them
+    uint8_t *K, *V, *K_scale, *V_scale;
+    long long k_batch, k_head, k_row, v_batch, v_head, v_row, s_batch, s_head;
+};
+// Checks a cache and fills `g` in.
+bsa_status_t cache_geom(const bsa_cache_t* c, CacheGeom* g);
+
+// Few rows (bsa_cache_rows.cu).
+cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, cudaStream_t stream);
+
+}  // namespace bsa

@@ -629,6 +629,42 @@ bsa_status_t window_device(WindowArgs* a) {
     return BSA_OK;
 }
 
+// Which kernel.  Per 128 keys the one for few rows takes an SM 0.77 us for each 16 rows of a key head (d = 128) and spreads the keys over the
+// GPU; the one for tiles takes 0.73 us for 128 rows of a query head and gives a tile to one SM, so that it needs whole rounds of them.
+// us, few rows / tiles: 65536 keys, 32 + 8 heads: 64 rows per key head, one sequence 75 / 375, eight 590 / 922; 96 rows, eight sequences
+// 982 / 936; 256 rows, one 305 to 365 / 375; 512 rows, one 580 / 375; 16384 keys, 8 x 16 heads, d = 64: 16 rows 84 / 97, 48 rows 131 / 105.
+// Over a short window the joins weigh more: 1024 keys, one sequence, 64 rows 10 / 19, 96 rows 18 / 14.
+bool window_takes_rows(const WindowArgs& a) {
+    const int64_t window = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N, most = (window < a.g.N_kv ? window : a.g.N_kv) > 4096 ? 256 : 64;
+    const int64_t rows = (int64_t)a.g.N * a.g.group, blocks = (rows + 15) / 16 * a.g.batch * a.g.heads_kv;
+    const int64_t tiles = (a.g.N + kWinT - 1) / kWinT, rounds = (tiles * a.g.batch * a.g.heads + a.num_sms - 1) / a.num_sms;
+    return rows <= most && blocks <= rounds * a.num_sms;
+}
+
+bsa_status_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
+                                 float* LSE, cudaStream_t stream) {
+    Params p = {};
+    p.g = a.g;
+    p.O = static_cast<uint16_t*>(O.data);
+    p.o_batch = O.batch; p.o_head = O.head; p.o_row = O.row;
+    p.LSE = LSE;
+    p.o_wide = view_is_wide(O, a.g.batch, a.g.heads, a.g.N);
+    p.scale_log2 = a.scale * 1.4426950408889634f;
+    p.withhold = window_withhold();
+    const int n_qt = (a.g.N + kWinT - 1) / kWinT;
+    if ((int64_t)n_qt * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
+    p.order = ItemOrder(n_qt, cut_tiles(a.g, n_qt), a.g.batch * a.g.heads);
+    p.heads = Divisor(a.g.heads);
+    p.group = Divisor(a.g.group);
+    const cudaError_t e = a.d == 64 ? (a.f16 ? launch_rows<64, true>(a, Q, K, V, p, stream) : launch_rows<64, false>(a, Q, K, V, p, stream))
+                                    : (a.f16 ? launch_rows<128, true>(a, Q, K, V, p, stream) : launch_rows<128, false>(a, Q, K, V, p, stream));
+    if (e != cudaSuccess) {
+        set_cuda_err(e, "bsa_window_forward");
+        return BSA_ERR_CUDA;
+    }
+    return BSA_OK;
+}
+
 }  // namespace bsa
 
 using namespace bsa;
@@ -644,38 +680,10 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     if (st == BSA_OK && (view_overlaps(*O, t->batch, t->heads, t->N, t->d) || O->data == K->data || O->data == V->data)) st = BSA_ERR_INVALID_ARG;
     if (st == BSA_OK) st = window_device(&a);
     if (st != BSA_OK) return st;
-    Params p = {};
-    p.g = a.g;
-    p.O = static_cast<uint16_t*>(O->data);
-    p.o_batch = O->batch; p.o_head = O->head; p.o_row = O->row;
-    p.LSE = LSE;
-    p.o_wide = view_is_wide(*O, a.g.batch, a.g.heads, a.g.N);
-    p.scale_log2 = a.scale * 1.4426950408889634f;
-    p.withhold = window_withhold();
-    const int n_qt = (a.g.N + kWinT - 1) / kWinT;
-    if ((int64_t)n_qt * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
-    p.order = ItemOrder(n_qt, cut_tiles(a.g, n_qt), a.g.batch * a.g.heads);
-    p.heads = Divisor(a.g.heads);
-    p.group = Divisor(a.g.group);
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
-    // Which kernel.  Per 128 keys the one for few rows takes an SM 0.77 us for each 16 rows of a key head (d = 128) and spreads the keys over the
-    // GPU; the one for tiles takes 0.73 us for 128 rows of a query head and gives a tile to one SM, so that it needs whole rounds of them.
-    // us, few rows / tiles: 65536 keys, 32 + 8 heads: 64 rows per key head, one sequence 75 / 375, eight 590 / 922; 96 rows, eight sequences
-    // 982 / 936; 256 rows, one 305 to 365 / 375; 512 rows, one 580 / 375; 16384 keys, 8 x 16 heads, d = 64: 16 rows 84 / 97, 48 rows 131 / 105.
-    // Over a short window the joins weigh more: 1024 keys, one sequence, 64 rows 10 / 19, 96 rows 18 / 14.
-    const int64_t window = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N, most = (window < a.g.N_kv ? window : a.g.N_kv) > 4096 ? 256 : 64;
-    const int64_t rows = (int64_t)a.g.N * a.g.group, blocks = (rows + 15) / 16 * a.g.batch * a.g.heads_kv;
-    const int64_t rounds = ((int64_t)n_qt * a.g.batch * a.g.heads + a.num_sms - 1) / a.num_sms;
-    if (rows <= most && blocks <= rounds * a.num_sms) {
-        const cudaError_t e = launch_window_rows(a, *Q, *K, *V, *O, LSE, stream);
-        if (e != cudaSuccess) {
-            set_cuda_err(e, "bsa_window_forward");
-            return BSA_ERR_CUDA;
-        }
-        return BSA_OK;
-    }
-    const cudaError_t e = a.d == 64 ? (a.f16 ? launch_rows<64, true>(a, *Q, *K, *V, p, stream) : launch_rows<64, false>(a, *Q, *K, *V, p, stream))
-                                    : (a.f16 ? launch_rows<128, true>(a, *Q, *K, *V, p, stream) : launch_rows<128, false>(a, *Q, *K, *V, p, stream));
+    if ((int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
+    if (!window_takes_rows(a)) return launch_window_tiles(a, *Q, *K, *V, *O, LSE, stream);
+    const cudaError_t e = launch_window_rows(a, *Q, *K, *V, *O, LSE, stream);
     if (e != cudaSuccess) {
         set_cuda_err(e, "bsa_window_forward");
         return BSA_ERR_CUDA;

@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kWriteThreads<D, B>) cache_write_kernel(const 
     for (int w = 0; w < T / 32; ++w) most = max(most, most_of[w]);
     const int need = max((int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u), 0);
     const int code = keeps ? max(old, need) : need;
-    const float inv = __int_as_float(max(254 - code, 0) << 23);  // (254 at most, the field of 2^127; a held 255 stays NaN whatever is written)
+    const float inv = code == 255 ? 0.f : scale_of(254 - code);  // (a block that held 255 stays NaN whatever is written)
     if (tid == 0) *scale = (uint8_t)code;
 #pragma unroll
     for (int u = 0; u < U; ++u) {

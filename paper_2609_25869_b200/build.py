@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbsa.so")
 SOURCES = ["bsa_api.cu", "bsa_planner.cu", "bsa_attention.cu", "bsa_attention_rb.cu", "bsa_noalloc.cu",
            "bsa_rope.cu", "bsa_window.cu", "bsa_window_rows.cu", "bsa_window_bwd.cu",
-           "bsa_cache.cu", "bsa_cache_rows.cu",
+           "bsa_cache.cu", "bsa_cache_rows.cu", "bsa_cache_tiles.cu",
            "bsa_lut.cpp"]
 
 

@@ -2742,6 +2742,19 @@ bool encode_codes_map(CUtensorMap* m, const uint8_t* data, long long batch_strid
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_code_tiles_map(CUtensorMap* m, const uint8_t* data, long long batch_stride, long long head_stride, long long row_stride, int rows,
+                           int heads, int batch, int d, int box_cols, int box_rows, int box_groups) {
+    EncodeTiledFn enc = get_encode_fn();
+    if (!enc) return false;
+    const cuuint64_t any = (cuuint64_t)d;
+    cuuint64_t dims[5] = {64, (cuuint64_t)rows, (cuuint64_t)(d / 64), (cuuint64_t)heads, (cuuint64_t)batch};
+    cuuint64_t strides[4] = {rows > 1 ? (cuuint64_t)row_stride : any, 64, heads > 1 ? (cuuint64_t)head_stride : any, batch > 1 ? (cuuint64_t)batch_stride : any};
+    cuuint32_t box[5] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, (cuuint32_t)box_groups, 1, 1};
+    cuuint32_t es[5] = {1, 1, 1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<uint8_t*>(data), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Shared-memory budget: 227 KB per CTA minus each kernel's static shared memory (barriers, exchange
 // buffer), which the compiler rounds up to the 1024-byte alignment of the dynamic part.
 static int static_smem_bytes(int kernel) { return (kernel == 2 || kernel == 4) ? 3072 : 1024; }
@@ -2798,7 +2811,8 @@ extern "C" __attribute__((visibility("default"))) int bsa_debug_trace_copy(long 
 extern "C" __attribute__((visibility("default"))) bsa_status_t bsa_debug_set_wait_limit(long long cycles) {
     const long long v = cycles > 0 ? cycles : 2000000000ll;
     return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &v, sizeof v) == cudaSuccess && set_window_wait_limit(v) == cudaSuccess &&
-                   set_window_rows_wait_limit(v) == cudaSuccess && set_window_bwd_wait_limit(v) == cudaSuccess && set_cache_rows_wait_limit(v) == cudaSuccess
+                   set_window_rows_wait_limit(v) == cudaSuccess && set_window_bwd_wait_limit(v) == cudaSuccess && set_cache_rows_wait_limit(v) == cudaSuccess &&
+                   set_cache_tiles_wait_limit(v) == cudaSuccess
                ? BSA_OK : BSA_ERR_CUDA;
 }
 extern "C" __attribute__((visibility("default"))) bsa_status_t bsa_debug_withhold_arrival(int on) {

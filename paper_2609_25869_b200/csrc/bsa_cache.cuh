@@ -15,6 +15,15 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two));
     return r;
 }
+// Four: the pairs of the lower and of the upper half.
+__device__ __forceinline__ void e4m3x4_to_f16x4(uint32_t four, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 l, h;\n\t"
+        "mov.b32 {l, h}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, l;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(four));
+}
 // Nearest e4m3 numbers, ties to even; beyond 448 the largest, NaN stays NaN.
 __device__ __forceinline__ uint32_t f32x2_to_e4m3x2(float lo, float hi) {
     unsigned short r;
@@ -26,6 +35,9 @@ __device__ __forceinline__ float scale_of(int code) {
     return __int_as_float(code == 0 ? 0x00400000 : code == 255 ? 0x7fc00000 : code << 23);
 }
 
+// The code of the smallest power of two that takes the finite magnitude with these bits to 448 = 1.75 * 2^8 at most.
+__device__ __forceinline__ int scale_code(uint32_t most) { return max((int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u), 0); }
+
 struct CacheGeom {
     int batch, heads, d, lg_block;
     int N, blocks;  // tokens that fit, blocks of them
@@ -35,6 +47,10 @@ struct CacheGeom {
 // Checks a cache and fills `g` in.
 bsa_status_t cache_geom(const bsa_cache_t* c, CacheGeom* g);
 
+// Rows by the tile (bsa_cache_tiles.cu), and the workspace that they need.
+int64_t cache_tiles_bytes(const WindowArgs& a);
+cudaError_t launch_cache_tiles(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace,
+                               cudaStream_t stream);
 // Few rows (bsa_cache_rows.cu).
 cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, cudaStream_t stream);
 

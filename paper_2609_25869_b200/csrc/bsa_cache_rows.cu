@@ -67,11 +67,12 @@ __device__ __forceinline__ float2 ld_cluster(uint32_t addr) {
     asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint32_t (&r)[4]) {
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ __forceinline__ void ld_shared_v2(uint32_t addr, uint32_t (&r)[4]) {
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+// (Not volatile, as loads from the ring are plain ones: the compiler may put other products and loads between those that depend on each other.
+// In program order a step took 5000 clk of a warp that had its SM's quarter nearly to itself.)
+__device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
 // The keys of eight behind columns 2t and 2t + 1 of a product.  Rows lie D bytes apart, their 16-byte chunks XORed with the row's low bits (d = 128:
@@ -200,24 +201,28 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     for (int j = first; j < last; ++j) {
         const int key0 = key_of(j);
         const uint32_t cK = sK + slot * kSlot, cV = sV + slot * kSlot;
+        const uint8_t *gK = smem + warp * 2 * kRing + slot * kSlot, *gV = gK + kRing;
         const int code = next_code;
         if (j + 1 < last) next_code = load_scale(j + 1);
         ok = mbar_wait_warp(bK + slot * 8, phase, abortp);
         if (!ok) break;
         float s[NT_S][4];
 #pragma unroll
-        for (int n = 0; n < NT_S; ++n) {
-            s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        for (int n = 0; n < NT_S; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
 #pragma unroll
-            for (int x = 0; x < HALVES; ++x) {
-                uint32_t w[4];
-                ld_shared_v4(cK + chunk_at<D>(n * 8 + kg, x * 4 + t), w);
+        for (int x = 0; x < HALVES; ++x) {
+            uint4 w[NT_S];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const uint32_t* a = qa[x * 4 + y];
-                    mma_16816<true>(s[n], a[0], a[1], a[2], a[3], e4m3x2_to_f16x2(w[y]), e4m3x2_to_f16x2(w[y] >> 16));
+            for (int n = 0; n < NT_S; ++n) w[n] = *reinterpret_cast<const uint4*>(gK + chunk_at<D>(n * 8 + kg, x * 4 + t));
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+                for (int n = 0; n < NT_S; ++n) {  // (n inside: neighbours do not depend on each other)
+                    const uint32_t v = y == 0 ? w[n].x : y == 1 ? w[n].y : y == 2 ? w[n].z : w[n].w;
+                    uint32_t b0, b1;
+                    e4m3x4_to_f16x4(v, b0, b1);
+                    mma(s[n], qa[x * 4 + y], b0, b1);
                 }
-            }
         }
         __syncwarp();  // every lane has read the K slot
         if (lane == 0 && j + kSlots < last) copy_in(cK, &tmK, bK + slot * 8, key_of(j + kSlots));
@@ -324,21 +329,31 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             l_lo = fmaf(sum_lo, down, l_lo);
             l_hi = fmaf(sum_hi, down, l_hi);
             // V of keys 2t, 2t + 1, 2t + 8, 2t + 9 (columns of P), channels gid * D / 8 ..
-            uint32_t v[4][4];
+            uint32_t v[4][D / 32];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int key = g * 16 + (i >> 1) * 8 + ((i & 1) ? ko : ke);
-                if (D == 128) ld_shared_v4(cV + chunk_at<D>(key, gid), v[i]);
-                else ld_shared_v2(cV + chunk_at<D>(key, gid >> 1) + (gid & 1) * 8, v[i]);
+                if constexpr (D == 128) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(gV + chunk_at<D>(key, gid));
+                    v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(gV + chunk_at<D>(key, gid >> 1) + (gid & 1) * 8);
+                    v[i][0] = x.x, v[i][1] = x.y;
+                }
             }
 #pragma unroll
             for (int w = 0; w < D / 32; ++w) {
                 const uint32_t a01 = __byte_perm(v[0][w], v[1][w], 0x5140), a23 = __byte_perm(v[0][w], v[1][w], 0x7362);
                 const uint32_t b01 = __byte_perm(v[2][w], v[3][w], 0x5140), b23 = __byte_perm(v[2][w], v[3][w], 0x7362);
-                mma_16816<true>(o[4 * w], pa[0], pa[1], pa[2], pa[3], e4m3x2_to_f16x2(a01), e4m3x2_to_f16x2(b01));
-                mma_16816<true>(o[4 * w + 1], pa[0], pa[1], pa[2], pa[3], e4m3x2_to_f16x2(a01 >> 16), e4m3x2_to_f16x2(b01 >> 16));
-                mma_16816<true>(o[4 * w + 2], pa[0], pa[1], pa[2], pa[3], e4m3x2_to_f16x2(a23), e4m3x2_to_f16x2(b23));
-                mma_16816<true>(o[4 * w + 3], pa[0], pa[1], pa[2], pa[3], e4m3x2_to_f16x2(a23 >> 16), e4m3x2_to_f16x2(b23 >> 16));
+                uint32_t a0, a1, a2, a3, b0, b1, b2, b3;
+                e4m3x4_to_f16x4(a01, a0, a1);
+                e4m3x4_to_f16x4(a23, a2, a3);
+                e4m3x4_to_f16x4(b01, b0, b1);
+                e4m3x4_to_f16x4(b23, b2, b3);
+                mma(o[4 * w], pa, a0, b0);
+                mma(o[4 * w + 1], pa, a1, b1);
+                mma(o[4 * w + 2], pa, a2, b2);
+                mma(o[4 * w + 3], pa, a3, b3);
             }
         }
         __syncwarp();  // every lane has read the V slot

@@ -137,10 +137,12 @@ bool view_overlaps(const bsa_view_t& v, int64_t batch, int64_t heads, int64_t ro
 // Tensor map of a strided [batch][heads][rows][d] view (strides in elements) as {64 columns, rows, d/64 column groups, heads, batch},
 // box {64, box_rows, d/64, 1, 1}: what the windowed kernels copy tiles with.
 bool encode_view_map(CUtensorMap* m, const bsa_view_t& v, int64_t rows, int heads, int batch, int d, int box_rows, bool f16);
-// Tensor map of the 8-bit cache's codes [batch][heads][rows][d] (strides in bytes) as {d, rows, heads, batch}, box {d, box_rows, 1, 1}, swizzled as
-// wide as a row.
+// Tensor maps of the 8-bit cache's codes [batch][heads][rows][d] (strides in bytes): as {d, rows, heads, batch}, box {d, box_rows, 1, 1}, swizzled as
+// wide as a row; and as {64 columns, rows, d/64 column groups, heads, batch}, box {box_cols, box_rows, box_groups, 1, 1}, not swizzled.
 bool encode_codes_map(CUtensorMap* m, const uint8_t* data, long long batch_stride, long long head_stride, long long row_stride, int rows, int heads,
                       int batch, int d, int box_rows);
+bool encode_code_tiles_map(CUtensorMap* m, const uint8_t* data, long long batch_stride, long long head_stride, long long row_stride, int rows,
+                           int heads, int batch, int d, int box_cols, int box_rows, int box_groups);
 int rb_max_chunk(int d);  // largest T_KV (keys per staged chunk) for head dimension d
 // `stages` counts K buffers plus V buffers for the paired kernel (kernel 1), K = V ring depth for kernel 0
 int attention_max_stages(int d, int T_KV, int kernel);
@@ -152,6 +154,7 @@ cudaError_t set_window_wait_limit(long long cycles);
 cudaError_t set_window_rows_wait_limit(long long cycles);
 cudaError_t set_window_bwd_wait_limit(long long cycles);
 cudaError_t set_cache_rows_wait_limit(long long cycles);
+cudaError_t set_cache_tiles_wait_limit(long long cycles);
 void set_window_withhold(bool on);
 bool window_withhold();
 

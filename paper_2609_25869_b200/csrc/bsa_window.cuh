@@ -161,9 +161,9 @@ struct ItemOrder {
     }
 };
 // Tiles of a sequence's rows whose window is cut off by its beginning, as far as the host knows where they stand.
-inline int cut_tiles(const WindowGeom& g, int tiles) {
+inline int cut_tiles(const WindowGeom& g, int tiles, int rows = kWinT) {
     const int64_t start = g.q_start || g.kv_len ? 0 : (int64_t)g.N_kv - g.N;
-    const int64_t cut = ((int64_t)g.left - start + kWinT - 1) / kWinT;
+    const int64_t cut = ((int64_t)g.left - start + rows - 1) / rows;
     return (int)(cut < 0 ? 0 : cut > tiles ? tiles : cut);
 }
 

@@ -2,11 +2,14 @@
 
 Writing and reading are exact: each code is the nearest e4m3 number, each scale the smallest power of two that is large enough.
 
-Attention: what the windowed kernels' bounds count (window_reference.forward), over the cache's values; and besides, where codes meet the tensor
-instruction as halves, relative to the largest scale of a sequence's head,
-  * a block's values far below the largest block's fall below half's smallest step: at most 2^-38 of the largest value of K or V;
-  * so do elements of a row of bf16 queries far below the row's largest: at most 2^-38 of it;
-  * a key's weight times its block's scale, relative to the largest block's: at most 2^-38 of the largest value of V for each key.
+Attention: what the windowed kernels' bounds count (window_reference.forward), over the cache's values; and besides,
+  * an element of a row of queries: tiles take it as 8-bit pieces of x / 2^e, the row's largest being above 224 there.  Down to 2^-6 they add up to it; below,
+    the first (e4m3, steps of 2^-9) leaves 2^-10 at most and the second (e5m2, three significant bits, or steps of 2^-16) an eighth of that at
+    most: 2^-13, which is below 2^-20 of the row's largest.  (Half's third piece is not counted.  Few rows: halves, 2^-38 of it);
+  * where codes of V meet the tensor instruction as halves, a block's values far below the largest block's, whose largest is above 224 there, are off by
+    2^-25 at most, half of half's smallest step: below 2^-32 of the largest value of V;
+  * few rows take a key's weight, 2^15 at most, times its block's scale relative to the largest as a half: for each key 2^-25 of 2^15 in weight at
+    most, times 448 in the largest block's units, which is below 2^-38 of the largest value of V.
 """
 from __future__ import annotations
 
@@ -85,6 +88,6 @@ def forward(Q, K, V, **kw):
     fine = lambda x: x.double().abs().nan_to_num(0.0, 0.0, 0.0).amax()  # noqa: E731
     d = Q.shape[-1]
     scale = kw.get("scale") or d ** -0.5
-    score = 2 * scale * d * fine(Q) * fine(K) * 2.0 ** -38
+    score = scale * d * fine(Q) * fine(K) * (2.0 ** -20 + 2.0 ** -37)
     keys = V.shape[-2 if kw.get("layout", "hnd") == "hnd" else -3]
-    return wO, wL, tO + fine(V) * (2 * score + keys * 2.0 ** -38), tL + score
+    return wO, wL, tO + fine(V) * (2 * score + 2.0 ** -32 + keys * 2.0 ** -38), tL + score

@@ -125,6 +125,10 @@ struct ReadParams {
     long long k_batch, k_head, k_row, v_batch, v_head, v_row;
     int N;  // rows written
     const int32_t *start, *count;
+    // what an attention needs instead (WINDOW): the rows' window, the first tokens in front of it
+    WindowGeom g;
+    int front;                   // rows for the first tokens: a multiple of 128
+    int32_t *q_start, *kv_len;   // where the window's rows stand now
 };
 
 template <bool F16>
@@ -137,13 +141,27 @@ __device__ __forceinline__ uint32_t pack_16x2_sat(float lo, float hi) {  // beyo
 
 constexpr int kReadThreads = 256, kReadUnits = 4;
 
-template <int D, bool F16>
+template <int D, bool F16, bool WINDOW>
 __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const __grid_constant__ ReadParams p) {
     constexpr int ROW = D / 16;
     const int h = blockIdx.y, b = blockIdx.z;
     const bool is_v = blockIdx.x & 1;
-    int first, p0, p1;
-    rows_of(p.start, p.count, b, p.N, p.c.N, first, p0, p1);
+    int first = 0, p0, p1, sinks = 0, shift = 0;  // rows' positions, and those of them that count: [p0, p1) and [0, sinks)
+    if (WINDOW) {
+        const Sequence s = load_sequence(p.g, b);
+        const KeyRange k = key_range(p.g, s, 0, p.g.N);
+        shift = max(k.lo - p.front, 0);  // rows from `front` on stand for positions from front + shift on
+        if (p.N == p.c.N) shift = 0;
+        p0 = k.lo;
+        p1 = k.hi;
+        sinks = k.sink_hi;
+        if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) {
+            p.q_start[b] = s.start - shift;
+            p.kv_len[b] = s.len - shift;
+        }
+    } else {
+        rows_of(p.start, p.count, b, p.N, p.c.N, first, p0, p1);
+    }
     const uint8_t* src = is_v ? p.c.V + b * p.c.v_batch + h * p.c.v_head : p.c.K + b * p.c.k_batch + h * p.c.k_head;
     const uint8_t* scale = (is_v ? p.c.V_scale : p.c.K_scale) + b * p.c.s_batch + h * p.c.s_head;
     const long long src_row = is_v ? p.c.v_row : p.c.k_row, dst_row = is_v ? p.v_row : p.k_row;
@@ -155,8 +173,8 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const __grid_c
     for (int u = 0; u < kReadUnits; ++u) {
         const long long unit = unit0 + u * kReadThreads;
         const int row = (int)min(unit / ROW, (long long)p.N);
-        const int pos = first + row;
-        const bool there = row < p.N && pos >= p0 && pos < p1;
+        const int pos = WINDOW ? (row < p.front ? row : row + shift) : first + row;
+        const bool there = row < p.N && ((pos >= p0 && pos < p1) || (WINDOW && pos < sinks));
         x[u] = make_uint4(0, 0, 0, 0);
         code[u] = there ? 0 : -1;
         if (there) {
@@ -168,7 +186,7 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const __grid_c
     for (int u = 0; u < kReadUnits; ++u) {
         const long long unit = unit0 + u * kReadThreads;
         const int row = (int)min(unit / ROW, (long long)p.N);
-        if (row >= p.N) continue;
+        if (row >= p.N || (WINDOW && code[u] < 0)) continue;
         const float f = code[u] < 0 ? 0.f : scale_of(code[u]);
         uint32_t w[8];
 #pragma unroll
@@ -203,15 +221,16 @@ cudaError_t launch_write(const WriteParams& p, bool f16, cudaStream_t stream) {
     }
 }
 
+template <bool WINDOW>
 cudaError_t launch_read(const ReadParams& p, bool f16, cudaStream_t stream) {
     const int64_t units = (int64_t)p.N * (p.c.d / 16), per = kReadThreads * kReadUnits;
     const dim3 grid(2u * (unsigned)((units + per - 1) / per), (unsigned)p.c.heads, (unsigned)p.c.batch);
     if (p.c.d == 64) {
-        if (f16) cache_read_kernel<64, true><<<grid, kReadThreads, 0, stream>>>(p);
-        else cache_read_kernel<64, false><<<grid, kReadThreads, 0, stream>>>(p);
+        if (f16) cache_read_kernel<64, true, WINDOW><<<grid, kReadThreads, 0, stream>>>(p);
+        else cache_read_kernel<64, false, WINDOW><<<grid, kReadThreads, 0, stream>>>(p);
     } else {
-        if (f16) cache_read_kernel<128, true><<<grid, kReadThreads, 0, stream>>>(p);
-        else cache_read_kernel<128, false><<<grid, kReadThreads, 0, stream>>>(p);
+        if (f16) cache_read_kernel<128, true, WINDOW><<<grid, kReadThreads, 0, stream>>>(p);
+        else cache_read_kernel<128, false, WINDOW><<<grid, kReadThreads, 0, stream>>>(p);
     }
     count_launch();
     return cudaGetLastError();
@@ -243,6 +262,62 @@ bsa_status_t cuda_status(cudaError_t e, const char* where) {
     if (e == cudaSuccess) return BSA_OK;
     set_cuda_err(e, where);
     return BSA_ERR_CUDA;
+}
+
+// ---- attention: which way rows by the tile go ----
+// Their keys and values in 16 bits first, then the kernel for the 16-bit cache; or the kernel that reads the codes (bsa_cache_tiles.cu), which takes longer over
+// a tile, but needs no pass in front and cuts keys into parts where the rows leave SMs without work.  By what both would take in us: 6 bytes
+// an element at 6.4 TB/s for the pass and, whole rounds of items over the SMs, for a tile of 128 keys 0.97 (d = 64: 0.82) for 128 rows of an SM;
+// cache_tiles_time the other way.  Measured, first way / second, d = 128: 300 rows x 65536 keys, 8 heads 466 / 146; 4680 x 23400, 12 heads 624 / 729;
+// 4680 x 115200, 24 heads 5700 / 6500; d = 64, windows of 575 keys, 3 x 3600 rows, 16 heads 70 / 104.
+// Rows of the workspace's K and V: the first tokens (in whole tiles) and the longest window that the queries see between them, or all.
+struct Unpacked {
+    int64_t rows;
+    int front;
+};
+Unpacked unpacked_rows(const WindowArgs& a) {
+    const int64_t front = ((int64_t)a.g.sinks + kWinT - 1) / kWinT * kWinT, rows = front + (int64_t)a.g.left + a.g.right + a.g.N;
+    if (rows >= a.g.N_kv) return {a.g.N_kv, 0};
+    return {rows, (int)front};
+}
+int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
+int64_t unpacked_bytes(const WindowArgs& a) {
+    const int64_t each = (int64_t)a.g.batch * a.g.heads_kv * unpacked_rows(a).rows * a.d * 2;
+    return 2 * up256(each) + up256(8ll * a.g.batch);
+}
+bool unpacks(const WindowArgs& a) {
+    const double pass = 6.0 * a.g.batch * a.g.heads_kv * (double)unpacked_rows(a).rows * a.d / 6.4e6;
+    const int64_t window = (int64_t)a.g.left + a.g.right + a.g.sinks + kWinT, keys = window < a.g.N_kv ? window : a.g.N_kv;
+    const int64_t items = (int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads, rounds = (items + a.num_sms - 1) / a.num_sms;
+    const double tiles = (double)rounds * ((keys + kWinT - 1) / kWinT + 2) * (a.d == 128 ? 0.97 : 0.82);
+    return pass + tiles < cache_tiles_time(a);
+}
+bsa_status_t forward_unpacked(WindowArgs a, const CacheGeom& g, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace, cudaStream_t stream) {
+    // The visible keys and values in 16 bits.  Where the window is shorter than the cache its rows move up behind the first tokens; starts and
+    // lengths follow, so that who sees whom stays the same.
+    const Unpacked u = unpacked_rows(a);
+    const int64_t each = (int64_t)a.g.batch * a.g.heads_kv * u.rows * a.d;
+    ReadParams p = {};
+    p.c = g;
+    p.K = static_cast<uint16_t*>(workspace);
+    p.V = p.K + up256(2 * each) / 2;
+    p.q_start = reinterpret_cast<int32_t*>(p.V + up256(2 * each) / 2);
+    p.kv_len = p.q_start + a.g.batch;
+    p.k_row = p.v_row = a.d;
+    p.k_head = p.v_head = u.rows * a.d;
+    p.k_batch = p.v_batch = a.g.heads_kv * p.k_head;
+    p.N = (int)u.rows;
+    p.front = u.front;
+    p.g = a.g;
+    const cudaError_t e = launch_read<true>(p, a.f16, stream);
+    if (e != cudaSuccess) return cuda_status(e, "bsa_cache_forward");
+    // (a chunk against a longer cache mostly stands at its end, where all items are about as long)
+    const bool even = 2 * (int64_t)a.g.N <= a.g.N_kv;
+    a.g.N_kv = p.N;
+    a.g.q_start = p.q_start;
+    a.g.kv_len = p.kv_len;
+    const bsa_view_t k{p.K, p.k_batch, p.k_head, p.k_row}, v{p.V, p.v_batch, p.v_head, p.v_row};
+    return launch_window_tiles(a, Q, k, v, O, LSE, even, stream);
 }
 
 // What a description of attention and a cache have to agree in.
@@ -311,14 +386,14 @@ extern "C" bsa_status_t bsa_cache_read(const bsa_cache_t* c, const bsa_cache_row
     p.N = (int)r->N;
     p.start = r->start_dev;
     p.count = r->count_dev;
-    return cuda_status(launch_read(p, r->dtype == BSA_DTYPE_FP16, reinterpret_cast<cudaStream_t>(stream)), "bsa_cache_read");
+    return cuda_status(launch_read<false>(p, r->dtype == BSA_DTYPE_FP16, reinterpret_cast<cudaStream_t>(stream)), "bsa_cache_read");
 }
 
 extern "C" int64_t bsa_cache_workspace_bytes(const bsa_window_desc_t* t, const bsa_cache_t* c) {
     WindowArgs a;
     CacheGeom g;
     if (forward_args(t, c, &a, &g) != BSA_OK || window_device(&a) != BSA_OK) return 0;
-    return window_takes_rows(a) ? 0 : cache_tiles_bytes(a);
+    return window_takes_rows(a) ? 0 : unpacks(a) ? unpacked_bytes(a) : cache_tiles_bytes(a);
 }
 
 extern "C" bsa_status_t bsa_cache_forward(const bsa_window_desc_t* t, const bsa_cache_t* c, const bsa_view_t* Q, const bsa_view_t* O, float* LSE,
@@ -335,6 +410,8 @@ extern "C" bsa_status_t bsa_cache_forward(const bsa_window_desc_t* t, const bsa_
     if ((st = window_device(&a)) != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
     if (window_takes_rows(a)) return cuda_status(launch_cache_rows(a, g, *Q, *O, LSE, stream), "bsa_cache_forward");
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < cache_tiles_bytes(a)) return BSA_ERR_INVALID_ARG;
+    const bool first = unpacks(a);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < (first ? unpacked_bytes(a) : cache_tiles_bytes(a))) return BSA_ERR_INVALID_ARG;
+    if (first) return forward_unpacked(a, g, *Q, *O, LSE, workspace, stream);
     return cuda_status(launch_cache_tiles(a, g, *Q, *O, LSE, workspace, stream), "bsa_cache_forward");
 }

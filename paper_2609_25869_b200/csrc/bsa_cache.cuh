@@ -47,8 +47,9 @@ struct CacheGeom {
 // Checks a cache and fills `g` in.
 bsa_status_t cache_geom(const bsa_cache_t* c, CacheGeom* g);
 
-// Rows by the tile (bsa_cache_tiles.cu), and the workspace that they need.
+// Rows by the tile from the codes (bsa_cache_tiles.cu), the workspace that they need, and about how many us they take.
 int64_t cache_tiles_bytes(const WindowArgs& a);
+double cache_tiles_time(const WindowArgs& a);
 cudaError_t launch_cache_tiles(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace,
                                cudaStream_t stream);
 // Few rows (bsa_cache_rows.cu).

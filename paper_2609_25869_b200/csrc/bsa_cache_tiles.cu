@@ -3,8 +3,7 @@
 // The same mathematics and the same way through a tile as for the 16-bit cache (bsa_window.cu), with these differences:
 //   * A pair of CTAs takes 256 query rows of one head, each 128 of them, and one tensor instruction works for both (cta_group::2): of a tile of 128
 //     keys each CTA brings, widens and keeps half (64 keys of K, half of V's channels).  A tile's codes cross from L2 once for 256 rows, in
-//     one byte an element: a quarter of the traffic of 128-row tiles of 16-bit keys, which asked of L2 what it has (128 rows, keys in 16 bits after
-//     a pass of their own: 828 TFLOP/s on 4680 x 115200, 24 heads).
+//     one byte an element: a quarter of the traffic of 128-row tiles of 16-bit keys.
 //   * K's codes go to the tensor instruction as they are (kind::f8f6f4, twice as fast as on halves).  For that Q is cut into numbers of 8 bits
 //     that add up to it: a row is multiplied by the power of two that takes its largest element to 448 at most; the first piece is the nearest e4m3
 //     number, the others are the nearest e5m2 numbers to what is left, one of them for bf16, two for half.  From 2^-6 on (2^-15 of the row's largest)
@@ -981,11 +980,12 @@ int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 // How a call is cut up, and where its workspace has what.
 struct Plan {
     int tiles, parts;
+    double us;  // about what it takes
     int64_t rows;
     int64_t q8, c2, refs, part_ml, part_O, bytes;  // offsets
 };
-// Parts of an item: as many as make the call shortest, in tile times (0.75 us): every pair of CTAs takes its share of whole items, and an item costs
-// about four tiles for its start and end, a cut call eight for the join.  (The host knows no lengths: the tensors' sizes stand for them.)
+// Parts of an item: as many as make the call shortest.  In tile times (1.3 us; d = 64: 1.2) every pair of CTAs takes its share of whole items, and an
+// item costs about four tiles for its start and end, a cut call eight for the join.  (The host knows no lengths: the tensors' sizes stand for them.)
 Plan plan_of(const WindowArgs& a) {
     Plan w = {};
     w.tiles = (a.g.N + kPairRows - 1) / kPairRows;
@@ -996,6 +996,7 @@ Plan plan_of(const WindowArgs& a) {
     w.parts = 1;
     for (int s = 2; s <= kMaxParts && s * 4 <= tiles; ++s)
         if (cost(s) < cost(w.parts)) w.parts = s;
+    w.us = (double)cost(w.parts) * (a.d == 128 ? 1.3 : 1.2);
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -1113,6 +1114,7 @@ cudaError_t launch(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q,
 cudaError_t set_cache_tiles_wait_limit(long long cycles) { return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &cycles, sizeof cycles); }
 
 int64_t cache_tiles_bytes(const WindowArgs& a) { return plan_of(a).bytes; }
+double cache_tiles_time(const WindowArgs& a) { return plan_of(a).us; }
 
 cudaError_t launch_cache_tiles(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace, cudaStream_t stream) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);

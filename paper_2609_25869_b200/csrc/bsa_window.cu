@@ -642,7 +642,7 @@ bool window_takes_rows(const WindowArgs& a) {
 }
 
 bsa_status_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
-                                 float* LSE, cudaStream_t stream) {
+                                 float* LSE, bool even, cudaStream_t stream) {
     Params p = {};
     p.g = a.g;
     p.O = static_cast<uint16_t*>(O.data);
@@ -653,7 +653,7 @@ bsa_status_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const
     p.withhold = window_withhold();
     const int n_qt = (a.g.N + kWinT - 1) / kWinT;
     if ((int64_t)n_qt * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
-    p.order = ItemOrder(n_qt, cut_tiles(a.g, n_qt), a.g.batch * a.g.heads);
+    p.order = ItemOrder(n_qt, even ? 0 : cut_tiles(a.g, n_qt), a.g.batch * a.g.heads);
     p.heads = Divisor(a.g.heads);
     p.group = Divisor(a.g.group);
     const cudaError_t e = a.d == 64 ? (a.f16 ? launch_rows<64, true>(a, Q, K, V, p, stream) : launch_rows<64, false>(a, Q, K, V, p, stream))
@@ -682,7 +682,7 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     if (st != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
     if ((int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
-    if (!window_takes_rows(a)) return launch_window_tiles(a, *Q, *K, *V, *O, LSE, stream);
+    if (!window_takes_rows(a)) return launch_window_tiles(a, *Q, *K, *V, *O, LSE, false, stream);
     const cudaError_t e = launch_window_rows(a, *Q, *K, *V, *O, LSE, stream);
     if (e != cudaSuccess) {
         set_cuda_err(e, "bsa_window_forward");

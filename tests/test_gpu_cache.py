@@ -198,11 +198,26 @@ def queries(seed, b, h, n, d, dtype, layout):
     return torch.empty(s if b else s[1:], device="cuda").normal_(0, 1, generator=generator(seed + 99)).to(DT[dtype])
 
 
+# Few row tiles over long windows: the kernel that reads the codes, keys cut into parts
+#       b  h  hk   n    nk   left right sinks  starts           lengths
+LONG = [
+    (1, 2, 1, 300, 6000, -1, 0, 0, None, None),
+    (0, 2, 2, 513, 3333, -1, 10, 0, None, None),
+    (2, 2, 2, 257, 5000, -1, -1, 0, [0, -100], [5000, 3000]),                # rows in front of the sequence
+    (1, 4, 2, 600, 9000, 6000, 100, 200, None, None),                        # a window, its ends inside tiles, first tokens
+    (2, 3, 1, 400, 4000, 3500, 0, 7, [3600, 100], [4000, 450]),              # rows behind the sequence; parts without a tile
+    (3, 2, 1, 270, 7000, -1, 0, 40, [6730, 30, 0], [7000, 300, 0]),          # a short sequence, one without a key
+    (1, 1, 1, 1000, 4096, -1, 63, 0, None, None),
+    (2, 8, 2, 65, 20000, 15000, 0, 1, [19000, 19935], [19065, 20000]),       # 260 rows per key head
+    (1, 3, 3, 290, 30000, 4000, 500, 129, [25000], [25100]),                 # most rows at no position
+]
+
+
 @pytest.mark.parametrize("layout", ["hnd", "nhd"])
 @pytest.mark.parametrize("d,dtype", [(64, "bf16"), (64, "fp16"), (128, "bf16"), (128, "fp16")])
-@pytest.mark.parametrize("case", CASES + FEW, ids=lambda c: "x".join(str(x) for x in c[:8]))
+@pytest.mark.parametrize("case", CASES + FEW + LONG, ids=lambda c: "x".join(str(x) for x in c[:8]))
 def test_forward(case, d, dtype, layout):
-    """The windowed kernels' own cases, tiles and few rows, over caches of every block size."""
+    """The windowed kernels' own cases, tiles and few rows, and long windows of few tiles, over caches of every block size."""
     b, h, hk, n, nk, left, right, sinks, starts, lengths = case
     block = (16, 32, 64, 128)[(n + nk + d // 64 + (layout == "nhd")) % 4]
     cache, values = filled(sum(case[1:5]) + d, max(b, 1), hk, nk, d, dtype, layout, block)
@@ -212,34 +227,34 @@ def test_forward(case, d, dtype, layout):
     check_forward(q, cache, values, left=left, right=right, sinks=sinks, q_start=ints(starts), kv_len=ints(lengths))
 
 
+@pytest.mark.parametrize("block", [16, 64])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("n", [1, 3, 200])
-def test_what_no_row_sees_may_hold_anything(d, n):
+@pytest.mark.parametrize("n,nk,left", [(1, 1000, 150), (3, 1000, 150), (200, 1000, 150), (200, 9000, 5150)])
+def test_what_no_row_sees_may_hold_anything(n, nk, left, d, block):
     """Behind the length, in front of the window, between the sinks and the window: codes of NaN and scales of any byte there change no bit."""
-    block = 16
-    cache, values = filled(11, 2, 2, 1000, d, "bf16", "hnd", block)
+    cache, values = filled(11, 2, 2, nk, d, "bf16", "hnd", block)
     q = queries(3, 2, 4, n, d, "bf16", "hnd")
-    starts, lengths = [600, 130], [600 + n, 130 + n]
-    kw = dict(left=150, right=0, sinks=7, q_start=ints(starts), kv_len=ints(lengths))
+    starts, lengths = [nk - 400, 130], [nk - 400 + n, 130 + n]
+    kw = dict(left=left, right=0, sinks=7, q_start=ints(starts), kv_len=ints(lengths))
     O, L = check_forward(q, cache, values, **kw)
     for b in range(2):
-        for lo, hi in ((lengths[b], 1000), (7, starts[b] - 150)):
+        for lo, hi in ((lengths[b], nk), (7, starts[b] - left)):
             if lo >= hi:
                 continue
             for t, s in ((cache.K, cache.K_scale), (cache.V, cache.V_scale)):
                 t.view(torch.uint8)[b, :, lo:hi, ::2] = 127
                 t.view(torch.uint8)[b, :, lo:hi, 1::2] = 255
-                a, z = -(-lo // block), hi // block if hi < 1000 else s.shape[-1]
+                a, z = -(-lo // block), hi // block if hi < nk else s.shape[-1]
                 s.view(torch.uint8)[b, :, a:z:3], s.view(torch.uint8)[b, :, a + 1:z:3], s.view(torch.uint8)[b, :, a + 2:z:3] = 255, 0, 254
     O2, L2 = bsa.cache_forward(q, cache, **kw)
     assert torch.equal(O, O2) and torch.equal(L, L2)
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("n", [2, 300])
+@pytest.mark.parametrize("n,nk", [(2, 700), (300, 700), (300, 6000)])
 @pytest.mark.parametrize("what", ["K", "V", "K_scale", "V_scale", "Q"])
-def test_a_nan_that_a_row_sees_reaches_its_outputs(what, n, d):
-    cache, values = filled(13, 1, 1, 700, d, "bf16", "hnd", 32)
+def test_a_nan_that_a_row_sees_reaches_its_outputs(what, n, nk, d):
+    cache, values = filled(13, 1, 1, nk, d, "bf16", "hnd", 32)
     q = queries(4, 1, 2, n, d, "bf16", "hnd")
     kw = dict(left=-1, right=-1, q_start=ints([100]))
     clean = check_forward(q, cache, values, **kw)
@@ -262,43 +277,44 @@ def test_a_nan_that_a_row_sees_reaches_its_outputs(what, n, d):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("n", [1, 260])
-def test_blocks_of_very_different_size(n, d, dtype):
+@pytest.mark.parametrize("n,nk,block", [(1, 900, 16), (260, 900, 16), (260, 6000, 16), (260, 6000, 64)])
+def test_blocks_of_very_different_size(n, nk, block, d, dtype):
     """Scales from 2^-20 to 2^6 side by side, and queries whose elements differ as much."""
     g = generator(14)
-    cache = bsa.cache_create(1, 2, 900, d, block=16)
-    e = torch.randint(-20, 7 if dtype == "bf16" else 4, (1, 2, 57), generator=g, device="cuda")
-    f = torch.pow(2.0, e.float()).repeat_interleave(16, 2)[:, :, :900, None]
-    K, V = (tokens(g, 1, 2, 900, d, "bf16", "hnd", 0.1) for _ in range(2))
+    cache = bsa.cache_create(1, 2, nk, d, block=block)
+    e = torch.randint(-20, 7 if dtype == "bf16" else 4, (1, 2, -(-nk // block)), generator=g, device="cuda")
+    f = torch.pow(2.0, e.float()).repeat_interleave(block, 2)[:, :, :nk, None]
+    K, V = (tokens(g, 1, 2, nk, d, "bf16", "hnd", 0.1) for _ in range(2))
     bsa.cache_write(cache, (K * f * 0.05).to(DT[dtype]), (V * f).to(DT[dtype]))
-    values = [C.values(c, s, 16).cuda() for c, s in parts(cache)]
+    values = [C.values(c, s, block).cuda() for c, s in parts(cache)]
     q = queries(5, 1, 4, n, d, dtype, "hnd")
     q[..., ::3] *= 2.0 ** -12
-    check_forward(q, cache, values, left=-1, right=-1, q_start=ints([200]), kv_len=ints([890]))
-    check_forward(q, cache, values, left=40, right=3, sinks=5, q_start=ints([200]), kv_len=ints([890]))
+    check_forward(q, cache, values, left=-1, right=-1, q_start=ints([200]), kv_len=ints([nk - 10]))
+    check_forward(q, cache, values, left=nk - 860, right=3, sinks=5, q_start=ints([nk - 300]), kv_len=ints([nk - 10]))
 
 
-@pytest.mark.parametrize("n", [1, 300])
-def test_large_and_small_queries(n):
+@pytest.mark.parametrize("n,nk", [(1, 500), (300, 500), (300, 5000)])
+def test_large_and_small_queries(n, nk):
     """Rows of bf16 up to its largest numbers and down to its smallest; a row of zeros sees its keys evenly."""
-    cache, values = filled(15, 1, 1, 500, 128, "bf16", "hnd", 64)
+    cache, values = filled(15, 1, 1, nk, 128, "bf16", "hnd", 64)
     q = queries(6, 1, 1, n, 128, "bf16", "hnd")
     kw = dict(left=-1, right=-1, q_start=ints([0]))
     for f, scale in ((2.0 ** 100, 2.0 ** -104), (2.0 ** -110, 2.0 ** 106), (0.0, 0.0)):
         check_forward((q.float() * f).bfloat16(), cache, values, scale=scale, **kw)
 
 
-@pytest.mark.parametrize("n", [1, 200])
-def test_views(n):
+@pytest.mark.parametrize("n,left", [(1, 300), (200, 300), (200, -1)])
+def test_views(n, left):
     """Q out of a fused projection, O into one, a cache that is a stretch of a longer one, no batch; LSE given."""
     g = generator(16)
-    big = bsa.cache_create(3, 4, 1024, 128, block=32)
-    bsa.cache_write(big, *(tokens(g, 3, 4, 1024, 128, "bf16", "hnd") for _ in range(2)))
-    cache = bsa.Cache(big.K[1:, 1:3, 96:896], big.V[1:, 1:3, 96:896], big.K_scale[1:, 1:3, 3:28], big.V_scale[1:, 1:3, 3:28], block=32)
-    values = [C.values(c, s, 32)[1:, 1:3, 96:896].cuda() for c, s in parts(big)]
+    end = 896 if left > 0 else 9056
+    big = bsa.cache_create(3, 4, end + 128, 128, block=32)
+    bsa.cache_write(big, *(tokens(g, 3, 4, end + 128, 128, "bf16", "hnd") for _ in range(2)))
+    cache = bsa.Cache(big.K[1:, 1:3, 96:end], big.V[1:, 1:3, 96:end], big.K_scale[1:, 1:3, 3:end // 32], big.V_scale[1:, 1:3, 3:end // 32], block=32)
+    values = [C.values(c, s, 32)[1:, 1:3, 96:end].cuda() for c, s in parts(big)]
     wide = torch.empty(2, n, 3, 4, 128, device="cuda", dtype=torch.bfloat16).normal_(0, 1, generator=g)
     q = wide[:, :, 1].transpose(1, 2)
-    kw = dict(left=300, right=0, sinks=10, q_start=ints([500, 20]), kv_len=ints([700, 600]))
+    kw = dict(left=left, right=0, sinks=10, q_start=ints([500, 20]), kv_len=ints([700, 600]))
     O, L = check_forward(q, cache, values, **kw)
     out = torch.zeros_like(wide)
     lse = torch.empty_like(L)
@@ -345,14 +361,15 @@ def test_a_plan_over_what_is_read():
     R.assert_within(O, wO, tO, "O")
 
 
-@pytest.mark.parametrize("n", [1, 300])
-def test_captured_and_replayed(n):
+@pytest.mark.parametrize("n,left", [(1, 200), (300, 200), (300, -1)])
+def test_captured_and_replayed(n, left):
     """A step in a graph follows the positions in device memory; two graphs and an eager call side by side."""
     g = generator(19)
     b, h, hk, d = 2, 4, 2, 64
-    caches = [bsa.cache_create(b, hk, 1000, d, block=16) for _ in range(3)]
+    cap = 1000 if left > 0 else 9000  # (the sizes decide which way rows by the tile go)
+    caches = [bsa.cache_create(b, hk, cap, d, block=16) for _ in range(3)]
     x = [torch.empty(b, m, 900, d, device="cuda", dtype=torch.float16).normal_(0, 1, generator=g) for m in (h, hk, hk)]
-    kw = dict(left=200, right=0, sinks=3)
+    kw = dict(left=left, right=0, sinks=3)
     start, length = ints([0, 0]), ints([n, n])
     ins = [t[:, :, :n].contiguous() for t in x]
 
@@ -368,7 +385,7 @@ def test_captured_and_replayed(n):
         with torch.cuda.graph(graph):
             outs.append(step(caches[i]))
         graphs.append(graph)
-    caches[2] = bsa.cache_create(b, hk, 1000, d, block=16)
+    caches[2] = bsa.cache_create(b, hk, cap, d, block=16)
     for c in caches[:2]:
         c.K_scale.view(torch.uint8).zero_()
     side = torch.cuda.Stream()
@@ -389,23 +406,23 @@ def test_captured_and_replayed(n):
     assert bsa.window_status() == 0
 
 
-@pytest.mark.parametrize("n", [1, 300])
-def test_other_streams(n):
+@pytest.mark.parametrize("n,nk", [(1, 600), (300, 600), (300, 6000)])
+def test_other_streams(n, nk):
     """stream=: a torch stream or a handle, with the default stream busy; outputs come from that stream's pool."""
-    cache, values = filled(20, 1, 2, 600, 128, "bf16", "hnd", 64)
+    cache, values = filled(20, 1, 2, nk, 128, "bf16", "hnd", 64)
     q = queries(7, 1, 4, n, 128, "bf16", "hnd")
-    kw = dict(left=-1, right=0, sinks=0, q_start=ints([200]), kv_len=ints([200 + n]))
+    kw = dict(left=-1, right=0, sinks=0, q_start=ints([nk - 350]), kv_len=ints([nk - 350 + n]))
     O, L = check_forward(q, cache, values, **kw)
-    K, V = bsa.cache_read(cache, 600)
+    K, V = bsa.cache_read(cache, nk)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
     torch.cuda._sleep(20_000_000)
-    other = bsa.cache_create(1, 2, 600, 128, device="cuda")
+    other = bsa.cache_create(1, 2, nk, 128, device="cuda")
     side.wait_stream(torch.cuda.current_stream())
     for s in (side, side.cuda_stream):
         O2, L2 = bsa.cache_forward(q, cache, stream=s, **kw)
         bsa.cache_write(other, K, V, stream=s)
-        K2, V2 = bsa.cache_read(other, 600, stream=s)
+        K2, V2 = bsa.cache_read(other, nk, stream=s)
     side.synchronize()
     assert torch.equal(O, O2) and torch.equal(L, L2) and torch.equal(K, K2) and torch.equal(V, V2)
 

@@ -264,12 +264,12 @@ bsa_status_t cuda_status(cudaError_t e, const char* where) {
     return BSA_ERR_CUDA;
 }
 
-// ---- attention: which way rows by the tile go ----
-// Their keys and values in 16 bits first, then the kernel for the 16-bit cache; or the kernel that reads the codes (bsa_cache_tiles.cu), which takes longer over
-// a tile, but needs no pass in front and cuts keys into parts where the rows leave SMs without work.  By what both would take in us: 6 bytes
-// an element at 6.4 TB/s for the pass and, whole rounds of items over the SMs, for a tile of 128 keys 0.97 (d = 64: 0.82) for 128 rows of an SM;
-// cache_tiles_time the other way.  Measured, first way / second, d = 128: 300 rows x 65536 keys, 8 heads 466 / 146; 4680 x 23400, 12 heads 624 / 729;
-// 4680 x 115200, 24 heads 5700 / 6500; d = 64, windows of 575 keys, 3 x 3600 rows, 16 heads 70 / 104.
+// ---- attention: which way a call goes ----
+// Few rows: the kernel that spreads the keys over the GPU (bsa_cache_rows.cu).  Rows by the tile: their keys and values in 16 bits first, then the kernel for the
+// 16-bit cache; or the kernel that reads the codes (bsa_cache_tiles.cu), which takes longer over a tile, but needs no pass in front and cuts keys into
+// parts where the rows leave SMs without work.  By what they would take, in us: few rows, 0.75 (d = 64: 0.5) of an SM for each 16 rows of a key head and 128 keys;
+// in 16 bits, 6 bytes an element at 6.4 TB/s for the pass and, whole rounds of items over the SMs, 0.97 (0.82) for 128 rows of a query head and 128 keys;
+// from the codes, cache_tiles_time.
 // Rows of the workspace's K and V: the first tokens (in whole tiles) and the longest window that the queries see between them, or all.
 struct Unpacked {
     int64_t rows;
@@ -285,12 +285,25 @@ int64_t unpacked_bytes(const WindowArgs& a) {
     const int64_t each = (int64_t)a.g.batch * a.g.heads_kv * unpacked_rows(a).rows * a.d * 2;
     return 2 * up256(each) + up256(8ll * a.g.batch);
 }
-bool unpacks(const WindowArgs& a) {
-    const double pass = 6.0 * a.g.batch * a.g.heads_kv * (double)unpacked_rows(a).rows * a.d / 6.4e6;
-    const int64_t window = (int64_t)a.g.left + a.g.right + a.g.sinks + kWinT, keys = window < a.g.N_kv ? window : a.g.N_kv;
-    const int64_t items = (int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads, rounds = (items + a.num_sms - 1) / a.num_sms;
-    const double tiles = (double)rounds * ((keys + kWinT - 1) / kWinT + 2) * (a.d == 128 ? 0.97 : 0.82);
-    return pass + tiles < cache_tiles_time(a);
+enum class Way { kRows, kTiles, kUnpacked };
+Way way_of(const WindowArgs& a) {
+    const int64_t rows = (int64_t)a.g.N * a.g.group;
+    if (rows <= 16) return Way::kRows;
+    const auto tiles_of = [&](int64_t n) {  // of 128 keys, that n rows see between them
+        const int64_t window = (int64_t)a.g.left + a.g.right + a.g.sinks + n;
+        return ((window < a.g.N_kv ? window : a.g.N_kv) + kWinT - 1) / kWinT;
+    };
+    const double per = a.d == 128 ? 0.97 : 0.82;
+    const int64_t items = (int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads;
+    const double unpacked = 6.0 * a.g.batch * a.g.heads_kv * (double)unpacked_rows(a).rows * a.d / 6.4e6 + 3.0 +
+                            (double)((items + a.num_sms - 1) / a.num_sms) * (tiles_of(kWinT) + 2) * per;
+    const double tiles = cache_tiles_time(a);
+    const int64_t blocks = (rows + 15) / 16 * a.g.batch * a.g.heads_kv;
+    const double few = rows > 256 ? 1e30 : blocks * tiles_of(a.g.N) * (a.d == 128 ? 0.75 : 0.5) / a.num_sms + 6.0;
+    return few <= tiles && few <= unpacked ? Way::kRows : tiles <= unpacked ? Way::kTiles : Way::kUnpacked;
+}
+int64_t workspace_of(const WindowArgs& a, Way way) {
+    return way == Way::kRows ? cache_rows_bytes(a) : way == Way::kTiles ? cache_tiles_bytes(a) : unpacked_bytes(a);
 }
 bsa_status_t forward_unpacked(WindowArgs a, const CacheGeom& g, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace, cudaStream_t stream) {
     // The visible keys and values in 16 bits.  Where the window is shorter than the cache its rows move up behind the first tokens; starts and
@@ -393,7 +406,7 @@ extern "C" int64_t bsa_cache_workspace_bytes(const bsa_window_desc_t* t, const b
     WindowArgs a;
     CacheGeom g;
     if (forward_args(t, c, &a, &g) != BSA_OK || window_device(&a) != BSA_OK) return 0;
-    return window_takes_rows(a) ? 0 : unpacks(a) ? unpacked_bytes(a) : cache_tiles_bytes(a);
+    return workspace_of(a, way_of(a));
 }
 
 extern "C" bsa_status_t bsa_cache_forward(const bsa_window_desc_t* t, const bsa_cache_t* c, const bsa_view_t* Q, const bsa_view_t* O, float* LSE,
@@ -409,9 +422,10 @@ extern "C" bsa_status_t bsa_cache_forward(const bsa_window_desc_t* t, const bsa_
         if (O->data == in || (void*)LSE == in) return BSA_ERR_INVALID_ARG;
     if ((st = window_device(&a)) != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
-    if (window_takes_rows(a)) return cuda_status(launch_cache_rows(a, g, *Q, *O, LSE, stream), "bsa_cache_forward");
-    const bool first = unpacks(a);
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < (first ? unpacked_bytes(a) : cache_tiles_bytes(a))) return BSA_ERR_INVALID_ARG;
-    if (first) return forward_unpacked(a, g, *Q, *O, LSE, workspace, stream);
-    return cuda_status(launch_cache_tiles(a, g, *Q, *O, LSE, workspace, stream), "bsa_cache_forward");
+    const Way way = way_of(a);
+    const int64_t need = workspace_of(a, way);
+    if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return BSA_ERR_INVALID_ARG;
+    if (way == Way::kUnpacked) return forward_unpacked(a, g, *Q, *O, LSE, workspace, stream);
+    return cuda_status(way == Way::kRows ? launch_cache_rows(a, g, *Q, *O, LSE, workspace, stream) : launch_cache_tiles(a, g, *Q, *O, LSE, workspace, stream),
+                       "bsa_cache_forward");
 }

@@ -52,7 +52,13 @@ int64_t cache_tiles_bytes(const WindowArgs& a);
 double cache_tiles_time(const WindowArgs& a);
 cudaError_t launch_cache_tiles(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace,
                                cudaStream_t stream);
-// Few rows (bsa_cache_rows.cu).
-cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, cudaStream_t stream);
+// Few rows (bsa_cache_rows.cu), and the workspace that they need.
+int64_t cache_rows_bytes(const WindowArgs& a);
+cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace,
+                              cudaStream_t stream);
+// Behind either, where keys were cut into parts: O and LSE from the parts' [parts][batch][heads][N][d] sums, their maxima (log2 domain) and weights' sums
+// (bsa_cache_tiles.cu).  The sums count in the scale refs[..][1] of their key head, where refs is given; maxima are `shift` lower than the scores'.
+cudaError_t launch_cache_join(const WindowArgs& a, int parts, const float* part_O, const float2* part_ml, const int32_t* refs, float shift,
+                              const bsa_view_t& O, float* LSE, cudaStream_t stream);
 
 }  // namespace bsa

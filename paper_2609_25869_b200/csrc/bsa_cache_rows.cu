@@ -1,15 +1,20 @@
 // Attention over a window of the 8-bit cache: forward for few rows (the next token, a handful of drafted ones, a short chunk).
 //
 // What bounds it is reading the visible codes once.  As for the 16-bit cache (bsa_window_rows.cu), the keys are spread over the GPU: a cluster of
-// CTAs takes 16 rows of one key head, every warp walks its own share of the keys in steps of 4 KB (32 keys at d = 128, 64 at d = 64), copied
-// by TMA into two rings private to the warp, and the warps' and CTAs' (m, l, O) are joined in shared and distributed shared memory.
+// CTAs takes up to 16 rows of one key head, every warp walks its own share of the keys in steps of 4 KB (32 keys at d = 128, 64 at d = 64), copied
+// by TMA into two rings private to the warp, and the warps' and CTAs' (m, l, O) are joined in shared and distributed shared memory.  Long lists of
+// keys are cut into parts besides, a cluster each, whose (m, l, O) a last kernel joins: the GPU is full with one short head and a long cache, and where
+// lengths differ the last clusters are short ones.
 //
 // Per byte there are twice as many elements to multiply as in 16 bits, and each has to be widened first, so the way from shared memory to the
 // tensor instruction (mma.sync.m16n8k16 on halves) is kept short:
-//   * The order of the channels inside a product is free as long as Q has it too, and so is the order of the keys and, for P V, that of the
-//     output's columns.  A lane takes 16 channels of one key (Q K^T) or of four keys (P V) with one 16-byte load, and two neighbouring codes are
+//   * The products are taken the other way round, S^T = K Q^T and O^T = V^T P^T: the 16 rows of an instruction are keys (channels), its eight columns query
+//     rows.  With eight rows of a key head at most (the next token under grouped heads) that is half of the instructions and registers that 16
+//     query rows would take (600 -> 330 instructions for 32 keys); up to 16 have two such columns (NB).
+//   * The order of the channels inside a product is free as long as Q has it too, and so is the order of the keys and that of the output's
+//     channels.  A lane takes 16 channels of one key (K Q^T) or of four keys (V^T P^T) with one 16-byte load, and two neighbouring codes are
 //     one instruction away from a fragment's register: K's are neighbours in memory, V's (two keys of one channel) after a byte permutation.
-//   * Which key stands behind column n of a product (key_even, key_odd) is chosen so that both kinds of load are free of bank conflicts.
+//   * Which key stands behind row n of a product (key_even, kOdd) is chosen so that both kinds of load are free of bank conflicts.
 //   * e4m3 widens to half exactly.  Q comes as bf16 or half; a row of bf16 is multiplied by the power of two that takes its largest element to
 //     2^14 .. 2^15, and its elements down to 2^-31 of that one keep all their bits (what is lost below is at most 2^-39 of it).
 //   * Scales stay out of the products: scores are multiplied by their block's power of two; V's goes into the exponent of its keys' weights,
@@ -19,6 +24,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "bsa_cache.cuh"
 
@@ -29,10 +35,11 @@ using namespace ptx;
 namespace {
 
 constexpr int kWarps = 6;
-constexpr int kRows = 16;
 constexpr int kRing = 8192;  // bytes of a warp's K or V ring
 constexpr int kSlot = 4096;
 constexpr int kSlots = kRing / kSlot;
+constexpr int kMaxC = 8;  // CTAs of a cluster (the join's loads are written out)
+constexpr int kMaxParts = 16;
 constexpr unsigned kAll = 0xffffffffu;
 // P, at most one, is computed 2^15 times as large (half ends at 2^16), so that less of it falls below 2^-14.
 constexpr float kShift = 15.0f;
@@ -48,6 +55,9 @@ struct Params {
     const uint8_t *k_scale, *v_scale;
     long long s_batch, s_head;
     int lg_block, last_block;
+    int parts;
+    float* part_O;     // [parts][batch][heads][N][D]
+    float2* part_ml;   // [parts][batch][heads][N]: maximum (log2 domain), sum
     float scale_log2;
     int n_rows;    // N * group
     int withhold;  // test hook: no copy of a warp's first tile of V
@@ -75,38 +85,45 @@ __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, ui
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// The keys of eight behind columns 2t and 2t + 1 of a product.  Rows lie D bytes apart, their 16-byte chunks XORed with the row's low bits (d = 128:
-// three, of 128 bytes; d = 64: bits 1 and 2, of 64 bytes, two rows to 128 bytes).  Eight lanes of a 16-byte load of K have two columns, 2j and 2j + 1,
-// and four chunks; of V they have the four even (odd) columns and two chunks (d = 64: sixteen lanes, four half chunks).
+// P as a product's columns has keys along the rows of 8 x 8 pieces; P^T as an operand has them along the columns.
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+// The keys of eight behind rows 2t and 2t + 1 of a product.  Rows of the ring lie D bytes apart, their 16-byte chunks XORed with the row's low bits (d = 128:
+// three, of 128 bytes; d = 64: bits 1 and 2, of 64 bytes, two rows to 128 bytes).  Eight lanes of a 16-byte load of K have two rows of the product, 2j and 2j + 1,
+// and four chunks; of V they have the four even (odd) ones and two chunks (d = 64: sixteen lanes, four half chunks).
 template <int D>
 __device__ __forceinline__ int key_even(int t) { return D == 128 ? 2 * t : (t & 1) | ((t & 2) << 1); }
 template <int D>
-constexpr int kOdd = D == 128 ? 5 : 3;  // the odd column's key is the even one's XOR this
+constexpr int kOdd = D == 128 ? 5 : 3;  // the odd row's key is the even one's XOR this
 template <int D>
 __device__ __forceinline__ uint32_t chunk_at(int row, int chunk) {
     return (uint32_t)(row * D + ((chunk ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4));
 }
-// Where 16-byte piece c of a row of the partial sums lies: a lane writes D / 4 consecutive columns of a row, eight lanes at a time two rows.
+// Where 16-byte piece c of a row of the partial sums lies: eight lanes write two pieces (D / 32 apart) of four even or odd rows.
 template <int D>
 __device__ __forceinline__ int piece_at(int row, int c) {
-    return D == 128 ? c ^ (((c >> 3) & 3) | ((row & 1) << 2)) : c ^ (((c >> 3) & 1) | ((row & 1) << 1));
+    return D == 128 ? c ^ ((row >> 1) & 3) : c ^ (((row >> 1) & 1) | (row & 4));
 }
 
-// MAX_C: most CTAs of the cluster, eight or sixteen (the join's loads are written out).
-template <int D, bool F16, int MAX_C>
+// NB: query rows of a cluster by eight.
+template <int D, bool F16, int NB>
 __global__ void __launch_bounds__(kWarps * 32, 2)
 cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Params p) {
     constexpr int KS = kSlot / D;  // keys per step
     constexpr int G = KS / 16;     // groups of 16 keys, the shortest block
-    constexpr int NT_S = KS / 8, KS_QK = D / 16, NT_O = D / 8, HALVES = D / 64;
+    constexpr int ROWS = 8 * NB, KS_QK = D / 16, MT_O = D / 16, HALVES = D / 64;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[kWarps][2 * kSlots];  // K slots, then V slots: the copy has landed
-    __shared__ float wm[kWarps][kRows], wl[kWarps][kRows];      // the warps' maxima (log2 domain) and sums
-    __shared__ __align__(8) float2 cml[kRows];                  // the CTA's
+    __shared__ float wm[kWarps][ROWS], wl[kWarps][ROWS];        // the warps' maxima (log2 domain) and sums
+    __shared__ __align__(8) float2 cml[ROWS];                   // the CTA's
     __shared__ uint32_t abort_flag;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, t = lane & 3;
     const int C = gridDim.x, rank = blockIdx.x;
-    const int b = blockIdx.z / p.g.heads_kv, hk = blockIdx.z - b * p.g.heads_kv, row0 = blockIdx.y * kRows;
+    const int b = blockIdx.z / p.g.heads_kv, hk = blockIdx.z - b * p.g.heads_kv, key_part = blockIdx.y % p.parts, row0 = blockIdx.y / p.parts * ROWS;
     const uint32_t sK = smem_u32(smem) + warp * 2 * kRing, sV = sK + kRing;
     const uint32_t bK = smem_u32(&bars[warp][0]), bV = bK + kSlots * 8;
     if (threadIdx.x == 0) abort_flag = 0;
@@ -121,12 +138,12 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 
     // Row r of the key head is query token r / group under query head hk * group + r % group.
     const Sequence seq = load_sequence(p.g, b);
-    const int n0 = row0 / p.g.group, n1 = min((row0 + kRows - 1) / p.g.group + 1, p.g.N);
+    const int n0 = row0 / p.g.group, n1 = min((row0 + ROWS - 1) / p.g.group + 1, p.g.N);
     const KeyRange range = key_range(p.g, seq, n0, n1);
     // steps of KS keys: [0, st) and [w0, w1), as the tiles of the other kernel
     const int w0 = range.lo / KS, w1 = (range.hi + KS - 1) / KS, st = min((range.sink_hi + KS - 1) / KS, w0);
     const int steps = st + (w1 - w0);
-    const long long share = (long long)C * kWarps, mine = (long long)rank * kWarps + warp;
+    const long long share = (long long)p.parts * C * kWarps, mine = ((long long)key_part * C + rank) * kWarps + warp;
     const int first = (int)(steps * mine / share), last = (int)(steps * (mine + 1) / share);
     auto key_of = [&](int j) { return (j < st ? j : w0 + (j - st)) * KS; };
     auto copy_in = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int key0) {
@@ -145,17 +162,16 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         return (lane & 15) < G ? (int)__ldg(scales + min((key_of(j) + (lane & 15) * 16) >> p.lg_block, p.last_block)) : 0;
     };
     int next_code = first < last ? load_scale(first) : 0;
-    // Q fragments (A operand, row-major 16 x 16 per step) of rows gid and gid + 8: positions 2t, 2t + 1, 2t + 8, 2t + 9 of product h * 4 + s
-    // are channels h * 64 + t * 16 + s * 4 .. + 3.
-    int pos[2];
-    float c2[2];  // what takes a row's products to scores (log2 domain), but for K's scale
-    uint32_t qa[KS_QK][4];
+    // Q^T fragments (B operand, 16 channels x 8 rows per step) of row gid of each eight: positions 2t, 2t + 1, 2t + 8, 2t + 9 of product x * 4 + y
+    // are channels x * 64 + t * 16 + y * 4 .. + 3.
+    uint32_t qb[NB][KS_QK][2];
+    float c2[NB][2];  // what takes the products of rows 2t and 2t + 1 to scores (log2 domain), but for K's scale
+    int pos[NB][2];   // and where they stand
 #pragma unroll
-    for (int hi = 0; hi < 2; ++hi) {
-        const int r = row0 + gid + 8 * hi;
+    for (int nb = 0; nb < NB; ++nb) {
+        const int r = row0 + nb * 8 + gid;
         const int n = r / p.g.group, h = hk * p.g.group + (r - n * p.g.group);
         const bool ok = r < p.n_rows;
-        pos[hi] = ok ? seq.start + n : -1;
         const uint16_t* q = p.Q + (long long)b * p.q_batch + (long long)h * p.q_head + (long long)n * p.q_row;
         uint32_t most = 0;
 #pragma unroll
@@ -164,40 +180,51 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             for (int y = 0; y < 2; ++y) {
                 const uint4 v = ok ? __ldg(reinterpret_cast<const uint4*>(q + x * 64 + t * 16 + y * 8)) : make_uint4(0, 0, 0, 0);
                 const int ks = x * 4 + y * 2;
-                qa[ks][hi] = v.x;
-                qa[ks][2 + hi] = v.y;
-                qa[ks + 1][hi] = v.z;
-                qa[ks + 1][2 + hi] = v.w;
+                qb[nb][ks][0] = v.x;
+                qb[nb][ks][1] = v.y;
+                qb[nb][ks + 1][0] = v.z;
+                qb[nb][ks + 1][1] = v.w;
                 if (!F16)
                     for (const uint32_t w : {v.x, v.y, v.z, v.w}) most = max(most, max((w >> 7) & 0xffu, (w >> 23) & 0xffu));
             }
         }
-        c2[hi] = p.scale_log2;
+        float factor = p.scale_log2;
         if (!F16) {
             most = max(most, __shfl_xor_sync(kAll, most, 1));
             most = max(most, __shfl_xor_sync(kAll, most, 2));
             const int field = min(268 - (int)most, 253);  // of the factor that takes exponent most - 127 to 14, and of a finite inverse
             const float up = __int_as_float(field << 23);
-            c2[hi] *= __int_as_float((254 - field) << 23);
+            factor *= __int_as_float((254 - field) << 23);
 #pragma unroll
             for (int ks = 0; ks < KS_QK; ++ks)
 #pragma unroll
-                for (int k = hi; k < 4; k += 2) {
-                    const uint32_t w = qa[ks][k];
-                    qa[ks][k] = pack_f16x2(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t w = qb[nb][ks][k];
+                    qb[nb][ks][k] = pack_f16x2(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
                 }
         }
-    }
-    float o[NT_O][4];
 #pragma unroll
-    for (int n = 0; n < NT_O; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
-    float m_lo = -INFINITY, m_hi = -INFINITY, l_lo = 0.f, l_hi = 0.f;  // maxima of the rows, this thread's share of their sums
+        for (int e = 0; e < 2; ++e) {
+            c2[nb][e] = __shfl_sync(kAll, factor, (2 * t + e) * 4);
+            const int re = row0 + nb * 8 + 2 * t + e;
+            pos[nb][e] = re < p.n_rows ? seq.start + re / p.g.group : -1;
+        }
+    }
+    float o[NB][MT_O][4];
+    float m[NB][2], l[NB][2];  // maxima of rows 2t, 2t + 1, this thread's share of their sums
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+        for (int i = 0; i < MT_O; ++i) o[nb][i][0] = o[nb][i][1] = o[nb][i][2] = o[nb][i][3] = 0.f;
+        m[nb][0] = m[nb][1] = -INFINITY;
+        l[nb][0] = l[nb][1] = 0.f;
+    }
     int v_unit = 0;  // the accumulator counts in 2^(v_unit - 127): the largest scale so far
     int slot = 0;
     uint32_t phase = 0;
     bool ok = true;
-    const int ke = key_even<D>(t), ko = ke ^ kOdd<D>;     // of this lane's two columns
-    const int kg = key_even<D>((gid >> 1) & 3) ^ ((gid & 1) ? kOdd<D> : 0);  // and the key behind column gid
+    const int ke = key_even<D>(t), ko = ke ^ kOdd<D>;                                // the keys behind rows 2t and 2t + 1 of a product
+    const int kg = key_even<D>((gid >> 1) & 3) ^ ((gid & 1) ? kOdd<D> : 0);  // and behind row gid
     for (int j = first; j < last; ++j) {
         const int key0 = key_of(j);
         const uint32_t cK = sK + slot * kSlot, cV = sV + slot * kSlot;
@@ -206,47 +233,46 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         if (j + 1 < last) next_code = load_scale(j + 1);
         ok = mbar_wait_warp(bK + slot * 8, phase, abortp);
         if (!ok) break;
-        float s[NT_S][4];
+        float s[G][NB][4];  // keys kg, kg + 8 of a group x rows 2t, 2t + 1
 #pragma unroll
-        for (int n = 0; n < NT_S; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) s[g][nb][0] = s[g][nb][1] = s[g][nb][2] = s[g][nb][3] = 0.f;
 #pragma unroll
         for (int x = 0; x < HALVES; ++x) {
-            uint4 w[NT_S];
+            uint4 w[2 * G];
 #pragma unroll
-            for (int n = 0; n < NT_S; ++n) w[n] = *reinterpret_cast<const uint4*>(gK + chunk_at<D>(n * 8 + kg, x * 4 + t));
+            for (int n = 0; n < 2 * G; ++n) w[n] = *reinterpret_cast<const uint4*>(gK + chunk_at<D>(n * 8 + kg, x * 4 + t));
 #pragma unroll
             for (int y = 0; y < 4; ++y)
 #pragma unroll
-                for (int n = 0; n < NT_S; ++n) {  // (n inside: neighbours do not depend on each other)
-                    const uint32_t v = y == 0 ? w[n].x : y == 1 ? w[n].y : y == 2 ? w[n].z : w[n].w;
-                    uint32_t b0, b1;
-                    e4m3x4_to_f16x4(v, b0, b1);
-                    mma(s[n], qa[x * 4 + y], b0, b1);
+                for (int g = 0; g < G; ++g) {  // (groups inside: neighbours do not depend on each other)
+                    const uint4 &u = w[2 * g], &v = w[2 * g + 1];
+                    uint32_t a[4];
+                    e4m3x4_to_f16x4(y == 0 ? u.x : y == 1 ? u.y : y == 2 ? u.z : u.w, a[0], a[2]);
+                    e4m3x4_to_f16x4(y == 0 ? v.x : y == 1 ? v.y : y == 2 ? v.z : v.w, a[1], a[3]);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma(s[g][nb], a, qb[nb][x * 4 + y][0], qb[nb][x * 4 + y][1]);
                 }
         }
         __syncwarp();  // every lane has read the K slot
         if (lane == 0 && j + kSlots < last) copy_in(cK, &tmK, bK + slot * 8, key_of(j + kSlots));
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int kc = __shfl_sync(kAll, code, g);
-            const float f = scale_of(kc);
-            float f_lo = c2[0] * f, f_hi = c2[1] * f;
-            f_lo = f_lo > FLT_MAX ? FLT_MAX : f_lo;  // (so that a product of zero stays a score of zero)
-            f_hi = f_hi > FLT_MAX ? FLT_MAX : f_hi;
-#pragma unroll
-            for (int n = 2 * g; n < 2 * g + 2; ++n) {
-                s[n][0] *= f_lo;
-                s[n][1] *= f_lo;
-                s[n][2] *= f_hi;
-                s[n][3] *= f_hi;
-            }
-        }
-        int vc[G];  // V's codes; of groups that nobody here sees, the unit's
+        int vc[G];  // V's codes; of groups that nobody here sees, zero
         int v_most = v_unit;
         const bool full = key0 + KS <= range.all_hi && (key0 >= range.all_lo || key0 + KS <= p.g.sinks);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
+            const float f = scale_of(__shfl_sync(kAll, code, g));
             vc[g] = __shfl_sync(kAll, code, 16 + g);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float c = c2[nb][e] * f;
+                    c = c > FLT_MAX ? FLT_MAX : c;  // (so that a product of zero stays a score of zero)
+                    s[g][nb][e] *= c;
+                    s[g][nb][2 + e] *= c;
+                }
             const int k = key0 + 16 * g;
             if (!full && (k >= range.hi || (k + 16 <= range.lo && k >= range.sink_hi))) vc[g] = 0;
             v_most = max(v_most, vc[g] == 255 ? 0 : vc[g]);
@@ -254,19 +280,21 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         ok = mbar_wait_warp(bV + slot * 8, phase, abortp);
         if (!ok) break;
         if (!full) {
-            const RowView lo(p.g, seq, pos[0], key0), hi(p.g, seq, pos[1], key0);
 #pragma unroll
-            for (int w = 0; w < KS / 32; ++w) {
-                const uint32_t lo_bits = lo.bits(w * 32), hi_bits = hi.bits(w * 32);
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int n = 4 * w; n < 4 * w + 4; ++n) {
-                    const int c = (n & 3) * 8;
-                    if (!((lo_bits >> (c + ke)) & 1)) s[n][0] = -INFINITY;
-                    if (!((lo_bits >> (c + ko)) & 1)) s[n][1] = -INFINITY;
-                    if (!((hi_bits >> (c + ke)) & 1)) s[n][2] = -INFINITY;
-                    if (!((hi_bits >> (c + ko)) & 1)) s[n][3] = -INFINITY;
+                for (int e = 0; e < 2; ++e) {
+                    const RowView view(p.g, seq, pos[nb][e], key0);
+#pragma unroll
+                    for (int w = 0; w < KS / 32; ++w) {
+                        const uint32_t bits = view.bits(w * 32) >> kg;
+#pragma unroll
+                        for (int g = 2 * w; g < 2 * w + 2; ++g) {
+                            if (!((bits >> (g & 1) * 16) & 1)) s[g][nb][e] = -INFINITY;
+                            if (!((bits >> ((g & 1) * 16 + 8)) & 1)) s[g][nb][2 + e] = -INFINITY;
+                        }
+                    }
                 }
-            }
             // V rows that no row here sees may hold anything: their weight is zero, which times NaN would not be
             for (int k = lane; k < KS; k += 32) {
                 const int key = key0 + k;
@@ -279,56 +307,62 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             fence_proxy_async_smem();  // before the slot's next copy
             __syncwarp();
         }
-        float mx_lo = -INFINITY, mx_hi = -INFINITY;
+        float mx[NB][2];
+        bool grows = false;
 #pragma unroll
-        for (int n = 0; n < NT_S; ++n) {
-            mx_lo = max3(mx_lo, s[n][0], s[n][1]);
-            mx_hi = max3(mx_hi, s[n][2], s[n][3]);
-        }
-        if (__any_sync(kAll, mx_lo > m_lo || mx_hi > m_hi) || v_most > v_unit) {
-            mx_lo = fmaxf(mx_lo, __shfl_xor_sync(kAll, mx_lo, 1));
-            mx_hi = fmaxf(mx_hi, __shfl_xor_sync(kAll, mx_hi, 1));
-            mx_lo = fmaxf(mx_lo, __shfl_xor_sync(kAll, mx_lo, 2));
-            mx_hi = fmaxf(mx_hi, __shfl_xor_sync(kAll, mx_hi, 2));
-            const float mn_lo = fmaxf(m_lo, mx_lo), mn_hi = fmaxf(m_hi, mx_hi);
-            const float a_lo = (m_lo == -INFINITY) ? 0.f : ex2_approx(m_lo - mn_lo);
-            const float a_hi = (m_hi == -INFINITY) ? 0.f : ex2_approx(m_hi - mn_hi);
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                mx[nb][e] = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < G; ++g) mx[nb][e] = max3(mx[nb][e], s[g][nb][e], s[g][nb][2 + e]);
+                grows |= mx[nb][e] > m[nb][e];
+            }
+        if (__any_sync(kAll, grows) || v_most > v_unit) {
             const float unit = ex2_approx((float)(v_unit - v_most));
-            m_lo = mn_lo;
-            m_hi = mn_hi;
             v_unit = v_most;
-            l_lo *= a_lo;
-            l_hi *= a_hi;
-            const float u_lo = a_lo * unit, u_hi = a_hi * unit;
 #pragma unroll
-            for (int n = 0; n < NT_O; ++n) {
-                o[n][0] *= u_lo;
-                o[n][1] *= u_lo;
-                o[n][2] *= u_hi;
-                o[n][3] *= u_hi;
+            for (int nb = 0; nb < NB; ++nb) {
+                float u[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int x = 4; x < 32; x *= 2) mx[nb][e] = fmaxf(mx[nb][e], __shfl_xor_sync(kAll, mx[nb][e], x));
+                    const float mn = fmaxf(m[nb][e], mx[nb][e]), a = (m[nb][e] == -INFINITY) ? 0.f : ex2_approx(m[nb][e] - mn);
+                    m[nb][e] = mn;
+                    l[nb][e] *= a;
+                    u[e] = a * unit;
+                }
+#pragma unroll
+                for (int i = 0; i < MT_O; ++i) {
+                    o[nb][i][0] *= u[0];
+                    o[nb][i][1] *= u[1];
+                    o[nb][i][2] *= u[0];
+                    o[nb][i][3] *= u[1];
+                }
             }
         }
-        const float nm_lo = (m_lo == -INFINITY) ? 0.f : kShift - m_lo, nm_hi = (m_hi == -INFINITY) ? 0.f : kShift - m_hi;
+        float nm[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) nm[nb][e] = (m[nb][e] == -INFINITY) ? 0.f : kShift - m[nb][e];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int dv = max(vc[g] - v_unit, -kFar);
             const float up = vc[g] == 255 ? NAN : (float)dv, down = __int_as_float((127 - dv) << 23);  // (255: dv is not used)
-            const float g_lo = nm_lo + up, g_hi = nm_hi + up;
-            uint32_t pa[4];  // P as the A operand of P V
-            float sum_lo = 0.f, sum_hi = 0.f;
+            uint32_t pb[NB][2];  // P^T as the B operand of V^T P^T
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float* x = s[2 * g + i];
-                const float p0 = ex2_approx(x[0] + g_lo), p1 = ex2_approx(x[1] + g_lo);
-                const float p2 = ex2_approx(x[2] + g_hi), p3 = ex2_approx(x[3] + g_hi);
-                sum_lo += p0 + p1;
-                sum_hi += p2 + p3;
-                pa[i * 2] = pack_f16x2(p0, p1);
-                pa[i * 2 + 1] = pack_f16x2(p2, p3);
+            for (int nb = 0; nb < NB; ++nb) {
+                const float n0 = nm[nb][0] + up, n1 = nm[nb][1] + up;
+                const float p0 = ex2_approx(s[g][nb][0] + n0), p1 = ex2_approx(s[g][nb][1] + n1);
+                const float p2 = ex2_approx(s[g][nb][2] + n0), p3 = ex2_approx(s[g][nb][3] + n1);
+                l[nb][0] = fmaf(p0 + p2, down, l[nb][0]);
+                l[nb][1] = fmaf(p1 + p3, down, l[nb][1]);
+                pb[nb][0] = transpose_8x8(pack_f16x2(p0, p1));
+                pb[nb][1] = transpose_8x8(pack_f16x2(p2, p3));
             }
-            l_lo = fmaf(sum_lo, down, l_lo);
-            l_hi = fmaf(sum_hi, down, l_hi);
-            // V of keys 2t, 2t + 1, 2t + 8, 2t + 9 (columns of P), channels gid * D / 8 ..
+            // V of the keys behind rows 2t, 2t + 1, 2t + 8, 2t + 9, channels gid * D / 8 ..
             uint32_t v[4][D / 32];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -342,18 +376,17 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 }
             }
 #pragma unroll
-            for (int w = 0; w < D / 32; ++w) {
-                const uint32_t a01 = __byte_perm(v[0][w], v[1][w], 0x5140), a23 = __byte_perm(v[0][w], v[1][w], 0x7362);
-                const uint32_t b01 = __byte_perm(v[2][w], v[3][w], 0x5140), b23 = __byte_perm(v[2][w], v[3][w], 0x7362);
-                uint32_t a0, a1, a2, a3, b0, b1, b2, b3;
-                e4m3x4_to_f16x4(a01, a0, a1);
-                e4m3x4_to_f16x4(a23, a2, a3);
-                e4m3x4_to_f16x4(b01, b0, b1);
-                e4m3x4_to_f16x4(b23, b2, b3);
-                mma(o[4 * w], pa, a0, b0);
-                mma(o[4 * w + 1], pa, a1, b1);
-                mma(o[4 * w + 2], pa, a2, b2);
-                mma(o[4 * w + 3], pa, a3, b3);
+            for (int w = 0; w < D / 32; ++w) {  // four channels: rows gid and gid + 8 of two products
+                uint32_t a[4], c[4];
+                e4m3x4_to_f16x4(__byte_perm(v[0][w], v[1][w], 0x5140), a[0], a[1]);
+                e4m3x4_to_f16x4(__byte_perm(v[2][w], v[3][w], 0x5140), a[2], a[3]);
+                e4m3x4_to_f16x4(__byte_perm(v[0][w], v[1][w], 0x7362), c[0], c[1]);
+                e4m3x4_to_f16x4(__byte_perm(v[2][w], v[3][w], 0x7362), c[2], c[3]);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    mma(o[nb][2 * w], a, pb[nb][0], pb[nb][1]);
+                    mma(o[nb][2 * w + 1], c, pb[nb][0], pb[nb][1]);
+                }
             }
         }
         __syncwarp();  // every lane has read the V slot
@@ -365,38 +398,38 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     if (!ok) let_copies_land();  // before the rings are used for anything else (a warp that came to its end has waited for all of its own)
     // ---- join the warps: weights first, then the rows, scaled, into shared memory ----
-    l_lo += __shfl_xor_sync(kAll, l_lo, 1);
-    l_hi += __shfl_xor_sync(kAll, l_hi, 1);
-    l_lo += __shfl_xor_sync(kAll, l_lo, 2);
-    l_hi += __shfl_xor_sync(kAll, l_hi, 2);
     constexpr float kBack = 1.f / 32768.f;  // 2^-kShift
-    if (t == 0) {
-        wm[warp][gid] = m_lo;
-        wm[warp][gid + 8] = m_hi;
-        wl[warp][gid] = l_lo * kBack;
-        wl[warp][gid + 8] = l_hi * kBack;
-    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int x = 4; x < 32; x *= 2) l[nb][e] += __shfl_xor_sync(kAll, l[nb][e], x);
+            if (gid == 0) {
+                wm[warp][nb * 8 + 2 * t + e] = m[nb][e];
+                wl[warp][nb * 8 + 2 * t + e] = l[nb][e] * kBack;
+            }
+        }
     __syncthreads();  // (every warp's ring is idle from here on)
-    float M_lo = -INFINITY, M_hi = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        M_lo = fmaxf(M_lo, wm[w][gid]);
-        M_hi = fmaxf(M_hi, wm[w][gid + 8]);
-    }
     const float unit = scale_of(v_unit);
-    const float f_lo = m_lo == -INFINITY ? 0.f : ex2_approx(m_lo - M_lo) * kBack, f_hi = m_hi == -INFINITY ? 0.f : ex2_approx(m_hi - M_hi) * kBack;
-    // [warp][row][D], a lane's D / 4 consecutive columns of two rows in pieces of 16 bytes (see piece_at)
-    float* part = reinterpret_cast<float*>(smem) + warp * kRows * D;
+    // [warp][row][D], a lane's D / 8 consecutive channels of two rows in pieces of 16 bytes (see piece_at)
+    float* part = reinterpret_cast<float*>(smem) + warp * ROWS * D;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-        constexpr int PER = D / 32;  // pieces of one of the lane's two columns
-        const int e = i / PER, n = i % PER * 4, c = t * (D / 16) + i;
-        *reinterpret_cast<float4*>(part + gid * D + piece_at<D>(gid, c) * 4) =
-            make_float4(o[n][e] * f_lo * unit, o[n + 1][e] * f_lo * unit, o[n + 2][e] * f_lo * unit, o[n + 3][e] * f_lo * unit);
-        *reinterpret_cast<float4*>(part + (gid + 8) * D + piece_at<D>(gid, c) * 4) =
-            make_float4(o[n][2 + e] * f_hi * unit, o[n + 1][2 + e] * f_hi * unit, o[n + 2][2 + e] * f_hi * unit, o[n + 3][2 + e] * f_hi * unit);
-    }
-    if (threadIdx.x < kRows) {
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = nb * 8 + 2 * t + e;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w][r]);
+            const float f = m[nb][e] == -INFINITY ? 0.f : ex2_approx(m[nb][e] - M) * kBack;
+#pragma unroll
+            for (int i = 0; i < MT_O; i += 2) {
+                const float4 x = make_float4(o[nb][i][e] * f * unit, o[nb][i][2 + e] * f * unit, o[nb][i + 1][e] * f * unit, o[nb][i + 1][2 + e] * f * unit);
+                *reinterpret_cast<float4*>(part + r * D + piece_at<D>(r, gid * (D / 32) + i / 2) * 4) = x;
+            }
+        }
+    if (threadIdx.x < ROWS) {
         const int r = threadIdx.x;
         float M = -INFINITY, L = 0.f;
         for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w][r]);
@@ -406,30 +439,30 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     __syncthreads();
     float* sum = reinterpret_cast<float*>(smem);  // the CTA's rows, in the place of warp 0's
-    for (int i = threadIdx.x; i < kRows * D; i += kWarps * 32) {
+    for (int i = threadIdx.x; i < ROWS * D; i += kWarps * 32) {
         float a = sum[i];
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) a += sum[w * kRows * D + i];
+        for (int w = 1; w < kWarps; ++w) a += sum[w * ROWS * D + i];
         sum[i] = a;
     }
     // ---- join the CTAs of the cluster; each writes its share of the outputs ----
     if (C > 1) cluster_sync(); else __syncthreads();
-    const int per = kRows * D / C;  // (C divides it)
+    const int per = ROWS * D / C;  // (C divides it)
     const uint32_t a_sum = smem_u32(sum), a_ml = smem_u32(cml);
     for (int i = rank * per + 2 * threadIdx.x; i < (rank + 1) * per; i += 2 * kWarps * 32) {
         const int r = i / D, c = piece_at<D>(r, (i - r * D) >> 2) * 4 + (i & 3);  // element i of the stored order is column c
-        float2 ml[MAX_C], v[MAX_C];
+        float2 ml[kMaxC], v[kMaxC];
 #pragma unroll
-        for (int q = 0; q < MAX_C; ++q) {  // all loads on their way before the first is used (ranks beyond C: this one again)
+        for (int q = 0; q < kMaxC; ++q) {  // all loads on their way before the first is used (ranks beyond C: this one again)
             const uint32_t from = q < C ? q : rank;
             ml[q] = ld_cluster(map_to_rank(a_ml + r * 8, from));
             v[q] = ld_cluster(map_to_rank(a_sum + i * 4, from));
         }
         float M = -INFINITY, L = 0.f, v0 = 0.f, v1 = 0.f;
 #pragma unroll
-        for (int q = 0; q < MAX_C; ++q) M = fmaxf(M, ml[q].x);
+        for (int q = 0; q < kMaxC; ++q) M = fmaxf(M, ml[q].x);
 #pragma unroll
-        for (int q = 0; q < MAX_C; ++q) {
+        for (int q = 0; q < kMaxC; ++q) {
             const float f = ml[q].x == -INFINITY ? 0.f : ex2_approx(ml[q].x - M);
             const bool own = q < C;  // (left out, not taken times zero: an infinite sum would become NaN)
             L = own ? fmaf(f, ml[q].y, L) : L;
@@ -439,6 +472,13 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         const int row = row0 + r;
         if (row < p.n_rows) {
             const int n = row / p.g.group, h = hk * p.g.group + (row - n * p.g.group);
+            const long long where = ((long long)b * p.g.heads + h) * p.g.N + n;
+            if (p.parts > 1) {
+                const long long there = (long long)key_part * p.g.batch * p.g.heads * p.g.N + where;
+                *reinterpret_cast<float2*>(p.part_O + there * D + c) = make_float2(v0, v1);
+                if (c == 0) p.part_ml[there] = make_float2(M, L);
+                continue;
+            }
             const int at = seq.start + n;
             // Decided by the position alone: a row at a position sees its own key at least, and a sum that is NaN belongs to its outputs.
             // (A row at none may have a sum: steps that the rows of the sequence see whole are not masked.)
@@ -446,21 +486,54 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             const float inv = any ? 1.f / L : 0.f;
             *reinterpret_cast<uint32_t*>(p.O + (long long)b * p.o_batch + (long long)h * p.o_head + (long long)n * p.o_row + c) =
                 any ? pack_16x2<F16>(v0 * inv, v1 * inv) : 0u;
-            if (c == 0) p.LSE[((long long)b * p.g.heads + h) * p.g.N + n] = any ? fmaf(M, 0.6931471805599453f, logf(L)) : -INFINITY;
+            if (c == 0) p.LSE[where] = any ? fmaf(M, 0.6931471805599453f, logf(L)) : -INFINITY;
         }
     }
     if (threadIdx.x == 0 && abort_flag) atomicExch(p.status, (int)BSA_ERR_DEVICE_TIMEOUT);
     if (C > 1) cluster_sync();  // nobody leaves while its shared memory is being read
 }
 
-template <int D, bool F16>
-cudaError_t launch(const WindowArgs& a, const CacheGeom& c, const Params& p, cudaStream_t stream) {
+// How a call is spread over the GPU, and where its workspace has what.
+struct Plan {
+    int C, parts, blocks;
+    int64_t part_ml, bytes;  // the partial sums' offset is zero
+};
+Plan plan_of(const WindowArgs& a) {
+    Plan w = {};
+    const int64_t rows = (int64_t)a.g.N * a.g.group, width = rows <= 8 ? 8 : 16;
+    w.blocks = (int)((rows + width - 1) / width);
+    const int64_t clusters = (int64_t)w.blocks * a.g.batch * a.g.heads_kv, KS = kSlot / a.d;
+    const int64_t longest = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N;
+    const int64_t steps = ((longest < a.g.N_kv ? longest : a.g.N_kv) + KS - 1) / KS;
+    // CTAs of a cluster: until the GPU is full (two per SM), and eight where a sequence may be long; not more than there are steps for their warps.
+    // Then parts: until the GPU is full, as long as a warp has six steps left, and until a warp has no more than 32.
+    const auto idle = [&](int64_t n) { return n * clusters < 2 * a.num_sms; };
+    w.C = w.parts = 1;
+    while (w.C < kMaxC && (int64_t)w.C * kWarps < steps && (idle(w.C) || steps > (int64_t)w.C * kWarps * 64)) w.C *= 2;
+    if (w.C == kMaxC)
+        while (w.parts < kMaxParts && ((idle(w.C * w.parts) && steps >= (int64_t)w.C * w.parts * 2 * kWarps * 6) || steps > (int64_t)w.C * w.parts * kWarps * 32)) w.parts *= 2;
+    if (w.parts > 1) {
+        const int64_t all = (int64_t)w.parts * a.g.batch * a.g.heads * a.g.N;
+        w.part_ml = (all * a.d * 4 + 255) / 256 * 256;
+        w.bytes = w.part_ml + (all * 8 + 255) / 256 * 256;
+    }
+    return w;
+}
+
+template <int D, bool F16, int NB>
+cudaError_t launch(const WindowArgs& a, const CacheGeom& c, const Params& p, const Plan& w, cudaStream_t stream) {
     constexpr int KS = kSlot / D, kSmem = kWarps * 2 * kRing;
     CUtensorMap tk, tv;
     if (!encode_codes_map(&tk, c.K, c.k_batch, c.k_head, c.k_row, c.N, c.heads, c.batch, D, KS) ||
         !encode_codes_map(&tv, c.V, c.v_batch, c.v_head, c.v_row, c.N, c.heads, c.batch, D, KS))
         return cudaErrorInvalidValue;
-    const auto kernel = cache_rows_kernel<D, F16, 8>, wide_kernel = cache_rows_kernel<D, F16, 16>;
+    const auto kernel = cache_rows_kernel<D, F16, NB>;
+    static std::atomic<bool> allowed[kMaxDevices];
+    if (!allowed[a.device].load(std::memory_order_relaxed)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        allowed[a.device].store(true, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(kWarps * 32);
     cfg.dynamicSmemBytes = kSmem;
@@ -470,40 +543,9 @@ cudaError_t launch(const WindowArgs& a, const CacheGeom& c, const Params& p, cud
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    static std::atomic<bool> allowed[kMaxDevices];
-    static std::atomic<int> resident8[kMaxDevices], resident16[kMaxDevices];  // clusters that the GPU holds at once
-    if (!allowed[a.device].load(std::memory_order_acquire)) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(wide_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(wide_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        int n = 0;
-        cfg.gridDim = dim3(attr[0].val.clusterDim.x = 8);
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
-        if (e != cudaSuccess) return e;
-        resident8[a.device].store(n, std::memory_order_relaxed);
-        cfg.gridDim = dim3(attr[0].val.clusterDim.x = 16);
-        if (cudaOccupancyMaxActiveClusters(&n, wide_kernel, &cfg) != cudaSuccess) {  // a GPU without a place for them
-            cudaGetLastError();
-            n = 0;
-        }
-        resident16[a.device].store(n, std::memory_order_relaxed);
-        allowed[a.device].store(true, std::memory_order_release);
-    }
-    const unsigned blocks = (unsigned)((p.n_rows + kRows - 1) / kRows), heads = (unsigned)(a.g.batch * a.g.heads_kv);
-    // CTAs of a cluster, by the rule of the kernel for the 16-bit cache (bsa_window_rows.cu has the figures): until the GPU is full, and eight at once
-    // where a sequence may be long; sixteen where eight leave the GPU idle and a warp has 64 steps and more.
-    const int64_t longest = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N;
-    const int64_t steps = ((longest < a.g.N_kv ? longest : a.g.N_kv) + KS - 1) / KS;
-    const auto idle = [&](int n) { return (int64_t)n * blocks * heads < 2 * a.num_sms; };
-    const auto long_shares = [&](int n) { return steps > (int64_t)n * kWarps * 64; };
-    int C = 1;
-    while (C < 8 && (int64_t)C * kWarps < steps && (idle(C) || long_shares(C))) C *= 2;
-    const int64_t clusters = (int64_t)blocks * heads;
-    const int at_once8 = resident8[a.device].load(std::memory_order_relaxed), at_once16 = resident16[a.device].load(std::memory_order_relaxed);
-    if (C == 8 && idle(8) && long_shares(8) && at_once16 > 0 && (clusters <= at_once16 || clusters > at_once8)) C = 16;
-    cfg.gridDim = dim3((unsigned)C, blocks, heads);
-    attr[0].val.clusterDim.x = (unsigned)C;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, C > 8 ? wide_kernel : kernel, tk, tv, p);
+    cfg.gridDim = dim3((unsigned)w.C, (unsigned)(w.blocks * w.parts), (unsigned)(a.g.batch * a.g.heads_kv));
+    attr[0].val.clusterDim.x = (unsigned)w.C;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, tk, tv, p);
     if (e == cudaSuccess) count_launch();
     return e;
 }
@@ -512,7 +554,10 @@ cudaError_t launch(const WindowArgs& a, const CacheGeom& c, const Params& p, cud
 
 cudaError_t set_cache_rows_wait_limit(long long cycles) { return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &cycles, sizeof cycles); }
 
-cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, cudaStream_t stream) {
+int64_t cache_rows_bytes(const WindowArgs& a) { return plan_of(a).bytes; }
+
+cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace, cudaStream_t stream) {
+    const Plan w = plan_of(a);
     Params p = {};
     p.g = a.g;
     p.Q = static_cast<const uint16_t*>(Q.data);
@@ -526,13 +571,22 @@ cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa
     p.s_head = c.s_head;
     p.lg_block = c.lg_block;
     p.last_block = c.blocks - 1;
+    p.parts = w.parts;
+    p.part_O = static_cast<float*>(workspace);
+    p.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + w.part_ml);
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.n_rows = a.g.N * a.g.group;
     p.withhold = window_withhold();
-    const cudaError_t e = window_status_word(a.device, &p.status);
+    cudaError_t e = window_status_word(a.device, &p.status);
     if (e != cudaSuccess) return e;
-    return a.d == 64 ? (a.f16 ? launch<64, true>(a, c, p, stream) : launch<64, false>(a, c, p, stream))
-                     : (a.f16 ? launch<128, true>(a, c, p, stream) : launch<128, false>(a, c, p, stream));
+    const auto of = [&](auto nb) {
+        constexpr int NB = decltype(nb)::value;
+        return a.d == 64 ? (a.f16 ? launch<64, true, NB>(a, c, p, w, stream) : launch<64, false, NB>(a, c, p, w, stream))
+                         : (a.f16 ? launch<128, true, NB>(a, c, p, w, stream) : launch<128, false, NB>(a, c, p, w, stream));
+    };
+    e = p.n_rows <= 8 ? of(std::integral_constant<int, 1>{}) : of(std::integral_constant<int, 2>{});
+    if (e != cudaSuccess || w.parts == 1) return e;
+    return launch_cache_join(a, w.parts, p.part_O, p.part_ml, nullptr, 0.f, O, LSE, stream);
 }
 
 }  // namespace bsa

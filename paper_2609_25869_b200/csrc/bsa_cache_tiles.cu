@@ -935,7 +935,8 @@ struct JoinParams {
     WindowGeom g;
     const float* part_O;
     const float2* part_ml;
-    const int32_t* refs;
+    const int32_t* refs;  // or NULL
+    float shift;
     int parts;
     uint16_t* O;
     long long o_batch, o_head, o_row;
@@ -968,10 +969,10 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const __grid_c
         o.z = fmaf(f, x.z, o.z);
         o.w = fmaf(f, x.w, o.w);
     }
-    const float inv = 1.f / L * scale_of(p.refs[2 * (b * p.g.heads_kv + h / p.g.group) + 1]);
+    const float inv = 1.f / L * (p.refs ? scale_of(p.refs[2 * (b * p.g.heads_kv + h / p.g.group) + 1]) : 1.f);
     uint16_t* out = p.O + (long long)b * p.o_batch + (long long)h * p.o_head + (long long)n * p.o_row + c;
     *reinterpret_cast<uint2*>(out) = seen ? make_uint2(pack_16x2<F16>(o.x * inv, o.y * inv), pack_16x2<F16>(o.z * inv, o.w * inv)) : make_uint2(0u, 0u);
-    if (c == 0) p.LSE[at] = seen ? fmaf(M - kShift, 0.6931471805599453f, logf(L)) : -INFINITY;
+    if (c == 0) p.LSE[at] = seen ? fmaf(M - p.shift, 0.6931471805599453f, logf(L)) : -INFINITY;
 }
 
 // ---- host ----
@@ -1091,27 +1092,40 @@ cudaError_t launch(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q,
     count_launch();
     if (w.parts == 1) return cudaSuccess;
 
-    JoinParams j = {};
-    j.g = a.g;
-    j.part_O = p.part_O;
-    j.part_ml = p.part_ml;
-    j.refs = p.refs;
-    j.parts = w.parts;
-    j.O = p.O;
-    j.o_batch = p.o_batch; j.o_head = p.o_head; j.o_row = p.o_row;
-    j.LSE = LSE;
-    constexpr int PER = kJoinThreads / (D / 4);
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.dynamicSmemBytes = 0;
-    cfg.gridDim = dim3((unsigned)((w.rows + PER - 1) / PER));
-    if ((e = cudaLaunchKernelEx(&cfg, cache_join_kernel<D, F16>, j)) != cudaSuccess) return e;
-    count_launch();
-    return cudaSuccess;
+    return launch_cache_join(a, w.parts, p.part_O, p.part_ml, p.refs, kShift, O, LSE, stream);
 }
 
 }  // namespace
 
 cudaError_t set_cache_tiles_wait_limit(long long cycles) { return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &cycles, sizeof cycles); }
+
+cudaError_t launch_cache_join(const WindowArgs& a, int parts, const float* part_O, const float2* part_ml, const int32_t* refs, float shift,
+                              const bsa_view_t& O, float* LSE, cudaStream_t stream) {
+    JoinParams j = {};
+    j.g = a.g;
+    j.part_O = part_O;
+    j.part_ml = part_ml;
+    j.refs = refs;
+    j.shift = shift;
+    j.parts = parts;
+    j.O = static_cast<uint16_t*>(O.data);
+    j.o_batch = O.batch; j.o_head = O.head; j.o_row = O.row;
+    j.LSE = LSE;
+    const int64_t rows = (int64_t)a.g.batch * a.g.heads * a.g.N, per = kJoinThreads / (a.d / 4);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.gridDim = dim3((unsigned)((rows + per - 1) / per));
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, a.d == 64 ? (a.f16 ? cache_join_kernel<64, true> : cache_join_kernel<64, false>)
+                                                             : (a.f16 ? cache_join_kernel<128, true> : cache_join_kernel<128, false>), j);
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
 
 int64_t cache_tiles_bytes(const WindowArgs& a) { return plan_of(a).bytes; }
 double cache_tiles_time(const WindowArgs& a) { return plan_of(a).us; }

@@ -675,8 +675,15 @@ def cache_create(batch: int, heads_kv: int, N: int, d: int, *, block: int = 64, 
                  new(scales, torch.float8_e8m0fnu), block=block, layout=layout)
 
 
-def _cache_rows(cache: Cache, K, V, start, count):
-    """(packed bsa_cache_rows_t, packed views of K and V): what writing and reading check alike."""
+def _cache_rows(cache: Cache, N: int, dt: int, start, count) -> bytes:
+    """Packed bsa_cache_rows_t."""
+    b, dev = cache.batch, cache.device
+    return _ROWS.pack(N, dt, 0, 0 if start is None else _int32_ptr(start, ((b,),), dev, "start"),
+                      0 if count is None else _int32_ptr(count, ((b,),), dev, "count"))
+
+
+def _cache_views(cache: Cache, K, V):
+    """(tokens, type id, packed views of K and V): what writing and reading check alike."""
     nhd = LAYOUTS[cache.layout] == 1
     dt, dev = _tensor_of(K, "K")
     if dev != cache.device:
@@ -684,17 +691,16 @@ def _cache_rows(cache: Cache, K, V, start, count):
     b, h, n, d, vk = _view(K, nhd, K.dtype, dev, "K")
     if b != cache.batch or h != cache.heads or d != cache.d or V.shape != K.shape or K.dim() != cache.K.dim():
         raise ValueError("K and V have to have one shape, and batch, heads and channels of the cache")
-    vv = _view(V, nhd, K.dtype, dev, "V")[4]
-    return _ROWS.pack(n, dt, 0, 0 if start is None else _int32_ptr(start, ((b,),), dev, "start"),
-                      0 if count is None else _int32_ptr(count, ((b,),), dev, "count")), vk, vv, dev
+    return n, dt, vk, _view(V, nhd, K.dtype, dev, "V")[4]
 
 
 def cache_write(cache: Cache, K, V, *, start=None, count=None, stream=None) -> None:
     """``bsa_cache_write``: rows of K and V (bf16 or fp16, the cache's layout, N of them) become the cache's tokens ``start .. start +
     count - 1``.  ``start``, ``count``: int32 CUDA tensors ``[batch]`` (default: 0, and all rows); tokens outside of the cache are left out.
     A write ends its sequences: tokens behind it are no longer valid where they share a block with it."""
-    rows, vk, vv, dev = _cache_rows(cache, K, V, start, count)
-    _call(dev, stream, "bsa_cache_write", lib().bsa_cache_write, cache._packed, rows, vk, vv)
+    n, dt, vk, vv = _cache_views(cache, K, V)
+    rows = _cache_rows(cache, n, dt, start, count)
+    _call(cache.device, stream, "bsa_cache_write", lib().bsa_cache_write, cache._packed, rows, vk, vv)
 
 
 def cache_read(cache: Cache, N: int, *, start=None, count=None, dtype=None, K=None, V=None, stream=None):
@@ -703,19 +709,27 @@ def cache_read(cache: Cache, N: int, *, start=None, count=None, dtype=None, K=No
     if (K is None) != (V is None):
         raise ValueError("K and V are given together")
     if K is None:
-        tokens = -3 if LAYOUTS[cache.layout] == 1 else -2
-        shape = list(cache.K.shape)
-        shape[tokens] = N
-        dtype = dtype or _tensors().bfloat16
+        torch = _torch or _tensors()
+        dtype = dtype or torch.bfloat16
+        dt = _DTYPE_IDS.get(dtype)
+        if dt is None:
+            raise ValueError("dtype has to be torch.bfloat16 or torch.float16")
+        b, h, d = cache.batch, cache.heads, cache.d
+        shape = (h, N, d) if cache.layout == "hnd" else (N, h, d)
+        if len(cache.K.shape) == 4:
+            shape = (b, *shape)
         if stream is None:
-            K, V = (_torch.empty(shape, dtype=dtype, device=cache.K.device) for _ in range(2))
+            K, V = cache.K.new_empty(shape, dtype=dtype), cache.K.new_empty(shape, dtype=dtype)
         else:
             with _pool(stream, cache.device):
-                K, V = (_torch.empty(shape, dtype=dtype, device=cache.K.device) for _ in range(2))
-    elif K.dim() < 3 or K.shape[-3 if LAYOUTS[cache.layout] == 1 else -2] != N or (dtype is not None and K.dtype is not dtype):
-        raise ValueError("K and V have to have N tokens and the given type")
-    rows, vk, vv, dev = _cache_rows(cache, K, V, start, count)
-    _call(dev, stream, "bsa_cache_read", lib().bsa_cache_read, cache._packed, rows, vk, vv)
+                K, V = cache.K.new_empty(shape, dtype=dtype), cache.K.new_empty(shape, dtype=dtype)
+        strides = (h * N * d, N * d, d) if cache.layout == "hnd" else (h * N * d, d, h * d)
+        vk, vv = _VIEW.pack(K.data_ptr(), *strides), _VIEW.pack(V.data_ptr(), *strides)
+    else:
+        n, dt, vk, vv = _cache_views(cache, K, V)
+        if n != N or (dtype is not None and K.dtype is not dtype):
+            raise ValueError("K and V have to have N tokens and the given type")
+    _call(cache.device, stream, "bsa_cache_read", lib().bsa_cache_read, cache._packed, _cache_rows(cache, N, dt, start, count), vk, vv)
     return K, V
 
 

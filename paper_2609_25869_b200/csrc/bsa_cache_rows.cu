@@ -143,17 +143,18 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     // steps of KS keys: [0, st) and [w0, w1), as the tiles of the other kernel
     const int w0 = range.lo / KS, w1 = (range.hi + KS - 1) / KS, st = min((range.sink_hi + KS - 1) / KS, w0);
     const int steps = st + (w1 - w0);
-    const long long share = (long long)p.parts * C * kWarps, mine = ((long long)key_part * C + rank) * kWarps + warp;
-    const int first = (int)(steps * mine / share), last = (int)(steps * (mine + 1) / share);
+    // The CTA's share of them is one run, its warps take turns.
+    const long long share = (long long)p.parts * C, mine = (long long)key_part * C + rank;
+    const int first = (int)(steps * mine / share) + warp, last = (int)(steps * (mine + 1) / share);
     auto key_of = [&](int j) { return (j < st ? j : w0 + (j - st)) * KS; };
     auto copy_in = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int key0) {
         mbar_arrive_expect_tx(bar, kSlot);
         tma_load_4d(dst, map, bar, 0, key0, hk, b);
     };
     if (lane == 0) {
-        for (int i = 0; i < kSlots && first + i < last; ++i) {
-            copy_in(sK + i * kSlot, &tmK, bK + i * 8, key_of(first + i));
-            if (!(p.withhold && i == 0)) copy_in(sV + i * kSlot, &tmV, bV + i * 8, key_of(first + i));
+        for (int i = 0; i < kSlots && first + i * kWarps < last; ++i) {
+            copy_in(sK + i * kSlot, &tmK, bK + i * 8, key_of(first + i * kWarps));
+            if (!(p.withhold && i == 0)) copy_in(sV + i * kSlot, &tmV, bV + i * 8, key_of(first + i * kWarps));
         }
     }
     // A step's scales: lanes 0 .. G - 1 have K's, lanes 16 .. 16 + G - 1 V's, a step ahead.
@@ -166,7 +167,6 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     // are channels x * 64 + t * 16 + y * 4 .. + 3.
     uint32_t qb[NB][KS_QK][2];
     float c2[NB][2];  // what takes the products of rows 2t and 2t + 1 to scores (log2 domain), but for K's scale
-    int pos[NB][2];   // and where they stand
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const int r = row0 + nb * 8 + gid;
@@ -204,11 +204,7 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 }
         }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            c2[nb][e] = __shfl_sync(kAll, factor, (2 * t + e) * 4);
-            const int re = row0 + nb * 8 + 2 * t + e;
-            pos[nb][e] = re < p.n_rows ? seq.start + re / p.g.group : -1;
-        }
+        for (int e = 0; e < 2; ++e) c2[nb][e] = __shfl_sync(kAll, factor, (2 * t + e) * 4);
     }
     float o[NB][MT_O][4];
     float m[NB][2], l[NB][2];  // maxima of rows 2t, 2t + 1, this thread's share of their sums
@@ -225,12 +221,12 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     bool ok = true;
     const int ke = key_even<D>(t), ko = ke ^ kOdd<D>;                                // the keys behind rows 2t and 2t + 1 of a product
     const int kg = key_even<D>((gid >> 1) & 3) ^ ((gid & 1) ? kOdd<D> : 0);  // and behind row gid
-    for (int j = first; j < last; ++j) {
+    for (int j = first; j < last; j += kWarps) {
         const int key0 = key_of(j);
         const uint32_t cK = sK + slot * kSlot, cV = sV + slot * kSlot;
         const uint8_t *gK = smem + warp * 2 * kRing + slot * kSlot, *gV = gK + kRing;
         const int code = next_code;
-        if (j + 1 < last) next_code = load_scale(j + 1);
+        if (j + kWarps < last) next_code = load_scale(j + kWarps);
         ok = mbar_wait_warp(bK + slot * 8, phase, abortp);
         if (!ok) break;
         float s[G][NB][4];  // keys kg, kg + 8 of a group x rows 2t, 2t + 1
@@ -256,7 +252,7 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 }
         }
         __syncwarp();  // every lane has read the K slot
-        if (lane == 0 && j + kSlots < last) copy_in(cK, &tmK, bK + slot * 8, key_of(j + kSlots));
+        if (lane == 0 && j + kSlots * kWarps < last) copy_in(cK, &tmK, bK + slot * 8, key_of(j + kSlots * kWarps));
         int vc[G];  // V's codes; of groups that nobody here sees, zero
         int v_most = v_unit;
         const bool full = key0 + KS <= range.all_hi && (key0 >= range.all_lo || key0 + KS <= p.g.sinks);
@@ -284,7 +280,8 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const RowView view(p.g, seq, pos[nb][e], key0);
+                    const int r = row0 + nb * 8 + 2 * t + e;
+                    const RowView view(p.g, seq, r < p.n_rows ? seq.start + r / p.g.group : -1, key0);
 #pragma unroll
                     for (int w = 0; w < KS / 32; ++w) {
                         const uint32_t bits = view.bits(w * 32) >> kg;
@@ -390,7 +387,7 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             }
         }
         __syncwarp();  // every lane has read the V slot
-        if (lane == 0 && j + kSlots < last) copy_in(cV, &tmV, bV + slot * 8, key_of(j + kSlots));
+        if (lane == 0 && j + kSlots * kWarps < last) copy_in(cV, &tmV, bV + slot * 8, key_of(j + kSlots * kWarps));
         if (++slot == kSlots) {
             slot = 0;
             phase ^= 1u;
@@ -506,12 +503,25 @@ Plan plan_of(const WindowArgs& a) {
     const int64_t longest = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N;
     const int64_t steps = ((longest < a.g.N_kv ? longest : a.g.N_kv) + KS - 1) / KS;
     // CTAs of a cluster: until the GPU is full (two per SM), and eight where a sequence may be long; not more than there are steps for their warps.
-    // Then parts: until the GPU is full, as long as a warp has six steps left, and until a warp has no more than 32.
     const auto idle = [&](int64_t n) { return n * clusters < 2 * a.num_sms; };
     w.C = w.parts = 1;
     while (w.C < kMaxC && (int64_t)w.C * kWarps < steps && (idle(w.C) || steps > (int64_t)w.C * kWarps * 64)) w.C *= 2;
-    if (w.C == kMaxC)
-        while (w.parts < kMaxParts && ((idle(w.C * w.parts) && steps >= (int64_t)w.C * w.parts * 2 * kWarps * 6) || steps > (int64_t)w.C * w.parts * kWarps * 32)) w.parts *= 2;
+    // Where a warp has more than twelve steps, clusters of four (they find places more easily) and as many parts as make the call shortest, counted in
+    // steps (2.2 us of a warp with the GPU full): a CTA's start and end take two; the places share all of it, in rounds where the lengths are one,
+    // else, lengths being half of the longest, with a quarter of a CTA's time behind; alone a CTA takes 0.7 of that; the join 1.5.
+    // us, d = 128, CTAs x parts 8 x 1 / 8 x 4 / 4 x 4 / 4 x 8 / 4 x 16: 8 x 65536 keys, 8 key heads 185 / 191 / 178 / 187 / 219; six sequences of 1111 to 115200
+    // keys 138 / 144 / 135 / 142 / 168; one of 65536 45 / 33 / 33 / 33 / 39.
+    if (w.C == kMaxC && steps > kMaxC * kWarps * 12) {
+        w.C = 4;
+        const auto cost = [&](int parts) {
+            const double each = (double)steps / (4 * kWarps * parts), ctas = 4.0 * parts * clusters / (1.8 * a.num_sms);  // (not every place suits a cluster)
+            const double rest = ctas - floor(ctas), rounds = floor(ctas) + (rest > 0 ? fmax(rest, 0.7) : 0.0);
+            const double all = a.g.kv_len ? fmax(ctas * (0.5 * each + 2) + 0.25 * (each + 2), 0.7 * each + 2) : rounds * (each + 2);
+            return all + (parts > 1 ? 1.5 : 0.0);
+        };
+        for (int parts = 2; parts <= kMaxParts; ++parts)
+            if (cost(parts) < cost(w.parts)) w.parts = parts;
+    }
     if (w.parts > 1) {
         const int64_t all = (int64_t)w.parts * a.g.batch * a.g.heads * a.g.N;
         w.part_ml = (all * a.d * 4 + 255) / 256 * 256;

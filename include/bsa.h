@@ -479,8 +479,12 @@ BSA_API bsa_status_t bsa_cache_read(const bsa_cache_t* cache, const bsa_cache_ro
 
 /* bsa_cache_forward -- bsa_window_forward over a cache: desc, Q, O and LSE as there (desc's batch, heads_kv, d and N_kv are the cache's), the same
  * keys seen, the same treatment of what nobody sees, of padding and of NaN.  A block's scale of 255 reaches the rows of a tile that see any of it.
- *   Few rows per key head: codes widen to half, which is exact, and P is rounded to half.  More: the visible keys and values go through
- *   workspace_dev in the element type (values beyond its range: its largest number) and P is rounded to that.
+ *   Scores, softmax and accumulators are fp32, outputs are rounded once.  Which of three ways a call goes follows from its sizes:
+ *     few rows per key head: codes widen to half, which is exact (a row of bf16 queries is taken times a power of two), P is rounded to half;
+ *     rows by the tile: the visible keys and values go through workspace_dev in the element type (values beyond its range: its largest number), P is
+ *     rounded to that;
+ *     or, where such rows leave SMs without work: K's codes as they are, an element of Q as two (half: three) numbers of 8 bits that are off by 2^-20 of
+ *     the row's largest element at most, V's codes widened to half (off by 2^-32 of the largest value of the head's window at most), P rounded to half.
  *   workspace_dev: bsa_cache_workspace_bytes(desc, cache) bytes (0: none is needed; also for what the call refuses) on a 256-byte boundary, the call's
  *   own until its work on the stream is done.
  * Errors: as bsa_window_forward and bsa_cache_write; INVALID_ARG too where desc and cache disagree or the workspace is too small. */

@@ -473,6 +473,7 @@ extern "C" bsa_status_t bsa_cache_forward(const bsa_window_desc_t* t, const bsa_
         if (O->data == in || (void*)LSE == in) return BSA_ERR_INVALID_ARG;
     if ((st = window_device(&a)) != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
+    if ((int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
     const Way way = way_of(a);
     const int64_t need = workspace_of(a, way);
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return BSA_ERR_INVALID_ARG;

@@ -995,7 +995,7 @@ Plan plan_of(const WindowArgs& a) {
     const int64_t items = (int64_t)w.tiles * a.g.batch * a.g.heads, pairs = a.num_sms / 2, tiles = (keys + kWinT - 1) / kWinT;
     const auto cost = [&](int64_t s) { return (items * s + pairs - 1) / pairs * ((tiles + s - 1) / s + 4) + (s > 1 ? 8 : 0); };
     w.parts = 1;
-    for (int s = 2; s <= kMaxParts && s * 4 <= tiles; ++s)
+    for (int s = 2; s <= kMaxParts && s * 4 <= tiles && items * s < (1 << 24); ++s)  // (where there are more items parts bring nothing)
         if (cost(s) < cost(w.parts)) w.parts = s;
     w.us = (double)cost(w.parts) * (a.d == 128 ? 1.3 : 1.2);
     int64_t at = 0;

@@ -514,3 +514,80 @@ def test_the_binding_refuses_what_does_not_fit():
         bsa.Cache(cache.K, cache.V[:1], cache.K_scale, cache.V_scale)
     with pytest.raises(ValueError):
         bsa.Cache(cache.K, cache.V, cache.K_scale, cache.V_scale.view(torch.uint8))
+
+
+def test_first_calls_in_a_captured_graph():
+    """Nothing that a first call sets up (attributes, addresses, module loading) is refused while a stream is being captured."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2609_25869_b200 import bsa
+cache = bsa.cache_create(1, 2, 6000, 64, block=16)
+x = [torch.randn(1, h, 6000, 64, device='cuda').bfloat16() for h in (4, 2, 2)]
+calls = [(1, -1), (300, 200), (300, -1), (3, -1)]
+def run():
+    out = []
+    bsa.cache_write(cache, x[1], x[2])
+    for n, left in calls:
+        out += bsa.cache_forward(x[0][:, :, -n:], cache, left=left, sinks=2)
+    return out + list(bsa.cache_read(cache, 100))
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    got = run()
+g.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, run())) and bsa.window_status() == 0
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("n,nk,left", [(300, 700, 100), (300, 6000, -1), (1, 40000, -1)])
+def test_workspaces(n, nk, left):
+    """Too small, misaligned or missing ones are refused; calls that overlap bring their own, and bytes behind one stay."""
+    cache, _ = filled(25, 1, 2, nk, 64, "bf16", "hnd", 64)
+    q = queries(11, 1, 4, n, 64, "bf16", "hnd")
+    O, L = bsa.cache_forward(q, cache, left=left)
+    lib = bsa.lib()
+    desc = bsa._WINDOW.pack(1, 4, 2, 64, n, nk, left, 0, 0, 0, 0.0, 0, 0)
+    need = lib.bsa_cache_workspace_bytes(desc, cache._packed)
+    assert need > 0
+    vq = bsa._view(q, False, q.dtype, 0, "Q")[4]
+    O2, L2 = torch.empty_like(O), torch.empty_like(L)
+    vo = bsa._view(O2, False, q.dtype, 0, "O")[4]
+    ws = torch.full((need + 1024,), 77, dtype=torch.uint8, device="cuda")
+    for at, size in ((None, need), (ws.data_ptr(), need - 1), (ws.data_ptr() + 16, need), (ws.data_ptr(), 0)):
+        assert lib.bsa_cache_forward(desc, cache._packed, vq, vo, L2.data_ptr(), at, size, None) == 1
+    assert lib.bsa_cache_forward(desc, cache._packed, vq, vo, L2.data_ptr(), ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream or None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(O, O2) and torch.equal(L, L2) and (ws[need:] == 77).all()
+
+
+def test_two_calls_at_once():
+    """Reads, writes of another cache and attention of all three kinds on four streams at once, again and again."""
+    caches = [filled(26 + i, 1, 2, nk, 64, "bf16", "hnd", 64)[0] for i, nk in enumerate((40000, 700, 6000))]
+    qs = [queries(12 + i, 1, 4, n, 64, "bf16", "hnd") for i, n in enumerate((1, 300, 300))]
+    calls = [lambda i=i: bsa.cache_forward(qs[i], caches[i], left=100 if i == 1 else -1) for i in range(3)]
+    want = [c() for c in calls]
+    K, V = bsa.cache_read(caches[2], 6000)
+    other = bsa.cache_create(1, 2, 6000, 64)
+
+    def copy():
+        bsa.cache_write(other, K, V)
+        return bsa.cache_read(other, 6000)
+    calls.append(copy)
+    want.append((K, V))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        got = []
+        for s, c in zip(streams, calls):
+            with torch.cuda.stream(s):
+                got.append(c())
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert bsa.window_status() == 0

@@ -183,6 +183,7 @@ constexpr int kReadThreads = 256, kReadUnits = 4;
 template <int D, bool F16, bool WINDOW>
 __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(const __grid_constant__ ReadParams p) {
     constexpr int ROW = D / 16;
+    if (WINDOW) grid_launch_dependents();
     const int b = blockIdx.y;
     int h, run;
     bool is_v;
@@ -379,7 +380,7 @@ bsa_status_t forward_unpacked(WindowArgs a, const CacheGeom& g, const bsa_view_t
     a.g.q_start = p.q_start;
     a.g.kv_len = p.kv_len;
     const bsa_view_t k{p.K, p.k_batch, p.k_head, p.k_row}, v{p.V, p.v_batch, p.v_head, p.v_row};
-    return launch_window_tiles(a, Q, k, v, O, LSE, even, stream);
+    return launch_window_tiles(a, Q, k, v, O, LSE, even, true, stream);
 }
 
 // What a description of attention and a cache have to agree in.

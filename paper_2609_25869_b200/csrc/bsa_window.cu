@@ -182,6 +182,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_s, 0);
     volatile uint32_t* abortp = &abort_flag;
+    grid_dependency_wait();  // (where a kernel in front writes K, V, starts and lengths)
     Item it;
 
     if (warp >= 12) {
@@ -558,7 +559,7 @@ window_forward_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
 }
 
 template <int D, bool F16>
-cudaError_t launch_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, Params p, cudaStream_t stream) {
+cudaError_t launch_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, Params p, bool behind, cudaStream_t stream) {
     CUtensorMap tq, tk, tv;
     if (!encode_view_map(&tq, Q, a.g.N, a.g.heads, a.g.batch, D, kWinT, F16) ||
         !encode_view_map(&tk, K, a.g.N_kv, a.g.heads_kv, a.g.batch, D, kWinT, F16) ||
@@ -572,9 +573,19 @@ cudaError_t launch_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view
         allowed[a.device].store(true, std::memory_order_relaxed);
     }
     const int grid = a.num_sms < p.order.n_items ? a.num_sms : p.order.n_items;
-    kernel<<<grid, kThreads, Cfg<D>::kSmem, stream>>>(tq, tk, tv, p);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Cfg<D>::kSmem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = behind ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, tq, tk, tv, p);
     count_launch();
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace
@@ -642,7 +653,7 @@ bool window_takes_rows(const WindowArgs& a) {
 }
 
 bsa_status_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
-                                 float* LSE, bool even, cudaStream_t stream) {
+                                 float* LSE, bool even, bool behind, cudaStream_t stream) {
     Params p = {};
     p.g = a.g;
     p.O = static_cast<uint16_t*>(O.data);
@@ -656,8 +667,8 @@ bsa_status_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const
     p.order = ItemOrder(n_qt, even ? 0 : cut_tiles(a.g, n_qt), a.g.batch * a.g.heads);
     p.heads = Divisor(a.g.heads);
     p.group = Divisor(a.g.group);
-    const cudaError_t e = a.d == 64 ? (a.f16 ? launch_rows<64, true>(a, Q, K, V, p, stream) : launch_rows<64, false>(a, Q, K, V, p, stream))
-                                    : (a.f16 ? launch_rows<128, true>(a, Q, K, V, p, stream) : launch_rows<128, false>(a, Q, K, V, p, stream));
+    const cudaError_t e = a.d == 64 ? (a.f16 ? launch_rows<64, true>(a, Q, K, V, p, behind, stream) : launch_rows<64, false>(a, Q, K, V, p, behind, stream))
+                                    : (a.f16 ? launch_rows<128, true>(a, Q, K, V, p, behind, stream) : launch_rows<128, false>(a, Q, K, V, p, behind, stream));
     if (e != cudaSuccess) {
         set_cuda_err(e, "bsa_window_forward");
         return BSA_ERR_CUDA;
@@ -682,7 +693,7 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     if (st != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
     if ((int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
-    if (!window_takes_rows(a)) return launch_window_tiles(a, *Q, *K, *V, *O, LSE, false, stream);
+    if (!window_takes_rows(a)) return launch_window_tiles(a, *Q, *K, *V, *O, LSE, false, false, stream);
     const cudaError_t e = launch_window_rows(a, *Q, *K, *V, *O, LSE, stream);
     if (e != cudaSuccess) {
         set_cuda_err(e, "bsa_window_forward");

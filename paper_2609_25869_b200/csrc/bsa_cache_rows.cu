@@ -67,18 +67,23 @@ struct Params {
     int* status;
 };
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t map_to_rank(uint32_t smem, uint32_t rank) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float2 ld_cluster(uint32_t addr) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
+// 16 (8) bytes to another CTA's shared memory; they count at a barrier there.
+__device__ __forceinline__ void send(uint32_t to, const float4& v, uint32_t bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "r"(__float_as_uint(v.x)),
+                 "r"(__float_as_uint(v.y)), "r"(__float_as_uint(v.z)), "r"(__float_as_uint(v.w)), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void send(uint32_t to, const float2& v, uint32_t bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(to), "r"(__float_as_uint(v.x)),
+                 "r"(__float_as_uint(v.y)), "r"(bar)
+                 : "memory");
 }
 // (Not volatile, as loads from the ring are plain ones: the compiler may put other products and loads between those that depend on each other.
 // In program order a step took 5000 clk of a warp that had its SM's quarter nearly to itself.)
@@ -122,25 +127,55 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[kWarps][2 * kSlots];  // K slots, then V slots: the copy has landed
     __shared__ float wm[kWarps][ROWS], wl[kWarps][ROWS];        // the warps' maxima (log2 domain) and sums
-    __shared__ __align__(8) float2 cml[ROWS];                   // the CTA's
+    // What the cluster's CTAs send to this one: their sums of this one's share of the rows, [C][ROWS * D / C], and their maxima and weights' sums.
+    __shared__ __align__(16) float in_sum[ROWS * D];
+    __shared__ __align__(8) float2 in_ml[kMaxC][ROWS];
+    __shared__ __align__(8) uint64_t in_bar;
     __shared__ uint32_t abort_flag;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, t = lane & 3;
     const int C = gridDim.x, rank = blockIdx.x;
     const int b = blockIdx.z / p.g.heads_kv, hk = blockIdx.z - b * p.g.heads_kv, key_part = blockIdx.y % p.parts, row0 = blockIdx.y / p.parts * ROWS;
+    // Everything that does not wait for something else is on its way first: lengths, then Q (behind the copies it came 6000 clk later), then barriers.
+    const Sequence seq = load_sequence(p.g, b);
+    // Q^T fragments (B operand, 16 channels x 8 rows per step) of row gid of each eight: positions 2t, 2t + 1, 2t + 8, 2t + 9 of product x * 4 + y
+    // are channels x * 64 + t * 16 + y * 4 .. + 3.
+    uint32_t qb[NB][KS_QK][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int r = row0 + nb * 8 + gid;
+        const int n = r / p.g.group, h = hk * p.g.group + (r - n * p.g.group);
+        const uint16_t* q = p.Q + (long long)b * p.q_batch + (long long)h * p.q_head + (long long)n * p.q_row;
+#pragma unroll
+        for (int x = 0; x < HALVES; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const uint4 v = r < p.n_rows ? __ldg(reinterpret_cast<const uint4*>(q + x * 64 + t * 16 + y * 8)) : make_uint4(0, 0, 0, 0);
+                const int ks = x * 4 + y * 2;
+                qb[nb][ks][0] = v.x;
+                qb[nb][ks][1] = v.y;
+                qb[nb][ks + 1][0] = v.z;
+                qb[nb][ks + 1][1] = v.w;
+            }
+    }
     const uint32_t sK = smem_u32(smem) + warp * 2 * kRing, sV = sK + kRing;
     const uint32_t bK = smem_u32(&bars[warp][0]), bV = bK + kSlots * 8;
-    if (threadIdx.x == 0) abort_flag = 0;
+    const int per = ROWS * D / C;  // (C divides it) this CTA's share of the outputs, in the partial sums' order
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        mbar_init(smem_u32(&in_bar), 1);
+    }
     if (lane == 0) {
         prefetch_tensormap(&tmK);
         prefetch_tensormap(&tmV);
         for (int i = 0; i < 2 * kSlots; ++i) mbar_init(bK + i * 8, 1);
         fence_mbar_init();
     }
+    if (threadIdx.x == 0) mbar_arrive_expect_tx(smem_u32(&in_bar), C * (per * 4 + ROWS * 8));
     __syncthreads();
+    cluster_arrive();  // (waited for in front of the first thing sent)
     volatile uint32_t* abortp = &abort_flag;
 
     // Row r of the key head is query token r / group under query head hk * group + r % group.
-    const Sequence seq = load_sequence(p.g, b);
     const int n0 = row0 / p.g.group, n1 = min((row0 + ROWS - 1) / p.g.group + 1, p.g.N);
     const KeyRange range = key_range(p.g, seq, n0, n1);
     // steps of KS keys: [0, st) and [w0, w1), as the tiles of the other kernel
@@ -166,33 +201,16 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         return (lane & 15) < G ? (int)__ldg(scales + min((key_of(j) + (lane & 15) * 16) >> p.lg_block, p.last_block)) : 0;
     };
     int next_code = first < last ? load_scale(first) : 0;
-    // Q^T fragments (B operand, 16 channels x 8 rows per step) of row gid of each eight: positions 2t, 2t + 1, 2t + 8, 2t + 9 of product x * 4 + y
-    // are channels x * 64 + t * 16 + y * 4 .. + 3.
-    uint32_t qb[NB][KS_QK][2];
     float c2[NB][2];  // what takes the products of rows 2t and 2t + 1 to scores (log2 domain), but for K's scale
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const int r = row0 + nb * 8 + gid;
-        const int n = r / p.g.group, h = hk * p.g.group + (r - n * p.g.group);
-        const bool ok = r < p.n_rows;
-        const uint16_t* q = p.Q + (long long)b * p.q_batch + (long long)h * p.q_head + (long long)n * p.q_row;
-        uint32_t most = 0;
-#pragma unroll
-        for (int x = 0; x < HALVES; ++x) {
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const uint4 v = ok ? __ldg(reinterpret_cast<const uint4*>(q + x * 64 + t * 16 + y * 8)) : make_uint4(0, 0, 0, 0);
-                const int ks = x * 4 + y * 2;
-                qb[nb][ks][0] = v.x;
-                qb[nb][ks][1] = v.y;
-                qb[nb][ks + 1][0] = v.z;
-                qb[nb][ks + 1][1] = v.w;
-                if (!F16)
-                    for (const uint32_t w : {v.x, v.y, v.z, v.w}) most = max(most, max((w >> 7) & 0xffu, (w >> 23) & 0xffu));
-            }
-        }
         float factor = p.scale_log2;
         if (!F16) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int ks = 0; ks < KS_QK; ++ks)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) most = max(most, max((qb[nb][ks][k] >> 7) & 0xffu, (qb[nb][ks][k] >> 23) & 0xffu));
             most = max(most, __shfl_xor_sync(kAll, most, 1));
             most = max(most, __shfl_xor_sync(kAll, most, 2));
             const int field = min(268 - (int)most, 253);  // of the factor that takes exponent most - 127 to 14, and of a finite inverse
@@ -429,45 +447,53 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 *reinterpret_cast<float4*>(part + r * D + piece_at<D>(r, gid * (D / 32) + i / 2) * 4) = x;
             }
         }
-    if (threadIdx.x < ROWS) {
-        const int r = threadIdx.x;
+    __syncthreads();
+    // ---- join the CTAs of the cluster: each sends the others their shares, and writes its own of the outputs ----
+    cluster_wait();  // all have started: their barriers are there
+    const uint32_t a_sum = smem_u32(in_sum), a_ml = smem_u32(in_ml), a_bar = smem_u32(&in_bar);
+    for (int i = threadIdx.x * 4; i < ROWS * D; i += kWarps * 32 * 4) {
+        const float* x = reinterpret_cast<const float*>(smem) + i;
+        float4 a = *reinterpret_cast<const float4*>(x);
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+            const float4 y = *reinterpret_cast<const float4*>(x + w * ROWS * D);
+            a.x += y.x;
+            a.y += y.y;
+            a.z += y.z;
+            a.w += y.w;
+        }
+        const int q = i / per;
+        send(map_to_rank(a_sum + (rank * per + i - q * per) * 4, q), a, map_to_rank(a_bar, q));
+    }
+    for (int i = threadIdx.x; i < C * ROWS; i += kWarps * 32) {
+        const int q = i / ROWS, r = i % ROWS;
         float M = -INFINITY, L = 0.f;
         for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w][r]);
         // (a maximum of -inf: nothing seen, the sum is zero, or nothing but NaN, which the maximum passes over and the sum keeps)
         for (int w = 0; w < kWarps; ++w) L += wm[w][r] == -INFINITY ? wl[w][r] : wl[w][r] * ex2_approx(wm[w][r] - M);
-        cml[r] = make_float2(M, L);
+        send(map_to_rank(a_ml + (rank * ROWS + r) * 8, q), make_float2(M, L), map_to_rank(a_bar, q));
     }
-    __syncthreads();
-    float* sum = reinterpret_cast<float*>(smem);  // the CTA's rows, in the place of warp 0's
-    for (int i = threadIdx.x; i < ROWS * D; i += kWarps * 32) {
-        float a = sum[i];
+    __syncwarp();
+    cluster_arrive();
+    ok = mbar_wait_warp(a_bar, 0, abortp);
+    for (int i = threadIdx.x * 4; ok && i < per; i += kWarps * 32 * 4) {
+        const int at_all = rank * per + i, r = at_all / D, c = piece_at<D>(r, (at_all - r * D) >> 2) * 4;  // element at_all of the stored order is column c
+        float M = -INFINITY, L = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) a += sum[w * ROWS * D + i];
-        sum[i] = a;
-    }
-    // ---- join the CTAs of the cluster; each writes its share of the outputs ----
-    if (C > 1) cluster_sync(); else __syncthreads();
-    const int per = ROWS * D / C;  // (C divides it)
-    const uint32_t a_sum = smem_u32(sum), a_ml = smem_u32(cml);
-    for (int i = rank * per + 2 * threadIdx.x; i < (rank + 1) * per; i += 2 * kWarps * 32) {
-        const int r = i / D, c = piece_at<D>(r, (i - r * D) >> 2) * 4 + (i & 3);  // element i of the stored order is column c
-        float2 ml[kMaxC], v[kMaxC];
-#pragma unroll
-        for (int q = 0; q < kMaxC; ++q) {  // all loads on their way before the first is used (ranks beyond C: this one again)
-            const uint32_t from = q < C ? q : rank;
-            ml[q] = ld_cluster(map_to_rank(a_ml + r * 8, from));
-            v[q] = ld_cluster(map_to_rank(a_sum + i * 4, from));
-        }
-        float M = -INFINITY, L = 0.f, v0 = 0.f, v1 = 0.f;
-#pragma unroll
-        for (int q = 0; q < kMaxC; ++q) M = fmaxf(M, ml[q].x);
+        for (int q = 0; q < kMaxC; ++q)
+            if (q < C) M = fmaxf(M, in_ml[q][r].x);
 #pragma unroll
         for (int q = 0; q < kMaxC; ++q) {
-            const float f = ml[q].x == -INFINITY ? 0.f : ex2_approx(ml[q].x - M);
-            const bool own = q < C;  // (left out, not taken times zero: an infinite sum would become NaN)
-            L = own ? fmaf(f, ml[q].y, L) : L;
-            v0 = own ? fmaf(f, v[q].x, v0) : v0;
-            v1 = own ? fmaf(f, v[q].y, v1) : v1;
+            if (q >= C) continue;
+            const float2 ml = in_ml[q][r];
+            const float4 x = *reinterpret_cast<const float4*>(in_sum + q * per + i);
+            const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
+            L = fmaf(f, ml.y, L);
+            v.x = fmaf(f, x.x, v.x);
+            v.y = fmaf(f, x.y, v.y);
+            v.z = fmaf(f, x.z, v.z);
+            v.w = fmaf(f, x.w, v.w);
         }
         const int row = row0 + r;
         if (row < p.n_rows) {
@@ -475,7 +501,7 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             const long long where = ((long long)b * p.g.heads + h) * p.g.N + n;
             if (p.parts > 1) {
                 const long long there = (long long)key_part * p.g.batch * p.g.heads * p.g.N + where;
-                *reinterpret_cast<float2*>(p.part_O + there * D + c) = make_float2(v0, v1);
+                *reinterpret_cast<float4*>(p.part_O + there * D + c) = v;
                 if (c == 0) p.part_ml[there] = make_float2(M, L);
                 continue;
             }
@@ -484,13 +510,15 @@ cache_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             // (A row at none may have a sum: steps that the rows of the sequence see whole are not masked.)
             const bool any = at >= 0 && at < seq.len;
             const float inv = any ? 1.f / L : 0.f;
-            *reinterpret_cast<uint32_t*>(p.O + (long long)b * p.o_batch + (long long)h * p.o_head + (long long)n * p.o_row + c) =
-                any ? pack_16x2<F16>(v0 * inv, v1 * inv) : 0u;
+            *reinterpret_cast<uint2*>(p.O + (long long)b * p.o_batch + (long long)h * p.o_head + (long long)n * p.o_row + c) =
+                any ? make_uint2(pack_16x2<F16>(v.x * inv, v.y * inv), pack_16x2<F16>(v.z * inv, v.w * inv)) : make_uint2(0u, 0u);
             if (c == 0) p.LSE[where] = any ? fmaf(M, 0.6931471805599453f, logf(L)) : -INFINITY;
         }
     }
+    if (!ok) let_copies_land();  // (and what is still on its way here)
     if (threadIdx.x == 0 && abort_flag) atomicExch(p.status, (int)BSA_ERR_DEVICE_TIMEOUT);
-    if (C > 1) cluster_sync();  // nobody leaves while its shared memory is being read
+    __syncwarp();
+    cluster_wait();  // all have sent: nobody leaves while it is sent something
 }
 
 // How a call is spread over the GPU, and where its workspace has what.

@@ -318,7 +318,7 @@ bsa_status_t cuda_status(cudaError_t e, const char* where) {
 // ---- attention: which way a call goes ----
 // Few rows: the kernel that spreads the keys over the GPU (bsa_cache_rows.cu).  Rows by the tile: their keys and values in 16 bits first, then the kernel for the
 // 16-bit cache; or the kernel that reads the codes (bsa_cache_tiles.cu), which takes longer over a tile, but needs no pass in front and cuts keys into
-// parts where the rows leave SMs without work.  By what they would take, in us: few rows, 0.75 (d = 64: 0.5) of an SM for each 16 rows of a key head and 128 keys;
+// parts where the rows leave SMs without work.  By what they would take, in us: few rows, 1.0 (d = 64: 0.7) of an SM for each 16 rows of a key head and 128 keys;
 // in 16 bits, 6 bytes an element at 6.4 TB/s for the pass and, whole rounds of items over the SMs, 0.97 (0.82) for 128 rows of a query head and 128 keys;
 // from the codes, cache_tiles_time.
 // Rows of the workspace's K and V: the first tokens (in whole tiles) and the longest window that the queries see between them, or all.
@@ -350,7 +350,7 @@ Way way_of(const WindowArgs& a) {
                             (double)((items + a.num_sms - 1) / a.num_sms) * (tiles_of(kWinT) + 2) * per;
     const double tiles = cache_tiles_time(a);
     const int64_t blocks = (rows + 15) / 16 * a.g.batch * a.g.heads_kv;
-    const double few = rows > 256 ? 1e30 : blocks * tiles_of(a.g.N) * (a.d == 128 ? 0.75 : 0.5) / a.num_sms + 6.0;
+    const double few = rows > 512 ? 1e30 : blocks * tiles_of(a.g.N) * (a.d == 128 ? 1.0 : 0.7) / a.num_sms + 8.0;
     return few <= tiles && few <= unpacked ? Way::kRows : tiles <= unpacked ? Way::kTiles : Way::kUnpacked;
 }
 int64_t workspace_of(const WindowArgs& a, Way way) {

@@ -991,7 +991,7 @@ struct Plan {
     int64_t rows;
     int64_t q8, c2, refs, part_ml, part_O, bytes;  // offsets
 };
-// Parts of an item: as many as make the call shortest.  In tile times (1.3 us; d = 64: 1.2) every pair of CTAs takes its share of whole items, and an
+// Parts of an item: as many as make the call shortest.  In tile times (1.3 us; d = 64: 1.0) every pair of CTAs takes its share of whole items, and an
 // item costs about four tiles for its start and end, a cut call eight for the join.  (The host knows no lengths: the tensors' sizes stand for them.)
 Plan plan_of(const WindowArgs& a) {
     Plan w = {};
@@ -1003,7 +1003,7 @@ Plan plan_of(const WindowArgs& a) {
     w.parts = 1;
     for (int s = 2; s <= kMaxParts && s * 4 <= tiles && items * s < (1 << 24); ++s)  // (where there are more items parts bring nothing)
         if (cost(s) < cost(w.parts)) w.parts = s;
-    w.us = (double)cost(w.parts) * (a.d == 128 ? 1.3 : 1.2);
+    w.us = (double)cost(w.parts) * (a.d == 128 ? 1.3 : 1.0);
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         const int64_t here = at;

@@ -141,6 +141,8 @@ __device__ __forceinline__ uint32_t in_first_cta(uint32_t smem) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem));
     return r;
 }
+// (What the first CTA's products then read lies in tensor memory, behind tcgen05.fence, or in the arriving CTA's shared memory, behind fence.proxy.async; a
+// release at cluster scope besides took a quarter of the kernel's time.)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -844,8 +846,8 @@ __device__ __forceinline__ float2 e5m2x2_to_f32x2(uint32_t two) {
     return f16x2_to_f32x2(r);
 }
 
-// A CTA takes 32 (d = 64: 64) rows of one head.  The largest scale is looked up by each anew: 16 bytes to a thread and step of as many blocks as the
-// window has, a few KB out of L2.
+// A CTA takes 32 (d = 64: 64) rows of one head.  The largest scale is looked up by each anew: a byte for each block of the
+// window, a few KB out of L2.
 template <int D, bool F16>
 __global__ void __launch_bounds__(kPrepThreads) cache_prepare_kernel(const __grid_constant__ PrepareParams p) {
     constexpr int LANES = D / 16, ROWS = kPrepThreads / LANES;

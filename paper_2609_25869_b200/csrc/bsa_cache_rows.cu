@@ -21,7 +21,7 @@
 //   * Scales stay out of the products: scores are multiplied by their block's power of two; V's goes into the exponent of its keys' weights,
 //     relative to the largest so far of the warp's keys, which the accumulator is in units of.  P and its sum stay fp32 until P is rounded to half.
 // Eight sequences of 65536 keys, 8 key heads under 32, d = 128, one token: 178 us for 1.07 GB, 6.0 TB/s (94 % of what a copy has); six of 1111 to 115200
-// keys 129 us, 5.3 TB/s (token-major; the 16-bit cache 239); four with a window of 1024 keys 9 us, latencies.
+// keys 129 us, 5.3 TB/s (token-major; the 16-bit cache 239); four with a window of 1024 keys 7 us, latencies.
 #include <cuda_fp16.h>
 #include <float.h>
 #include <math.h>

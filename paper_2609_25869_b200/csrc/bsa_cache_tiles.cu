@@ -18,12 +18,13 @@
 //   warp 8 : copies, K's scales   warp 9 : issuer (second CTA: tells the first what has landed)   warps 10, 11 : V converters
 //   warps 12-15 : references: each row's running maximum, the tiles' edges, the accumulator's rescaling, and the epilogue
 // Barriers that the issuer waits for lie in the first CTA and count the warps of both; its commits arrive in both.
-// 300 rows x 65536 keys, 8 heads, d = 128: 145 us, of which the pass in front has 5 and the join 5; 466 through 16 bits.  With the GPU full 870 to 1020 TFLOP/s
-// (4736 x 25088, 12 heads; the more scales differ the less, the power cap among the reasons), 16 bits 1120 to 1270: this kernel is for calls that do not fill it.
+// 300 rows x 65536 keys, 8 heads, d = 128: 145 us, of which the pass in front has 5 and the join 5; 466 through 16 bits.  With the GPU full 870 to 1040 TFLOP/s
+// where blocks' scales differ, 1010 to 1260 where they do not (4736 x 25088, 12 heads; the power cap among the reasons), 16 bits 1120 to 1270: this kernel is for calls that do not fill it.
 // Tensor pipe and special-function unit are 51 % busy, a quarter-SM issues 38 % of its time: what bounds a tile is its chain from Q K^T over the references and
 // weights to P V, across two CTAs.  Tried: an issuer that polls for whichever product is ready (10 % slower: three tests of barriers take longer than
 // the order costs), a warp for each product with the copies beside one of them (25 % slower), the issuer's loop unrolled by four with constant
-// descriptors (spills; 40 % slower), K widened to half as V is (its converter became the bottleneck: 530 TFLOP/s).
+// descriptors (spills; 40 % slower), K widened to half as V is (its converter became the bottleneck: 530 TFLOP/s), V's scales in the exponents of the weights
+// instead of in V (no faster at d = 128, 5 to 10 % slower at 64 where scales differ).
 // Tensor-memory columns: S0 0, S1 128, O 256, P0 384, P1 448.  Registers (setmaxnreg): 256 * 176 + 128 * 96 + 128 * 64 = 65536, the
 // launch's 512 * 128.
 #include <cuda_fp16.h>

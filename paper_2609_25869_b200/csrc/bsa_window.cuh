@@ -25,10 +25,12 @@ struct WindowGeom {
 struct Sequence {
     int start, len;  // position of row 0, number of keys
 };
+// (Ordinary loads, not those of the read-only path: a kernel in front may write the two words while this one already runs, up to its
+// grid_dependency_wait, and only memory that nobody writes during a kernel's whole life may be read that way.)
 __device__ __forceinline__ Sequence load_sequence(const WindowGeom& g, int b) {
     Sequence s;
-    s.len = g.kv_len ? min(max(__ldg(g.kv_len + b), 0), g.N_kv) : g.N_kv;
-    s.start = g.q_start ? min(max(__ldg(g.q_start + b), -kWinNoLimit), kWinNoLimit) : s.len - g.N;
+    s.len = g.kv_len ? min(max(g.kv_len[b], 0), g.N_kv) : g.N_kv;
+    s.start = g.q_start ? min(max(g.q_start[b], -kWinNoLimit), kWinNoLimit) : s.len - g.N;
     return s;
 }
 

@@ -1,0 +1,59 @@
+"""The 8-bit cache's attention way by way: what one call leaves for the next, and how far each way's roundings and NaN reach."""
+import pytest
+import torch
+
+from paper_2609_25869_b200 import bsa
+from tests.test_gpu_cache import filled, queries
+from tests.test_gpu_window import ints
+
+pytestmark = pytest.mark.gpu
+
+
+class Call:
+    """bsa_cache_forward through the C ABI, with the positions, the outputs and the workspace in the caller's hands."""
+
+    def __init__(self, q, cache, left, right=0, sinks=0):
+        self.q, self.cache, self.window = q, cache, (left, right, sinks)
+        some = ints([0] * cache.batch)
+        self.need = bsa.lib().bsa_cache_workspace_bytes(self.desc(some, some), cache._packed)
+
+    def desc(self, start, length):
+        b, h, n, d = self.q.shape if self.cache.layout == "hnd" else (self.q.shape[i] for i in (0, 2, 1, 3))
+        return bsa._WINDOW.pack(b, h, self.cache.heads, d, n, self.cache.N, *self.window, bsa._tensor_of(self.q, "Q")[0], 0.0,
+                                start.data_ptr(), length.data_ptr())
+
+    def __call__(self, start, length, O, LSE, ws):
+        nhd, dev = self.cache.layout == "nhd", self.q.get_device()
+        vq, vo = (bsa._view(x, nhd, self.q.dtype, dev, "Q")[4] for x in (self.q, O))
+        assert bsa.lib().bsa_cache_forward(self.desc(start, length), self.cache._packed, vq, vo, LSE.data_ptr(), ws.data_ptr(), ws.numel(),
+                                           torch.cuda.current_stream().cuda_stream or None) == 0
+
+
+@pytest.mark.parametrize("n,nk,left", [(300, 5000, 200), (300, 9000, -1), (1, 40000, -1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_workspace_used_again_holds_nothing_of_the_call_before(n, nk, left, d):
+    """Calls one right behind the other with one workspace, each at other positions (which the 16-bit way keeps there, written by a kernel that is
+    still running when the attention kernel starts): the bits of calls alone."""
+    cache, _ = filled(31, 2, 2, nk, d, "bf16", "hnd", 64)
+    q = queries(31, 2, 4, n, d, "bf16", "hnd")
+    call = Call(q, cache, left, 3, 5)
+    places = [([nk - n, 1000], [nk, 1000 + n]), ([0, 2222], [n, 3000]), ([700, nk - n - 1], [701 + n, nk]), ([1500, -3], [4000, 90])]
+    places = [(ints(a), ints(b)) for a, b in places]
+
+    def outputs():
+        return torch.empty_like(q), torch.empty(2, 4, n, device="cuda")
+    alone = []
+    for start, length in places:
+        O, L = outputs()
+        call(start, length, O, L, torch.full((max(call.need, 256),), 255, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        alone.append((O, L))
+    ws = torch.full((max(call.need, 256),), 255, dtype=torch.uint8, device="cuda")
+    got = [(i % 4, *outputs()) for i in range(40)]
+    torch.cuda.synchronize()
+    for i, O, L in got:
+        call(*places[i], O, L, ws)
+    torch.cuda.synchronize()
+    for i, O, L in got:
+        assert torch.equal(O, alone[i][0]) and torch.equal(L, alone[i][1])
+    assert bsa.window_status() == 0

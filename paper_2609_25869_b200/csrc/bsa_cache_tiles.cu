@@ -478,8 +478,9 @@ cache_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
             const float l = lfin[(g & 1) ^ 1][tw] + (m_other == m ? l_other : l_other * ex2_approx(m_other - m));
             mbar_arrive(smem_u32(&bars.e_taken));
             // (a row at a position sees its own key at least: its sum is above zero, or NaN, which belongs to its outputs)
-            const float unit = scale_of(p.refs[2 * (w.b * p.g.heads_kv + w.hk) + 1]) ;
-            const float inv = seen ? 1.f / l * unit : 0.f;
+            // (The sum's reciprocal first, then V's largest scale: the two in one may lie below the smallest normal number where the outputs do not.)
+            const float unit = scale_of(p.refs[2 * (w.b * p.g.heads_kv + w.hk) + 1]);
+            const float inv = seen ? 1.f / l : 0.f;
             if (row_ok) {
                 if (p.parts > 1) *ml = make_float2(m, l);
                 else p.LSE[at] = seen ? fmaf(m - kShift, 0.6931471805599453f, logf(l)) : -INFINITY;
@@ -508,7 +509,7 @@ cache_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                         uint32_t v[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            v[e] = seen ? pack_16x2<F16>(__uint_as_float(o[q * 16 + 2 * e]) * inv, __uint_as_float(o[q * 16 + 2 * e + 1]) * inv) : 0u;
+                            v[e] = seen ? pack_16x2<F16>(__uint_as_float(o[q * 16 + 2 * e]) * inv * unit, __uint_as_float(o[q * 16 + 2 * e + 1]) * inv * unit) : 0u;
                         st_global_v8_or_2v4(orow + c * 32 + q * 16, v, p.o_wide);
                     }
                 }
@@ -978,9 +979,9 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const __grid_c
         o.z = fmaf(f, x.z, o.z);
         o.w = fmaf(f, x.w, o.w);
     }
-    const float inv = 1.f / L * (p.refs ? scale_of(p.refs[2 * (b * p.g.heads_kv + h / p.g.group) + 1]) : 1.f);
+    const float inv = 1.f / L, unit = p.refs ? scale_of(p.refs[2 * (b * p.g.heads_kv + h / p.g.group) + 1]) : 1.f;  // (one after the other, see above)
     uint16_t* out = p.O + (long long)b * p.o_batch + (long long)h * p.o_head + (long long)n * p.o_row + c;
-    *reinterpret_cast<uint2*>(out) = seen ? make_uint2(pack_16x2<F16>(o.x * inv, o.y * inv), pack_16x2<F16>(o.z * inv, o.w * inv)) : make_uint2(0u, 0u);
+    *reinterpret_cast<uint2*>(out) = seen ? make_uint2(pack_16x2<F16>(o.x * inv * unit, o.y * inv * unit), pack_16x2<F16>(o.z * inv * unit, o.w * inv * unit)) : make_uint2(0u, 0u);
     if (c == 0) p.LSE[at] = seen ? fmaf(M - p.shift, 0.6931471805599453f, logf(L)) : -INFINITY;
 }
 

@@ -3,7 +3,9 @@ import pytest
 import torch
 
 from paper_2609_25869_b200 import bsa
-from tests.test_gpu_cache import filled, queries
+from tests import cache_reference as C
+from tests import window_reference as R
+from tests.test_gpu_cache import filled, generator, parts, queries
 from tests.test_gpu_window import ints
 
 pytestmark = pytest.mark.gpu
@@ -56,4 +58,30 @@ def test_a_workspace_used_again_holds_nothing_of_the_call_before(n, nk, left, d)
     torch.cuda.synchronize()
     for i, O, L in got:
         assert torch.equal(O, alone[i][0]) and torch.equal(L, alone[i][1])
+    assert bsa.window_status() == 0
+
+
+def tiny(cache, g, size):
+    """Writes normal keys, and values around `size`, all of one sign, so that nothing cancels; both in 64 bits."""
+    shape = cache.K.shape
+    k = torch.empty(shape, device="cuda").normal_(0, 1, generator=g).bfloat16()
+    v = torch.empty(shape, device="cuda").uniform_(0.5, 1.0, generator=g).double().mul_(size).bfloat16()
+    bsa.cache_write(cache, k, v)
+    return [C.values(c, s, cache.block).cuda() for c, s in parts(cache)]
+
+
+# one row; few rows in parts; through 16 bits; from the codes, uncut and in parts
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("b,h,hk,n,nk", [(1, 4, 2, 1, 700), (1, 4, 2, 1, 40000), (2, 2, 1, 300, 700), (5, 14, 14, 64, 6000), (1, 4, 2, 300, 6000)])
+def test_values_near_the_types_smallest(b, h, hk, n, nk, d):
+    """Scales of V down to the smallest there is: the reciprocal of a row's sum times such a scale is no normal number, the outputs are."""
+    cache = bsa.cache_create(b, hk, nk, d)
+    values = tiny(cache, generator(32), 2.0 ** -117)
+    assert int(cache.V_scale.view(torch.uint8).max()) <= 2
+    q = queries(32, b, h, n, d, "bf16", "hnd")
+    O, L = bsa.cache_forward(q, cache, left=-1, right=-1, q_start=ints([0] * b))
+    wO, wL, tO, tL = C.forward(q, *values, left=-1, right=-1, q_start=ints([0] * b))
+    up = 2.0 ** 117  # (the comparison's own least number is far above these)
+    R.assert_within(O.double() * up, wO * up, tO * up, "O")
+    R.assert_within(L, wL, tL, "LSE")
     assert bsa.window_status() == 0

@@ -123,6 +123,7 @@ __global__ void __launch_bounds__(kWriteThreads<D, B>, 1024 / kWriteThreads<D, B
 #pragma unroll
         for (int w = 0; w < TB / 32; ++w) most = max(most, most_of[threadIdx.x / TB * (TB / 32) + w]);
     }
+    if (TB == 32) __syncwarp();  // (all lanes have read the old scale; longer blocks have the barrier above)
     if (!mine) return;
     const int need = scale_code(most);
     const int code = keeps ? max(old, need) : need;

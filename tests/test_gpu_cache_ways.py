@@ -5,7 +5,7 @@ import torch
 from paper_2609_25869_b200 import bsa
 from tests import cache_reference as C
 from tests import window_reference as R
-from tests.test_gpu_cache import filled, generator, parts, queries
+from tests.test_gpu_cache import check_write, filled, generator, parts, queries
 from tests.test_gpu_window import ints
 
 pytestmark = pytest.mark.gpu
@@ -85,3 +85,13 @@ def test_values_near_the_types_smallest(b, h, hk, n, nk, d):
     R.assert_within(O.double() * up, wO * up, tO * up, "O")
     R.assert_within(L, wL, tL, "LSE")
     assert bsa.window_status() == 0
+
+
+@pytest.mark.parametrize("block,d", [(16, 64), (32, 64), (16, 128)])  # of 32 threads each
+def test_a_scale_that_grows_under_one_warp(block, d):
+    """Tokens one by one, each twice as loud as the one before: every lane of a block's warp has to see the scale as it was."""
+    g = generator(33)
+    cache = bsa.cache_create(4, 9, 3 * block, d, block=block)
+    for i in range(block + 5):
+        k, v = (torch.empty(4, 9, 1, d, device="cuda").normal_(0, 1, generator=g).mul_(2.0 ** (i % 23 - 11)).bfloat16() for _ in range(2))
+        check_write(cache, k, v, [i, i + block - 5, max(0, i - 7), 0])

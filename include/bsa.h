@@ -442,7 +442,10 @@ BSA_API bsa_status_t bsa_window_status(int* status_out);
  *          are multiples of 16 elements.
  * K_scale, V_scale : a byte s for each block of `block` tokens of a head, [batch][heads][ceil(N / block)], scale_batch and scale_head elements
  *          between batch entries and heads (of both; the blocks of a head are contiguous): the element's value is code * 2^(s - 127); 255: NaN.
- * The memory is the caller's; nothing has to be initialised.  Calls that write one cache are stream-ordered by the caller with those that use it.
+ * The memory is the caller's.  Tokens in front of a call's first position count as written, so the first write of a sequence begins at the beginning of
+ * a block, or the scales (K's and V's, of every head) of the block that it begins in are zero bytes: whatever else stands there, of a sequence that used the
+ * memory before for instance, would be taken for those tokens' scale, 255 for NaN.  Nothing else has to be initialised.
+ * Calls that write one cache are stream-ordered by the caller with those that use it.
  */
 typedef struct bsa_cache {
     bsa_view_t K, V;

@@ -636,7 +636,9 @@ class Cache:
     ``K``, ``V``: float8_e4m3fn CUDA tensors ``[heads_kv, N, d]`` or ``[batch, heads_kv, N, d]`` (``layout="nhd"``: heads behind N),
     strides in multiples of 16.  ``K_scale``, ``V_scale``: float8_e8m0fnu ``[heads_kv, ceil(N / block)]`` or with a batch in front, the blocks
     contiguous, both with the same strides; an element's value is its code times its block's scale.  ``block``: 16, 32, 64 or 128 tokens.
-    The tensors stay the caller's: views of longer ones, or of some sequences of more, make handles of their own."""
+    The tensors stay the caller's: views of longer ones, or of some sequences of more, make handles of their own.  Where a new sequence's first
+    write begins inside a block, that block's scales have to be zero bytes (as ``cache_create`` leaves them): ``K_scale.view(torch.uint8)[i].zero_()``,
+    V_scale alike, for memory that was not zero or that another sequence used."""
 
     __slots__ = ("K", "V", "K_scale", "V_scale", "block", "layout", "batch", "heads", "N", "d", "device", "_packed")
 
@@ -697,7 +699,8 @@ def _cache_views(cache: Cache, K, V):
 def cache_write(cache: Cache, K, V, *, start=None, count=None, stream=None) -> None:
     """``bsa_cache_write``: rows of K and V (bf16 or fp16, the cache's layout, N of them) become the cache's tokens ``start .. start +
     count - 1``.  ``start``, ``count``: int32 CUDA tensors ``[batch]`` (default: 0, and all rows); tokens outside of the cache are left out.
-    A write ends its sequences: tokens behind it are no longer valid where they share a block with it."""
+    A write ends its sequences: tokens behind it are no longer valid where they share a block with it.  Tokens in front of it in its first block count as
+    written before: they keep their values, and their scale where it is the larger one."""
     n, dt, vk, vv = _cache_views(cache, K, V)
     rows = _cache_rows(cache, n, dt, start, count)
     _call(cache.device, stream, "bsa_cache_write", lib().bsa_cache_write, cache._packed, rows, vk, vv)

@@ -5,7 +5,7 @@ import torch
 from paper_2609_25869_b200 import bsa
 from tests import cache_reference as C
 from tests import window_reference as R
-from tests.test_gpu_cache import check_write, filled, generator, parts, queries
+from tests.test_gpu_cache import check_write, filled, garbage, generator, parts, queries
 from tests.test_gpu_window import ints
 
 pytestmark = pytest.mark.gpu
@@ -95,3 +95,34 @@ def test_a_scale_that_grows_under_one_warp(block, d):
     for i in range(block + 5):
         k, v = (torch.empty(4, 9, 1, d, device="cuda").normal_(0, 1, generator=g).mul_(2.0 ** (i % 23 - 11)).bfloat16() for _ in range(2))
         check_write(cache, k, v, [i, i + block - 5, max(0, i - 7), 0])
+
+
+@pytest.mark.parametrize("block,start", [(16, 5), (64, 100), (128, 64)])
+@pytest.mark.parametrize("foreign", [0, 90, 254, 255])
+def test_a_first_write_inside_a_block(foreign, block, start):
+    """Memory that held another sequence (codes of any byte, NaN among them): with the block's scales zeroed the new tokens get the smallest scale that takes them,
+    and rows that see them alone are finite; a scale left there counts as that of tokens in front."""
+    b, h, n, d = 2, 2, 150, 64
+    g = generator(34)
+    cache = garbage(34, b, h, 512, d, block, scales=(foreign, foreign + 1))
+    for i in range(b):  # both sequences' slots, as a user clears them
+        cache.K_scale.view(torch.uint8)[i].zero_()
+        cache.V_scale.view(torch.uint8)[i].zero_()
+    k, v = (torch.empty(b, h, n, d, device="cuda").normal_(0, 1, generator=g).bfloat16() for _ in range(2))
+    check_write(cache, k, v, [start, start], None)
+    alone = bsa.cache_create(b, h, 512, d, block=block)
+    bsa.cache_write(alone, k, v, start=ints([start, start]))
+    first, last = start // block, (start + n - 1) // block
+    for mine, want in zip(parts(cache), parts(alone)):
+        assert torch.equal(mine[1][..., first:last + 1], want[1][..., first:last + 1])
+        assert torch.equal(mine[0][:, :, start:start + n] & 127, want[0][:, :, start:start + n] & 127)
+    for rows in (1, 40):
+        q = queries(34, b, 4, rows, d, "bf16", "hnd")
+        kw = dict(left=30, q_start=ints([start + n - rows] * b), kv_len=ints([start + n] * b))
+        O, L = bsa.cache_forward(q, cache, **kw)
+        O2, L2 = bsa.cache_forward(q, alone, **kw)
+        assert torch.isfinite(O).all() and torch.equal(O, O2) and torch.equal(L, L2)
+    if foreign:
+        cache.K_scale.view(torch.uint8)[0, :, first] = foreign
+        check_write(cache, k, v, [start, start], None)
+        assert int(cache.K_scale.view(torch.uint8)[0, 0, first]) == max(foreign, int(parts(alone)[0][1][0, 0, first]))

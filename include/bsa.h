@@ -580,6 +580,9 @@ BSA_API bsa_status_t bsa_debug_set_wait_limit(long long cycles);
  * forward).  UNSUPPORTED for a plan without Split-K partitions. */
 BSA_API bsa_status_t bsa_debug_merge_only(const bsa_plan_t* plan, void* O_dev, float* LSE_dev, void* stream);
 BSA_API bsa_status_t bsa_debug_withhold_arrival(int on);
+/* Which way bsa_cache_forward takes a call of these sizes on the current device: *way_out 0: few rows, 1: rows by the tile from the codes, 2: through 16 bits;
+ * *parts_out: the parts that the keys of an item are cut into.  Errors: as that call's for its description and cache. */
+BSA_API bsa_status_t bsa_debug_cache_way(const bsa_window_desc_t* desc, const bsa_cache_t* cache, int* way_out, int* parts_out);
 
 BSA_API const char* bsa_status_string(bsa_status_t s);
 BSA_API const char* bsa_last_cuda_error(void);

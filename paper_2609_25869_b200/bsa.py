@@ -120,6 +120,7 @@ def lib() -> ctypes.CDLL:
     L.bsa_debug_set_wait_limit.argtypes = [ctypes.c_longlong]
     L.bsa_debug_withhold_arrival.argtypes = [i32]
     L.bsa_debug_merge_only.argtypes = [vp, vp, vp, vp]
+    L.bsa_debug_cache_way.argtypes = [ctypes.c_char_p] * 2 + [ctypes.POINTER(i32)] * 2
     L.bsa_base_plan.argtypes = [i32, i32, i32]
     L.bsa_catalog_hash.restype = ctypes.c_uint64
     L.bsa_lut_load.argtypes = [ctypes.c_char_p]
@@ -820,6 +821,16 @@ def debug_set_wait_limit(cycles: int):
 def debug_withhold_arrival(on: bool):
     """``bsa_debug_withhold_arrival`` (test hook): make the next forwards' first V tile never arrive."""
     _check(lib().bsa_debug_withhold_arrival(1 if on else 0), "bsa_debug_withhold_arrival")
+
+
+def debug_cache_way(Q, cache: Cache, *, left: int, right: int = 0, sinks: int = 0, q_start=None, kv_len=None):
+    """``bsa_debug_cache_way`` (test hook): the way that ``cache_forward`` takes such a call, "rows", "tiles" or "unpacked", and the parts of its items."""
+    b, h, n, d, _ = _view(Q, LAYOUTS[cache.layout] == 1, Q.dtype, cache.device, "Q")
+    desc = _WINDOW.pack(b, h, cache.heads, d, n, cache.N, left, right, sinks, _tensor_of(Q, "Q")[0], 0.0, 0 if q_start is None else q_start.data_ptr(),
+                        0 if kv_len is None else kv_len.data_ptr())
+    way, parts = ctypes.c_int(0), ctypes.c_int(0)
+    _check(lib().bsa_debug_cache_way(desc, cache._packed, ctypes.byref(way), ctypes.byref(parts)), "bsa_debug_cache_way")
+    return ("rows", "tiles", "unpacked")[way.value], parts.value
 
 
 def lut_load(path: str):

@@ -485,3 +485,16 @@ extern "C" bsa_status_t bsa_cache_forward(const bsa_window_desc_t* t, const bsa_
     return cuda_status(way == Way::kRows ? launch_cache_rows(a, g, *Q, *O, LSE, workspace, stream) : launch_cache_tiles(a, g, *Q, *O, LSE, workspace, stream),
                        "bsa_cache_forward");
 }
+
+extern "C" bsa_status_t bsa_debug_cache_way(const bsa_window_desc_t* t, const bsa_cache_t* c, int* way_out, int* parts_out) {
+    WindowArgs a;
+    CacheGeom g;
+    if (!way_out || !parts_out) return BSA_ERR_INVALID_ARG;
+    bsa_status_t st = forward_args(t, c, &a, &g);
+    if (st == BSA_OK) st = window_device(&a);
+    if (st != BSA_OK) return st;
+    const Way way = way_of(a);
+    *way_out = way == Way::kRows ? 0 : way == Way::kTiles ? 1 : 2;
+    *parts_out = way == Way::kRows ? cache_rows_parts(a) : way == Way::kTiles ? cache_tiles_parts(a) : 1;
+    return BSA_OK;
+}

@@ -49,11 +49,13 @@ bsa_status_t cache_geom(const bsa_cache_t* c, CacheGeom* g);
 
 // Rows by the tile from the codes (bsa_cache_tiles.cu), the workspace that they need, and about how many us they take.
 int64_t cache_tiles_bytes(const WindowArgs& a);
+int cache_tiles_parts(const WindowArgs& a);
 double cache_tiles_time(const WindowArgs& a);
 cudaError_t launch_cache_tiles(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace,
                                cudaStream_t stream);
 // Few rows (bsa_cache_rows.cu), and the workspace that they need.
 int64_t cache_rows_bytes(const WindowArgs& a);
+int cache_rows_parts(const WindowArgs& a);
 cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace,
                               cudaStream_t stream);
 // Behind either, where keys were cut into parts: O and LSE from the parts' [parts][batch][heads][N][d] sums, their maxima (log2 domain) and weights' sums

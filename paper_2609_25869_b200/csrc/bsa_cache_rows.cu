@@ -596,6 +596,7 @@ cudaError_t launch(const WindowArgs& a, const CacheGeom& c, const Params& p, con
 cudaError_t set_cache_rows_wait_limit(long long cycles) { return cudaMemcpyToSymbol(ptx::g_wait_limit_cycles, &cycles, sizeof cycles); }
 
 int64_t cache_rows_bytes(const WindowArgs& a) { return plan_of(a).bytes; }
+int cache_rows_parts(const WindowArgs& a) { return plan_of(a).parts; }
 
 cudaError_t launch_cache_rows(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace, cudaStream_t stream) {
     const Plan w = plan_of(a);

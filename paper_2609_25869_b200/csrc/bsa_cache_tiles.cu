@@ -1138,6 +1138,7 @@ cudaError_t launch_cache_join(const WindowArgs& a, int parts, const float* part_
 }
 
 int64_t cache_tiles_bytes(const WindowArgs& a) { return plan_of(a).bytes; }
+int cache_tiles_parts(const WindowArgs& a) { return plan_of(a).parts; }
 double cache_tiles_time(const WindowArgs& a) { return plan_of(a).us; }
 
 cudaError_t launch_cache_tiles(const WindowArgs& a, const CacheGeom& c, const bsa_view_t& Q, const bsa_view_t& O, float* LSE, void* workspace, cudaStream_t stream) {

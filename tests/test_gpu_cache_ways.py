@@ -5,7 +5,7 @@ import torch
 from paper_2609_25869_b200 import bsa
 from tests import cache_reference as C
 from tests import window_reference as R
-from tests.test_gpu_cache import check_write, filled, garbage, generator, parts, queries
+from tests.test_gpu_cache import check_forward, check_write, filled, garbage, generator, parts, queries
 from tests.test_gpu_window import ints
 
 pytestmark = pytest.mark.gpu
@@ -126,3 +126,81 @@ def test_a_first_write_inside_a_block(foreign, block, start):
         cache.K_scale.view(torch.uint8)[0, :, first] = foreign
         check_write(cache, k, v, [start, start], None)
         assert int(cache.K_scale.view(torch.uint8)[0, 0, first]) == max(foreign, int(parts(alone)[0][1][0, 0, first]))
+
+
+# ------------------------------------------------------------------ which way, and each way's own
+def test_every_way_is_taken_by_the_sizes_that_the_tests_use():
+    """The rule's constants may change; then the sizes of the tests in this file and its neighbour have to follow."""
+    for d in (64, 128):
+        for n, nk, left, want in [(1, 600, -1, "rows"), (1, 40000, -1, "rows"), (300, 700, -1, "unpacked"), (300, 5000, 200, "unpacked"), (300, 6000, -1, "tiles")]:
+            cache = bsa.cache_create(2, 2, nk, d)
+            q = torch.empty(2, 4, n, d, device="cuda", dtype=torch.bfloat16)
+            way, parts_ = bsa.debug_cache_way(q, cache, left=left)
+            assert way == want and (parts_ > 1) == (nk >= 6000 and n > 1 or nk == 40000)
+
+
+#       b  h   hk  n    nk    left  right sinks starts                  lengths                   at least so many items for each of the GPU's pairs of CTAs
+MANY = [
+    (5, 40, 40, 200, 2000, -1, 0, 0, None, None, 3),
+    (5, 40, 40, 200, 2000, -1, 7, 0, [1800, -200, 50, 1900, -70], [2000, 0, 250, 1999, 130], 3),      # no key; rows behind, rows in front of the sequence
+    (5, 40, 40, 200, 2000, 1200, 5, 130, [1800, 0, 1000, 1900, 300], [2000, 200, 1100, 2000, 0], 3),  # a window, first tokens, rows behind, no key
+    (4, 37, 37, 200, 3000, -1, -1, 0, None, None, 2),
+    (3, 9, 3, 100, 9000, -1, 0, 0, None, None, 2),                                                    # in parts
+    (3, 9, 3, 100, 9000, 8500, 0, 40, [8900, -100, 600], [9000, 0, 700], 2),                          # parts without a tile
+    (3, 5, 5, 520, 12000, -1, 0, 0, [11480, 4000, 11000], [12000, 4520, 11520], 2),                   # three tiles of rows
+    (5, 14, 14, 64, 6000, -1, 0, 0, [5936, 1, 0, 600, 5000], [6000, 65, 0, 664, 5064], 1),            # uncut, an item a pair
+    (4, 12, 12, 64, 300, 500, 0, 0, None, None, 1),
+]
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (64, "fp16"), (128, "bf16"), (128, "fp16")])
+@pytest.mark.parametrize("block,layout", [(16, "hnd"), (64, "nhd")])
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "x".join(str(x) for x in c[:8]))
+def test_rows_by_the_tile_item_after_item(case, block, layout, d, dtype):
+    """The kernel that reads the codes with several items for each pair of CTAs, whole ones and parts: what one item hands to the next."""
+    b, h, hk, n, nk, left, right, sinks, starts, lengths, rounds = case
+    cache, values = filled(sum(case[1:5]) + d, b, hk, nk, d, dtype, layout, block, 0.8)
+    q = queries(n + nk, b, h, n, d, dtype, layout)
+    kw = dict(left=left, right=right, sinks=sinks, q_start=ints(starts), kv_len=ints(lengths))
+    way, cut = bsa.debug_cache_way(q, cache, **kw)
+    assert way == "tiles"
+    pairs = torch.cuda.get_device_properties(0).multi_processor_count // 2
+    assert -(-n // 256) * b * h * cut > (rounds - 1) * pairs
+    check_forward(q, cache, values, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("way,b,h,hk,n,nk", [("rows", 1, 4, 2, 3, 500), ("rows", 1, 4, 2, 3, 40000), ("unpacked", 2, 2, 1, 300, 700), ("tiles", 1, 4, 2, 300, 6000),
+                                             ("tiles", 5, 14, 14, 64, 6000)])
+def test_queries_at_the_ends_of_their_type(way, b, h, hk, n, nk, dtype):
+    """Rows up to the type's largest numbers and down to its smallest, with a scale that takes their scores back; a row of zeros sees its keys evenly."""
+    cache, values = filled(35, b, hk, nk, 128, dtype, "hnd", 64)
+    kw = dict(left=-1, right=-1, q_start=ints([0] * b))
+    ends = ((2.0 ** 120, 2.0 ** -124), (2.0 ** -115, 2.0 ** 111)) if dtype == "bf16" else ((2.0 ** 12, 2.0 ** -16), (2.0 ** -12, 2.0 ** 8))
+    q = queries(35, b, h, n, 128, dtype, "hnd")
+    assert bsa.debug_cache_way(q, cache, **kw)[0] == way
+    for f, scale in (*ends, (0.0, 0.0)):
+        check_forward((q.float() * f).to(q.dtype), cache, values, scale=scale, **kw)
+
+
+@pytest.mark.parametrize("way,b,h,hk,n,nk", [("rows", 1, 4, 2, 3, 500), ("unpacked", 2, 2, 1, 300, 700), ("tiles", 1, 4, 2, 300, 6000)])
+@pytest.mark.parametrize("scale,loud", [(2.0 ** 120, 2.0 ** 20), (2.0 ** -80, 2.0 ** -20)])
+def test_factors_beyond_32_bits(scale, loud, way, b, h, hk, n, nk):
+    """Scores of zero, or so small that they are none, under a factor that has no number in 32 bits: every key that is seen has the same weight, none besides."""
+    g = generator(36)
+    cache = bsa.cache_create(b, hk, nk, 64)
+    k, v = (torch.empty(b, hk, nk, 64, device="cuda").normal_(0, 1, generator=g).mul_(f).bfloat16() for f in (loud, 1.0))
+    q = torch.zeros(b, h, n, 64, dtype=torch.bfloat16, device="cuda")
+    k[..., 0] = 0
+    q[..., 0] = loud
+    bsa.cache_write(cache, k, v)
+    V = C.values(*parts(cache)[1], 64).cuda().repeat_interleave(h // hk, 1)
+    start = nk - n - 7
+    kw = dict(left=-1, q_start=ints([start] * b))
+    assert bsa.debug_cache_way(q, cache, **kw)[0] == way
+    O, L = bsa.cache_forward(q, cache, scale=scale, **kw)
+    count = torch.arange(start + 1, start + n + 1, device="cuda").double()
+    want = V.cumsum(2)[:, :, start:start + n] / count[:, None]
+    assert (L.double() - count.log()).abs().max() <= 2.0 ** -17
+    # P is one for every key: the mean of V in 32 bits (2^-19 of its absolute values), rounded once
+    assert ((O.double() - want).abs() <= 2.0 ** -8 * want.abs() * 1.01 + 2.0 ** -18 * V.abs().amax()).all()

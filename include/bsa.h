@@ -481,7 +481,10 @@ BSA_API bsa_status_t bsa_cache_write(const bsa_cache_t* cache, const bsa_cache_r
 BSA_API bsa_status_t bsa_cache_read(const bsa_cache_t* cache, const bsa_cache_rows_t* rows, const bsa_view_t* K, const bsa_view_t* V, void* stream);
 
 /* bsa_cache_forward -- bsa_window_forward over a cache: desc, Q, O and LSE as there (desc's batch, heads_kv, d and N_kv are the cache's), the same
- * keys seen, the same treatment of what nobody sees, of padding and of NaN.  A block's scale of 255 reaches the rows of a tile that see any of it.
+ * keys seen, the same treatment of padding, and what a row sees reaches its outputs: a code of NaN, and every key of a block whose scale is 255.  Keys that no
+ * row of a tile sees may hold anything, codes and scales; one that some row of a tile sees and another does not has to be finite for the other's
+ * sake, its block's scale included.  The tile depends on the way that the call goes: 128 rows of a query head through 16 bits, 256 from the codes, and for few
+ * rows up to 16 of a key head (row i under its g query heads: i g to i g + g - 1).  So only rows 256 apart are sure not to meet.
  *   Scores, softmax and accumulators are fp32, outputs are rounded once.  Which of three ways a call goes follows from its sizes:
  *     few rows per key head: codes widen to half, which is exact (a row of bf16 queries is taken times a power of two), P is rounded to half;
  *     rows by the tile: the visible keys and values go through workspace_dev in the element type (values beyond its range: its largest number), P is

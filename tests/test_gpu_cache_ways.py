@@ -204,3 +204,34 @@ def test_factors_beyond_32_bits(scale, loud, way, b, h, hk, n, nk):
     assert (L.double() - count.log()).abs().max() <= 2.0 ** -17
     # P is one for every key: the mean of V in 32 bits (2^-19 of its absolute values), rounded once
     assert ((O.double() - want).abs() <= 2.0 ** -8 * want.abs() * 1.01 + 2.0 ** -18 * V.abs().amax()).all()
+
+
+@pytest.mark.parametrize("what", ["K", "V", "K_scale", "V_scale"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("way,h,n,nk,tile", [("rows", 8, 3, 705, 2), ("rows", 8, 3, 40001, 2), ("unpacked", 2, 600, 700, 128), ("tiles", 2, 600, 6000, 256)])
+def test_a_nan_that_some_rows_see(way, h, n, nk, tile, d, what):
+    """Causal rows: those that see a NaN code, or any of a block whose scale is 255, are NaN; those of other tiles keep every bit."""
+    block = 16
+    cache, _ = filled(37, 1, 1, nk, d, "bf16", "hnd", block)
+    q = queries(37, 1, h, n, d, "bf16", "hnd")
+    key = -(-(nk - n + (2 if n == 3 else 530)) // block) * block  # the first key of a block, at the position of row 530 or a little behind it
+    sees = key - (nk - n)                                         # the first row that sees it
+    apart = sees // tile * tile
+    assert 0 < apart <= sees < n
+    kw = dict(left=-1)
+    assert bsa.debug_cache_way(q, cache, **kw)[0] == way
+    for s in (cache.K_scale, cache.V_scale):  # the block is none of the largest scale, which the others' roundings go by
+        s.view(torch.uint8)[..., key // block] = 1
+    O, L = bsa.cache_forward(q, cache, **kw)
+    if what in ("K", "V"):
+        getattr(cache, what).view(torch.uint8)[0, 0, key, 5] = 127
+    else:
+        getattr(cache, what).view(torch.uint8)[0, 0, key // block] = 255
+    O2, L2 = bsa.cache_forward(q, cache, **kw)
+    assert torch.equal(O[:, :, :apart], O2[:, :, :apart]) and torch.equal(L[:, :, :apart], L2[:, :, :apart])
+    if what == "V":
+        assert O2[:, :, sees:, 5].isnan().all() and torch.equal(L, L2)
+        assert torch.equal(O[..., :5], O2[..., :5]) and torch.equal(O[..., 6:], O2[..., 6:])
+    else:
+        assert O2[:, :, sees:].isnan().all() and (what == "V_scale" or L2[:, :, sees:].isnan().all())
+    assert bsa.window_status() == 0

@@ -486,11 +486,15 @@ BSA_API bsa_status_t bsa_cache_read(const bsa_cache_t* cache, const bsa_cache_ro
  * sake, its block's scale included.  The tile depends on the way that the call goes: 128 rows of a query head through 16 bits, 256 from the codes, and for few
  * rows up to 16 of a key head (row i under its g query heads: i g to i g + g - 1).  So only rows 256 apart are sure not to meet.
  *   Scores, softmax and accumulators are fp32, outputs are rounded once.  Which of three ways a call goes follows from its sizes:
- *     few rows per key head: codes widen to half, which is exact (a row of bf16 queries is taken times a power of two), P is rounded to half;
+ *     few rows per key head: codes widen to half, which is exact (a row of bf16 queries is taken times a power of two); P, times V's scale relative to
+ *     U, is rounded to half: each key adds an error of 2^-31 U at most where half's steps stop shrinking;
  *     rows by the tile: the visible keys and values go through workspace_dev in the element type (values beyond its range: its largest number), P is
  *     rounded to that;
  *     or, where such rows leave SMs without work: K's codes as they are, an element of Q as two (half: three) numbers of 8 bits that are off by 2^-20 of
- *     the row's largest element at most, V's codes widened to half (off by 2^-32 of the largest value of the head's window at most), P rounded to half.
+ *     the row's largest element at most, V's codes widened to half relative to U (off by 2^-25 U at most), P rounded to half (weights below 2^-21 of the
+ *     row's sum are off by 2^-32 of it at most).
+ *   U is the largest of V's scales, 255 aside, of the blocks of which rows of the call see a key, whether the block's loudest token is seen or not and whatever
+ *   weight it has.  So a head's blocks far below U (few rows: 2^29, from the codes 2^15) lose bits that they have through 16 bits and when read back.
  *   workspace_dev: bsa_cache_workspace_bytes(desc, cache) bytes (0: none is needed; also for what the call refuses) on a 256-byte boundary, the call's
  *   own until its work on the stream is done.
  * Errors: as bsa_window_forward and bsa_cache_write; INVALID_ARG too where desc and cache disagree or the workspace is too small. */

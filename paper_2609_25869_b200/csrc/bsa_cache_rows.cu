@@ -19,7 +19,8 @@
 //   * e4m3 widens to half exactly.  Q comes as bf16 or half; a row of bf16 is multiplied by the power of two that takes its largest element to
 //     2^14 .. 2^15, and its elements down to 2^-31 of that one keep all their bits (what is lost below is at most 2^-39 of it).
 //   * Scales stay out of the products: scores are multiplied by their block's power of two; V's goes into the exponent of its keys' weights,
-//     relative to the largest so far of the warp's keys, which the accumulator is in units of.  P and its sum stay fp32 until P is rounded to half.
+//     relative to the largest so far of the warp's keys, which the accumulator is in units of.  P and its sum stay fp32 until P is rounded to half: 2^15 P times
+//     the relative scale, off by 2^-25 at most below half's normal numbers, so by 2^-40 of 448 times the largest scale for each key.
 // Eight sequences of 65536 keys, 8 key heads under 32, d = 128, one token: 178 us for 1.07 GB, 6.0 TB/s (94 % of what a copy has); six of 1111 to 115200
 // keys 129 us, 5.3 TB/s (token-major; the 16-bit cache 239); four with a window of 1024 keys 7 us, latencies.
 #include <cuda_fp16.h>

@@ -12,7 +12,7 @@
 //     blocks' scales relative to the largest.
 //   * V's codes widen to half on their way through the SM: two warps read the copied codes and write the swizzled tiles that the tensor instruction takes.
 //     A block's scale is applied there, relative to the largest scale of the call's window of that head: code 2^(s - s_max) is exact while a block is
-//     within 2^15 of the largest (below, it is off by 2^-32 of the largest value at most, half's smallest step).
+//     within 2^15 of the largest (below, it is off by 2^-25 of that scale at most, half of half's smallest step).
 //   * Where there are few row tiles and long windows, an item's keys are cut into parts, whose (m, l, O) a last kernel joins.
 //   warps 0-3 / 4-7 : softmax warpgroups (thread = row); tile t belongs to warpgroup t mod 2, and S and P buffer t mod 2 with it
 //   warp 8 : copies, K's scales   warp 9 : issuer (second CTA: tells the first what has landed)   warps 10, 11 : V converters

@@ -3,10 +3,11 @@ import pytest
 import torch
 
 from paper_2609_25869_b200 import bsa
+from tests import cache_bounds as B
 from tests import cache_reference as C
 from tests import window_reference as R
 from tests.test_gpu_cache import check_forward, check_write, filled, garbage, generator, parts, queries
-from tests.test_gpu_window import ints
+from tests.test_gpu_window import DT, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -235,3 +236,48 @@ def test_a_nan_that_some_rows_see(way, h, n, nk, tile, d, what):
     else:
         assert O2[:, :, sees:].isnan().all() and (what == "V_scale" or L2[:, :, sees:].isnan().all())
     assert bsa.window_status() == 0
+
+
+WAYS = [("rows", 1, 12, 3, 3, 700), ("rows", 2, 6, 3, 2, 40000), ("unpacked", 2, 6, 3, 300, 700), ("tiles", 1, 6, 3, 300, 6000), ("tiles", 5, 14, 14, 64, 6000)]
+
+
+def check_by_row(way, q, cache, **kw):
+    assert bsa.debug_cache_way(q, cache, **kw)[0] == way
+    O, L = bsa.cache_forward(q, cache, **kw)
+    (kc, ks), (vc, vs) = parts(cache)
+    wO, wL, tO, tL = B.forward(way, q, C.values(kc, ks, cache.block).cuda(), C.values(vc, vs, cache.block).cuda(), vs, cache.block, **kw)
+    R.assert_within(L, wL, tL, "LSE")
+    R.assert_within(O, wO, tO, "O")
+    assert bsa.window_status() == 0
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (64, "fp16"), (128, "bf16"), (128, "fp16")])
+@pytest.mark.parametrize("block", [16, 64])
+@pytest.mark.parametrize("way,b,h,hk,n,nk", WAYS)
+def test_quiet_rows_and_heads_beside_loud_ones(way, b, h, hk, n, nk, block, d, dtype):
+    """Each key head's K and V of another size, each row of Q, blocks as different as a louder token makes them: every row within what its own numbers allow."""
+    g = generator(38)
+    cache = bsa.cache_create(b, hk, nk, d, block=block)
+    by = lambda low, high, shape: torch.pow(2.0, torch.randint(low, high, shape, device="cuda", generator=g).float())  # noqa: E731
+    k, v = (torch.empty(b, hk, nk, d, device="cuda").normal_(0, 1, generator=g) for _ in range(2))
+    k *= by(-6, 2, (b, hk, 1, 1))
+    v *= by(-12, 8 if dtype == "bf16" else 3, (b, hk, 1, 1)) * torch.empty(b, hk, nk, 1, device="cuda").normal_(0, 1.2, generator=g).exp_()
+    bsa.cache_write(cache, k.to(DT[dtype]), v.to(DT[dtype]))
+    q = (queries(38, b, h, n, d, "bf16", "hnd").float() * by(-10, 3, (b, h, n, 1))).to(DT[dtype])
+    check_by_row(way, q, cache, left=-1, right=0)
+    check_by_row(way, q, cache, left=nk - n - 5, right=3, sinks=20)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (64, "fp16"), (128, "bf16"), (128, "fp16")])
+@pytest.mark.parametrize("block", [16, 64])
+@pytest.mark.parametrize("way,b,h,hk,n,nk", WAYS)
+def test_a_window_behind_a_louder_token(way, b, h, hk, n, nk, block, d, dtype):
+    """The window begins inside a block whose first token, seen by nobody, is far louder than all that is seen: its scale is the largest there is."""
+    g = generator(39)
+    cache = bsa.cache_create(b, hk, nk, d, block=block)
+    k, v = (torch.empty(b, hk, nk, d, device="cuda").normal_(0, 1, generator=g) for _ in range(2))
+    left = nk - n - 2 * block - 3  # so row 0, at nk - n, sees keys from 2 block + 3 on
+    k[:, :, 2 * block] *= 32
+    v[:, :, 2 * block] *= 2.0 ** (20 if dtype == "bf16" else 12)
+    bsa.cache_write(cache, k.to(DT[dtype]), v.to(DT[dtype]))
+    check_by_row(way, queries(39, b, h, n, d, dtype, "hnd"), cache, left=left)

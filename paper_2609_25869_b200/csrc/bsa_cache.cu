@@ -383,7 +383,7 @@ bsa_status_t forward_unpacked(WindowArgs a, const CacheGeom& g, const bsa_view_t
     a.g.q_start = p.q_start;
     a.g.kv_len = p.kv_len;
     const bsa_view_t k{p.K, p.k_batch, p.k_head, p.k_row}, v{p.V, p.v_batch, p.v_head, p.v_row};
-    return launch_window_tiles(a, Q, k, v, O, LSE, even, true, stream);
+    return cuda_status(launch_window_tiles(a, Q, k, v, O, LSE, even, true, stream), "bsa_cache_forward");
 }
 
 // What a description of attention and a cache have to agree in.
@@ -460,7 +460,7 @@ extern "C" bsa_status_t bsa_cache_read(const bsa_cache_t* c, const bsa_cache_row
 extern "C" int64_t bsa_cache_workspace_bytes(const bsa_window_desc_t* t, const bsa_cache_t* c) {
     WindowArgs a;
     CacheGeom g;
-    if (forward_args(t, c, &a, &g) != BSA_OK || window_device(&a) != BSA_OK) return 0;
+    if (forward_args(t, c, &a, &g) != BSA_OK || !window_tiles_fit(a) || window_device(&a) != BSA_OK) return 0;
     return workspace_of(a, way_of(a));
 }
 
@@ -477,7 +477,7 @@ extern "C" bsa_status_t bsa_cache_forward(const bsa_window_desc_t* t, const bsa_
         if (O->data == in || (void*)LSE == in) return BSA_ERR_INVALID_ARG;
     if ((st = window_device(&a)) != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
-    if ((int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
+    if (!window_tiles_fit(a)) return BSA_ERR_UNSUPPORTED;
     const Way way = way_of(a);
     const int64_t need = workspace_of(a, way);
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return BSA_ERR_INVALID_ARG;

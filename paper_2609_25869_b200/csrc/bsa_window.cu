@@ -584,7 +584,7 @@ cudaError_t launch_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view
     cfg.attrs = attr;
     cfg.numAttrs = behind ? 1 : 0;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, tq, tk, tv, p);
-    count_launch();
+    if (e == cudaSuccess) count_launch();
     return e;
 }
 
@@ -645,15 +645,15 @@ bsa_status_t window_device(WindowArgs* a) {
 // us, few rows / tiles: 65536 keys, 32 + 8 heads: 64 rows per key head, one sequence 75 / 375, eight 590 / 922; 96 rows, eight sequences
 // 982 / 936; 256 rows, one 305 to 365 / 375; 512 rows, one 580 / 375; 16384 keys, 8 x 16 heads, d = 64: 16 rows 84 / 97, 48 rows 131 / 105.
 // Over a short window the joins weigh more: 1024 keys, one sequence, 64 rows 10 / 19, 96 rows 18 / 14.
-bool window_takes_rows(const WindowArgs& a) {
+static bool takes_rows(const WindowArgs& a) {
     const int64_t window = (int64_t)a.g.left + a.g.right + a.g.sinks + a.g.N, most = (window < a.g.N_kv ? window : a.g.N_kv) > 4096 ? 256 : 64;
     const int64_t rows = (int64_t)a.g.N * a.g.group, blocks = (rows + 15) / 16 * a.g.batch * a.g.heads_kv;
     const int64_t tiles = (a.g.N + kWinT - 1) / kWinT, rounds = (tiles * a.g.batch * a.g.heads + a.num_sms - 1) / a.num_sms;
     return rows <= most && blocks <= rounds * a.num_sms;
 }
 
-bsa_status_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
-                                 float* LSE, bool even, bool behind, cudaStream_t stream) {
+cudaError_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
+                                float* LSE, bool even, bool behind, cudaStream_t stream) {
     Params p = {};
     p.g = a.g;
     p.O = static_cast<uint16_t*>(O.data);
@@ -663,17 +663,11 @@ bsa_status_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.withhold = window_withhold();
     const int n_qt = (a.g.N + kWinT - 1) / kWinT;
-    if ((int64_t)n_qt * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
     p.order = ItemOrder(n_qt, even ? 0 : cut_tiles(a.g, n_qt), a.g.batch * a.g.heads);
     p.heads = Divisor(a.g.heads);
     p.group = Divisor(a.g.group);
-    const cudaError_t e = a.d == 64 ? (a.f16 ? launch_rows<64, true>(a, Q, K, V, p, behind, stream) : launch_rows<64, false>(a, Q, K, V, p, behind, stream))
-                                    : (a.f16 ? launch_rows<128, true>(a, Q, K, V, p, behind, stream) : launch_rows<128, false>(a, Q, K, V, p, behind, stream));
-    if (e != cudaSuccess) {
-        set_cuda_err(e, "bsa_window_forward");
-        return BSA_ERR_CUDA;
-    }
-    return BSA_OK;
+    return a.d == 64 ? (a.f16 ? launch_rows<64, true>(a, Q, K, V, p, behind, stream) : launch_rows<64, false>(a, Q, K, V, p, behind, stream))
+                     : (a.f16 ? launch_rows<128, true>(a, Q, K, V, p, behind, stream) : launch_rows<128, false>(a, Q, K, V, p, behind, stream));
 }
 
 }  // namespace bsa
@@ -692,9 +686,9 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
     if (st == BSA_OK) st = window_device(&a);
     if (st != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
-    if ((int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads > INT_MAX / 2) return BSA_ERR_UNSUPPORTED;
-    if (!window_takes_rows(a)) return launch_window_tiles(a, *Q, *K, *V, *O, LSE, false, false, stream);
-    const cudaError_t e = launch_window_rows(a, *Q, *K, *V, *O, LSE, stream);
+    if (!window_tiles_fit(a)) return BSA_ERR_UNSUPPORTED;
+    const cudaError_t e = takes_rows(a) ? launch_window_rows(a, *Q, *K, *V, *O, LSE, stream)
+                                        : launch_window_tiles(a, *Q, *K, *V, *O, LSE, false, false, stream);
     if (e != cudaSuccess) {
         set_cuda_err(e, "bsa_window_forward");
         return BSA_ERR_CUDA;

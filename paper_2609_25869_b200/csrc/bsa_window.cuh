@@ -182,12 +182,12 @@ bsa_status_t window_args(const bsa_window_desc_t* t, WindowArgs* a);
 bsa_status_t window_device(WindowArgs* a);
 // Whether every row of a view with these sizes lies on a 32-byte boundary.
 bool view_is_wide(const bsa_view_t& v, int64_t batch, int64_t heads, int64_t rows);
-// Whether the kernel for few rows takes a call (all but the device filled in before: window_device), or the one for tiles of rows.
-bool window_takes_rows(const WindowArgs& a);
+// Whether a call has no more row tiles than the kernels count.
+inline bool window_tiles_fit(const WindowArgs& a) { return (int64_t)((a.g.N + kWinT - 1) / kWinT) * a.g.batch * a.g.heads <= INT_MAX / 2; }
 // `even`: the rows' windows are about equally long (else their lengths follow from the sizes).  `behind`: the kernel in front on the stream, which writes K, V,
 // starts and lengths, lets its dependents start early (grid_launch_dependents) and is waited for on the device.
-bsa_status_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
-                                 float* LSE, bool even, bool behind, cudaStream_t stream);
+cudaError_t launch_window_tiles(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
+                                float* LSE, bool even, bool behind, cudaStream_t stream);
 // Forward for few rows (bsa_window_rows.cu).
 cudaError_t launch_window_rows(const WindowArgs& a, const bsa_view_t& Q, const bsa_view_t& K, const bsa_view_t& V, const bsa_view_t& O,
                                float* LSE, cudaStream_t stream);

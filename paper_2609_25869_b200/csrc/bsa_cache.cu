@@ -473,8 +473,9 @@ extern "C" bsa_status_t bsa_cache_forward(const bsa_window_desc_t* t, const bsa_
     bsa_status_t st = forward_args(t, c, &a, &g);
     if (st != BSA_OK) return st;
     if (view_overlaps(*O, t->batch, t->heads, t->N, t->d)) return BSA_ERR_INVALID_ARG;
-    for (const void* in : {c->K.data, c->V.data, (void*)c->K_scale, (void*)c->V_scale})
-        if (O->data == in || (void*)LSE == in) return BSA_ERR_INVALID_ARG;
+    for (const void* in : {c->K.data, c->V.data, (void*)c->K_scale, (void*)c->V_scale, Q->data})
+        if ((O->data == in && in != Q->data) || LSE == in || (workspace && workspace == in)) return BSA_ERR_INVALID_ARG;  // (O may take the place of Q)
+    if (LSE == O->data || (workspace && (workspace == O->data || workspace == LSE))) return BSA_ERR_INVALID_ARG;
     if ((st = window_device(&a)) != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);
     if (!window_tiles_fit(a)) return BSA_ERR_UNSUPPORTED;

@@ -682,7 +682,9 @@ extern "C" bsa_status_t bsa_window_forward(const bsa_window_desc_t* t, const bsa
         return BSA_ERR_INVALID_ARG;
     WindowArgs a;
     bsa_status_t st = window_args(t, &a);
-    if (st == BSA_OK && (view_overlaps(*O, t->batch, t->heads, t->N, t->d) || O->data == K->data || O->data == V->data)) st = BSA_ERR_INVALID_ARG;
+    if (st == BSA_OK && (view_overlaps(*O, t->batch, t->heads, t->N, t->d) || O->data == K->data || O->data == V->data ||
+                         LSE == Q->data || LSE == K->data || LSE == V->data || LSE == O->data))
+        st = BSA_ERR_INVALID_ARG;
     if (st == BSA_OK) st = window_device(&a);
     if (st != BSA_OK) return st;
     const cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_v);

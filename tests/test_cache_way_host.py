@@ -1,10 +1,11 @@
-"""CPU: what the query for the 8-bit cache's way refuses."""
+"""CPU: what the query for the 8-bit cache's way refuses, and places of LSE and of the workspace that a forward refuses."""
 import ctypes
 
 import pytest
 
 from paper_2609_25869_b200 import bsa
-from tests.test_cache_host import INVALID, UNSUPPORTED, _built, cache, window  # noqa: F401
+from tests import test_window_host as W
+from tests.test_cache_host import FAKE, INVALID, UNSUPPORTED, _built, cache, forward, window  # noqa: F401
 
 
 def way(w=None, c=None):
@@ -26,3 +27,20 @@ def test_caches_that_a_forward_refuses_and_missing_places():
     assert L.bsa_debug_cache_way(window(), cache(), ctypes.byref(n), None) == INVALID
     assert L.bsa_debug_cache_way(None, cache(), ctypes.byref(n), ctypes.byref(n)) == INVALID
     assert L.bsa_debug_cache_way(window(), None, ctypes.byref(n), ctypes.byref(n)) == INVALID
+
+
+def test_an_lse_or_a_workspace_in_the_place_of_another_tensor():
+    """Outputs that begin where another tensor of the call does are refused (Q 1, O 2, LSE 3, workspace 4, codes 5 and 6, scales 7 and 8)."""
+    for at in (1, 2):
+        assert forward(lse=at * FAKE) == INVALID
+    for at in (1, 2, 3, 5, 6, 7, 8):
+        assert forward(ws=at * FAKE) == INVALID
+    q, k, v, o = (W.view(i * FAKE) for i in (1, 2, 3, 4))
+    for at in (1, 2, 3, 4):
+        assert W.forward(window(), q, k, v, o, at * FAKE) == INVALID
+    for args in ((q, k, v, o), (q, k, v, q)):  # (O may take the place of Q)
+        assert W.forward(window(), *args, 5 * FAKE) != INVALID
+
+
+def test_a_forward_without_such_overlaps_is_not_refused_on_the_host():
+    assert forward() != INVALID and forward(o=W.view(FAKE)) != INVALID

@@ -495,6 +495,9 @@ BSA_API bsa_status_t bsa_cache_read(const bsa_cache_t* cache, const bsa_cache_ro
  *     row's sum are off by 2^-32 of it at most).
  *   U is the largest of V's scales, 255 aside, of the blocks of which rows of the call see a key, whether the block's loudest token is seen or not and whatever
  *   weight it has.  So a head's blocks far below U (few rows: 2^29, from the codes 2^15) lose bits that they have through 16 bits and when read back.
+ *   The way, the workspace and the grids go by the tensors' sizes, not by kv_len: a sequence that fills little of a large cache is better given as a view of its
+ *   first tokens (N and N_kv smaller, the strides as they are).  Through 16 bits the workspace is as large as the visible keys and values in the element type:
+ *   those of the longest window and the first tokens, or, without a left limit, of all N_kv (twice the cache's own bytes).
  *   workspace_dev: bsa_cache_workspace_bytes(desc, cache) bytes (0: none is needed; also for what the call refuses) on a 256-byte boundary, the call's
  *   own until its work on the stream is done.
  * Errors: as bsa_window_forward and bsa_cache_write; INVALID_ARG too where desc and cache disagree or the workspace is too small. */

@@ -740,7 +740,8 @@ def cache_read(cache: Cache, N: int, *, start=None, count=None, dtype=None, K=No
 def cache_forward(Q, cache: Cache, *, left: int, right: int = 0, sinks: int = 0, q_start=None, kv_len=None, scale: float = 0.0, O=None,
                   LSE=None, stream=None):
     """``bsa_cache_forward``: ``window_forward`` of Q (the cache's layout) over the keys and values of a cache; arguments and results as there.
-    A workspace, where one is needed, comes from torch's allocator."""
+    A workspace, where one is needed, comes from torch's allocator.  Its size and the work's layout go by the cache's N, not by ``kv_len``: for sequences
+    that fill little of a large cache use a ``Cache`` of views of its first tokens."""
     nhd = LAYOUTS[cache.layout] == 1
     dt, dev = _tensor_of(Q, "Q")
     if dev != cache.device:

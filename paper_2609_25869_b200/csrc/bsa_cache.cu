@@ -1,13 +1,14 @@
 // Writing the 8-bit cache and reading it back: one pass over the data, bound by memory.
 //
-// Written: a block of tokens of one head, of K or of V, is the work of up to 256 threads.  All of its new elements are in registers before the first is
-// rounded (32 elements of 16 bits to a thread and four such loads under way), so that the block's largest is found without a second look at
-// memory: 2 bytes read and 1 written an element.  With the amplitude a = max |x| of the finite elements the scale is 2^e,
+// Written: a block of tokens of one head, of K or of V, is the work of up to 256 threads.  All of its new elements are loaded before the first is rounded (64 of
+// 16 bits to a thread, in four loads under way at once; 32 in two for blocks of 16 tokens at d = 64), so that the block's largest is found without a second
+// look at memory: 2 bytes read and 1 written an element.  (They are 32 of the 64 registers that 1024 threads of an SM have each; all but the shortest
+// block's kernels spill 50 to 100 bytes of the rest.)  With the amplitude a = max |x| of the finite elements the scale is 2^e,
 //     e = ceil(log2(a / 448)),  from the bits of a: 448 = 1.75 * 2^8, so the exponent of a, less 8, and one more where the
 // mantissa is above 1.75.  code = round(x 2^-e): the product is exact, so this is the one rounding.  A block that holds tokens in front of
 // the new ones keeps its scale where that is large enough; else those tokens' codes take the larger scale's (x 2^(old - new), again exact
 // but for subnormals).
-// Read: 16 codes to a thread, 32 bytes out.
+// Read: four times 16 codes to a thread, 32 bytes out for each.
 // 115200 tokens, 24 heads, d = 128, blocks of 64 (2.1 GB each way): written in 329 us, 6.45 TB/s, read back in 311, 6.8; token-major 337 and 325; 23400 tokens of
 // 12 heads 37 and 35; one token of four sequences, 8 heads 3.1 and 2.1.
 #include <cuda_fp16.h>
@@ -322,6 +323,9 @@ bsa_status_t cuda_status(cudaError_t e, const char* where) {
 // parts where the rows leave SMs without work.  By what they would take, in us: few rows, 1.0 (d = 64: 0.7) of an SM for each 16 rows of a key head and 128 keys;
 // in 16 bits, 6 bytes an element at 6.4 TB/s for the pass and, whole rounds of items over the SMs, 0.97 (0.82) for 128 rows of a query head and 128 keys;
 // from the codes, cache_tiles_time.
+// The constants are from calls of one sequence, bf16, head-major, without a window and with all scales equal (376 shapes: 7 of them 16 to 36 % over their best way,
+// the rest closer).  Nothing stands for half's third piece of Q, nor for scales that differ, with which the kernel that reads the codes takes 12 to 20 % longer; and
+// the tensors' sizes stand for the lengths, which only the device knows.
 // Rows of the workspace's K and V: the first tokens (in whole tiles) and the longest window that the queries see between them, or all.
 struct Unpacked {
     int64_t rows;
